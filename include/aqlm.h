@@ -84,7 +84,7 @@ enum aqlm_status {
   AQLM_ERR_UNSUPPORTED = 3, /* (M, B, g) outside the supported set */
   AQLM_ERR_ALIGN = 4,       /* a pointer breaks the alignment rule above */
   AQLM_ERR_HIP = 5,         /* the HIP runtime reported an error */
-  AQLM_ERR_WORKSPACE = 6,   /* aqlm_gemm: workspace smaller than aqlm_gemm_workspace_bytes */
+  AQLM_ERR_WORKSPACE = 6,   /* workspace smaller than the entry point's *_workspace_bytes */
   AQLM_ERR_SCRATCH = 7,     /* aqlm_gemm_noalloc: the product needs more than its fixed scratch */
   AQLM_ERR_TIMEOUT = 8      /* aqlm_gemv_step_status: a level barrier gave up waiting */
 };
@@ -484,6 +484,164 @@ typedef struct aqlm_sorted_problem {
  * the last bits (the row ranges differ). */
 int aqlm_gemv_sorted_grouped(const aqlm_sorted_problem* problems, int32_t count, int32_t M, int32_t B, int32_t g,
                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * What a transformer block and a decode step need between the products above:
+ * rotary positions and head norms with their gradients, a paged key/value cache,
+ * attention over it, and constraints on logits.
+ *
+ * Activations are [tokens][heads][head_dim] with strides in elements, the
+ * elements of a head contiguous (views of a fused projection's output need no
+ * copy).  Types: AQLM_F16, AQLM_BF16 and, where stated, AQLM_F32; sums, norms and
+ * softmax statistics are fp32, results are rounded once.  `tokens` of 0 is a
+ * call without work.  Values in device arrays (positions, lengths, page numbers)
+ * cannot be checked on the host: whatever they hold, nothing is read or
+ * written outside the arrays, and the text says what the results then are. */
+
+enum aqlm_dtype { AQLM_F16 = 0, AQLM_BF16 = 1, AQLM_F32 = 2 };
+
+/* One activation [tokens][heads][head_dim]. */
+typedef struct aqlm_heads {
+  void* data; /* read only where it is an input */
+  int64_t token_stride;
+  int64_t head_stride;
+  int32_t heads;
+} aqlm_heads;
+
+/* A rotation, and the norms before it (weights NULL: no norm). */
+typedef struct aqlm_rotation {
+  const float* table; /* [rows][rot / 2][2]: cos, sin (aqlm_rotary_table); NULL with rot = 0 */
+  int64_t rows;       /* positions that the table has */
+  int32_t rot;        /* elements of a head that are rotated: its first ones; even, 0 .. head_dim */
+  int32_t interleaved; /* pairs (2i, 2i + 1) instead of (i, i + rot / 2) */
+  const void* q_weight; /* [head_dim], of the activations' type */
+  const void* k_weight;
+  float eps;
+} aqlm_rotation;
+
+/* table[p][i] = scale * (cos, sin)(p * inv_freq[i]), computed in 64 bits and
+ * rounded once.  inv_freq: [half] fp64 on the device. */
+int aqlm_rotary_table(const double* inv_freq, int64_t rows, int32_t half, double scale, float* table, void* stream);
+
+/* q_out, k_out = the heads of q and k, normalised (y = x rsqrt(mean(x^2) + eps)
+ * w) where there is a weight, then rotated by their token's position.  positions:
+ * [tokens] int32; a token whose position the table does not have gives NaN.  The
+ * outputs may be the inputs (same addresses and strides) but not overlap them
+ * otherwise.  head_dim 1 .. 1024.  Heads of up to 512 elements in multiples of 8,
+ * with rot a multiple of 16 (interleaved: of 4), all addresses and strides
+ * multiples of 16 bytes, take the vectorised path; the rest a general one. */
+int aqlm_rope(const aqlm_heads* q, const aqlm_heads* k, const aqlm_heads* q_out, const aqlm_heads* k_out,
+              int32_t dtype, int64_t tokens, int32_t head_dim, const int32_t* positions, const aqlm_rotation* r,
+              void* stream);
+
+/* Gradients of aqlm_rope: dq, dk are those of its outputs, q, k what it read
+ * (needed, and read, only where there is a norm), gq, gk those of its inputs, and
+ * gq_weight, gk_weight (fp32 [head_dim], written, not added to) those of the
+ * norms' weights.  gq may be dq and gk dk.  Sums over tokens and heads are taken in a
+ * fixed order.  workspace: aqlm_rope_backward_workspace_bytes(head_dim) where
+ * there is a norm, 16-byte aligned, any contents. */
+size_t aqlm_rope_backward_workspace_bytes(int32_t head_dim);
+int aqlm_rope_backward(const aqlm_heads* dq, const aqlm_heads* dk, const aqlm_heads* q, const aqlm_heads* k,
+                       const aqlm_heads* gq, const aqlm_heads* gk, float* gq_weight, float* gk_weight, int32_t dtype,
+                       int64_t tokens, int32_t head_dim, const int32_t* positions, const aqlm_rotation* r,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* A paged cache and the batch that uses it.  Position p of sequence b is at slot
+ * p % page_size of page block_table[b][p / page_size].  kv_lens[b] counts the
+ * sequence's keys WITH its new tokens, which are the tokens cu_new[b] ..
+ * cu_new[b + 1] of the activations (cu_new[0] = 0, cu_new[seqs] = tokens) and its
+ * last positions; a sequence may have no new tokens, and one without keys
+ * (kv_lens 0) is an idle slot of a batch of fixed size.  Strides in elements. */
+typedef struct aqlm_paged_cache {
+  void* k;
+  void* v;
+  int64_t k_page_stride, k_slot_stride, k_head_stride;
+  int64_t v_page_stride, v_slot_stride, v_head_stride;
+  int64_t pages;
+  const int32_t* block_table; /* [seqs][table_width] */
+  int64_t table_stride;
+  const int32_t* kv_lens; /* [seqs] */
+  const int32_t* cu_new;  /* [seqs + 1] */
+  int32_t table_width;
+  int32_t seqs;      /* up to AQLM_MAX_SEQS */
+  int32_t page_size; /* a power of two */
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t dtype;
+} aqlm_paged_cache;
+
+#define AQLM_MAX_SEQS 4096
+
+/* Norms and rotation as aqlm_rope on the way into the cache: q_out gets the
+ * queries, the pages the keys and (unchanged) the values of the new tokens.  A
+ * token's position is its place in its sequence.  q and q_out may be NULL.  r
+ * may have rot = 0 (no rotation).  A token without a place (position below 0)
+ * gives zeros in q_out and no keys; one whose page the table or the cache does
+ * not have is not written to it; a position that the rotation's table does not
+ * have gives NaN.  Types: all three. */
+int aqlm_paged_append(const aqlm_heads* q, const aqlm_heads* k, const aqlm_heads* v, const aqlm_heads* q_out,
+                      const aqlm_paged_cache* cache, int64_t tokens, const aqlm_rotation* r, void* stream);
+
+/* out[t][e] = sum_j softmax_j(scale <q[t][e], K[j]>) V[j] over the keys of the
+ * token's sequence, query head e reading kv head e / (heads / kv_heads).  causal:
+ * keys up to the token's own position only; window > 0: only the last `window`
+ * positions up to the token's own (those after it, without causal, are not
+ * limited).  A row without keys gives zeros.  Keys that a row does not see
+ * take no part in it, whatever they hold.  lse (NULL or fp32 [tokens][heads]): the
+ * logarithm of the softmax's denominator, -inf for a row without keys.
+ *   max_new: the most new tokens of a sequence, if known (0: unknown); it
+ *   chooses the kernel, not the result: up to 16 rows (new tokens x heads per kv
+ *   head) of a sequence are bound by the cache's bytes, more by the products.
+ *   Pages outside the cache are read as its first or last page; lengths past the
+ *   block table's are cut to it.
+ *   workspace: aqlm_paged_attention_workspace_bytes(head_dim) bytes, 16-byte
+ *   aligned, whose first AQLM_ATTENTION_COUNTER_BYTES are zero before its first
+ *   use.  Every launch leaves them zero, so one workspace serves any
+ *   calls on one stream; calls that may overlap need one each.
+ * Types: AQLM_F16 and AQLM_BF16 (q, out and the cache alike); head_dim a multiple
+ * of 8 up to 256; addresses and strides multiples of 16 bytes.  Deterministic.
+ * The work is divided over the chip on the device, from kv_lens and cu_new: a
+ * captured launch serves any lengths. */
+#define AQLM_ATTENTION_COUNTER_BYTES 16384
+size_t aqlm_paged_attention_workspace_bytes(int32_t head_dim);
+int aqlm_paged_attention(const aqlm_heads* q, const aqlm_heads* out, float* lse, const aqlm_paged_cache* cache,
+                         int64_t tokens, int64_t max_new, float scale, int32_t causal, int32_t window,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Constraints on logits [rows][vocab]; each part is left out where its pointer is
+ * NULL.  Row strides in elements (of mask: words).
+ *   tokens [rows][history]: the row's tokens so far, of which the first
+ *   prompt_lens[row] (NULL: none) are its prompt and the rest, up to
+ *   token_lens[row], its output; ids outside the vocabulary are left out.
+ *   l = l > 0 ? l / repetition : l * repetition   for every token among them,
+ *   l = l - frequency * count - presence          for those of the output,
+ *   l = l + bias_values[i]                        for each bias_ids[row][i] = token
+ *                                                 (negative ids: no entry),
+ *   l = -inf                                      where bit token % 32 of
+ *                                                 mask[row][token / 32] is not set,
+ * in this order, in fp32, rounded once.  repetition, frequency, presence: [rows]
+ * fp32.  Several biases of a token are added in the order of the list.  out may be
+ * the logits (same address and stride).  Limits: 65535 rows, history below 2^20,
+ * 2047 biases. */
+typedef struct aqlm_logit_rules {
+  const int32_t* tokens;
+  const int32_t* token_lens;
+  const int32_t* prompt_lens;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  const uint32_t* mask;
+  int64_t token_stride;
+  int64_t bias_stride;
+  int64_t mask_stride;
+  int32_t history;
+  int32_t biases;
+} aqlm_logit_rules;
+
+int aqlm_process_logits(const void* logits, int64_t logits_stride, void* out, int64_t out_stride, int32_t dtype,
+                        int64_t rows, int64_t vocab, const aqlm_logit_rules* rules, void* stream);
 
 /* Static text for a status code (never NULL). */
 const char* aqlm_status_string(int status);

@@ -18,7 +18,10 @@ Eq. 2 and Fig. 3).  This package exposes the three operations of the C ABI in
   one persistent launch;
 - :class:`SortedCodes` - a chunk-sorted copy of the codes of the large-codebook
   formats (1x15, 1x16, 2x15, 2x16) whose matrix-vector product serves every
-  code from a codebook chunk held on chip.
+  code from a codebook chunk held on chip;
+- the operators around these products in a block and in a decode step
+  (``block.py``): :func:`rotary_table`, :func:`rope`, :func:`rope_backward`,
+  :func:`paged_append`, :func:`paged_attention`, :func:`process_logits`.
 
 Every computation runs in the hand-written HIP kernels of
 ``libaqlm_mi355x.so``; this module only marshals arguments.
@@ -43,7 +46,8 @@ from ._lib import AqlmError, status_string  # noqa: F401
 __all__ = ["dequantize", "gemv", "gemv_grouped", "gemm_small_batch", "gemm_workspace_bytes", "gemm", "backward",
            "beam_search", "DecodeStep", "SortedCodes", "gemv_sorted_grouped",
            "AqlmError",
-           "status_string", "layer_args", "packed_layer_args"]
+           "status_string", "layer_args", "packed_layer_args", "rotary_table", "rope", "rope_backward", "paged_append",
+           "paged_attention", "attention_workspace", "process_logits"]
 
 
 # The current stream's handle without building a torch.cuda.Stream (0.1 us
@@ -493,3 +497,7 @@ def gemv_sorted_grouped(problems, *, workspace=None, stream=None):
     st = lib.aqlm_gemv_sorted_grouped(arr, len(problems), first.M, first.B, first.g, workspace.data_ptr(),
                                       workspace.numel() * workspace.element_size(), _stream_handle(stream))
     _check(st, "aqlm_gemv_sorted_grouped")
+
+
+from .block import (  # noqa: E402,F401  (after the helpers it uses)
+    attention_workspace, paged_append, paged_attention, process_logits, rope, rope_backward, rotary_table)

@@ -1,0 +1,359 @@
+// Attention over a paged key/value cache: arguments, the division of the work
+// over workgroups, and the joining of split rows, shared by the kernel for a few
+// rows per sequence (attention_step.hip) and the one for many
+// (attention_chunk.hip).
+//
+//   out[t][e] = sum_j p_j V[j] / sum_j p_j,   p_j = exp(scale <q[t][e], K[j]>)
+//
+// over the keys j that token t may see, with the running maximum taken out of
+// the exponents.  The query heads e of one kv head h share its keys, so a
+// sequence's new tokens and those heads are packed into rows (row r: token
+// r / group, head h * group + r % group) and the rows are cut into units of R.
+// A unit reads the key tiles between the first key that its first token sees
+// and the last one that its last token sees.
+//
+// Division of the work.  Lengths live on the device (a captured launch serves
+// any lengths), so every workgroup adds up the tiles of all units by itself,
+// and takes an equal, contiguous share of the sequence (kv head, sequence,
+// unit, tile).  A share may hold many short units, or a piece of a long one.  A
+// workgroup that holds a whole unit writes its rows.  The pieces of a split one
+// (unnormalised sums, maximum, denominator, all fp32) go to the workspace, where
+// a workgroup has two places: one for the unit that it continues, one for the
+// unit that it begins.  The workgroup that finishes a unit's last piece (a
+// counter per beginning workgroup) adds the pieces up in the order of the
+// keys, so results do not depend on the order in which workgroups run, and sets
+// the counter back to zero for the next launch.
+#pragma once
+
+#include <limits.h>
+
+#include "common.h"
+
+namespace aqlm {
+
+typedef float f16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
+typedef float f2_t __attribute__((ext_vector_type(2)));
+typedef short s4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kAttnMaxSeqs = 4096;
+
+struct AttnArgs {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* out;
+  float* lse;  // [tokens][kv_heads * group] or null
+  const int32_t* block_table;
+  const int32_t* kv_lens;
+  const int32_t* cu_new;
+  uint32_t* counters;  // [grid]
+  float* parts;        // [2 * grid] places
+  int64_t q_token, q_head, out_token, out_head;  // strides, in elements
+  int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
+  int64_t table_stride;
+  int32_t tokens, seqs, kv_heads, group, head_dim;
+  int32_t pages, page_shift, table_width;
+  int32_t causal, window;
+  // |scale| * log2(e), above 0 (so that a masked score stays -inf under it); the
+  // queries are read as (q & q_keep) ^ q_flip, which brings in the sign, and a
+  // scale of 0 as queries of 0.
+  float scale_log2;
+  uint32_t q_keep, q_flip;
+};
+
+__device__ __forceinline__ u32x4_t attn_query(const AttnArgs& a, const u32x4_t& q) {
+  u32x4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (q[i] & a.q_keep) ^ a.q_flip;
+  return r;
+}
+
+// A sequence's new tokens and keys, whatever the device arrays hold: no read
+// goes past the arrays.
+struct AttnSeq {
+  int first, count, keys;
+};
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int b) {
+  AttnSeq s;
+  s.first = min(max(a.cu_new[b], 0), a.tokens);
+  s.count = min(max(a.cu_new[b + 1], s.first), a.tokens) - s.first;
+  const int64_t room = (int64_t)a.table_width << a.page_shift;
+  s.keys = (int)min((int64_t)max(a.kv_lens[b], 0), room);
+  return s;
+}
+
+// Keys [lo, hi) that token i of a sequence sees (hi <= lo: none).
+__device__ __forceinline__ void attn_visible(const AttnArgs& a, const AttnSeq& s, int i, int& lo, int& hi) {
+  const int pos = s.keys - s.count + i;
+  hi = a.causal ? min(pos + 1, s.keys) : s.keys;
+  lo = a.window > 0 ? (int)max((int64_t)0, (int64_t)pos - a.window + 1) : 0;
+}
+
+// Key tiles of KT of unit t: the first one and their number (at least one, so
+// that some workgroup writes the rows of a unit without keys).
+template <int R, int KT>
+__device__ __forceinline__ int attn_tiles(const AttnArgs& a, const AttnSeq& s, int t, int& tile0, int& k0, int& k1) {
+  int lo, hi, x;
+  attn_visible(a, s, (int)((uint32_t)(t * R) / (uint32_t)a.group), lo, x);
+  attn_visible(a, s, min(s.count - 1, (int)((uint32_t)(t * R + R - 1) / (uint32_t)a.group)), x, hi);
+  k0 = lo;
+  k1 = max(hi, lo);
+  tile0 = lo / KT;
+  return hi > lo ? (hi + KT - 1) / KT - tile0 : 1;
+}
+
+__device__ __forceinline__ int attn_units(const AttnArgs& a, const AttnSeq& s, int R) {
+  return (int)(((int64_t)s.count * a.group + R - 1) / R);
+}
+
+// Inclusive prefix sum over the wave.
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+struct AttnShare {
+  int per_head;    // tiles of one kv head over all sequences
+  int64_t total;   // tiles of all heads
+  int64_t quota;   // tiles of a workgroup's share
+  int64_t begin, end;
+};
+
+// Fills `prefix` (LDS, seqs + 1 ints: tiles of one kv head before each
+// sequence; `scratch`: 2 * waves ints) and returns this workgroup's share.
+// `pieces`: the most pieces that a unit is split into.
+template <int R, int KT, int WAVES>
+__device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, int* prefix, int* scratch, int wg, int grid,
+                                                int pieces) {
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  int most = 1;
+  if (a.seqs <= WAVES) {  // few sequences, perhaps of many units: a wave for each
+    for (int b = wave; b < a.seqs; b += WAVES) {
+      const AttnSeq s = attn_seq(a, b);
+      const int units = attn_units(a, s, R);
+      int sum = 0, tile0, k0, k1;
+      for (int t = lane; t < units; t += kWave) {
+        const int n = attn_tiles<R, KT>(a, s, t, tile0, k0, k1);
+        sum += n;
+        most = max(most, n);
+      }
+      sum = wave_scan(sum);
+      if (lane == kWave - 1) prefix[b + 1] = sum;
+    }
+  } else {
+    for (int b = tid; b < a.seqs; b += WAVES * kWave) {
+      const AttnSeq s = attn_seq(a, b);
+      const int units = attn_units(a, s, R);
+      int sum = 0, tile0, k0, k1;
+      for (int t = 0; t < units; ++t) {
+        const int n = attn_tiles<R, KT>(a, s, t, tile0, k0, k1);
+        sum += n;
+        most = max(most, n);
+      }
+      prefix[b + 1] = sum;
+    }
+  }
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d /= 2) most = max(most, __shfl_xor(most, d));
+  if (lane == 0) scratch[wave] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) most = max(most, scratch[w]);
+  // every wave scans the whole array in steps of 64; wave 0 writes it back
+  if (wave == 0) {
+    int before = 0;
+    if (lane == 0) prefix[0] = 0;
+    for (int b = 0; b < a.seqs; b += kWave) {
+      const int i = b + lane;
+      const int v = wave_scan(i < a.seqs ? prefix[i + 1] : 0) + before;
+      if (i < a.seqs) prefix[i + 1] = v;
+      before = __shfl(v, kWave - 1);
+    }
+  }
+  __syncthreads();
+  AttnShare h;
+  h.per_head = prefix[a.seqs];
+  h.total = (int64_t)h.per_head * a.kv_heads;
+  h.quota = max((h.total + grid - 1) / grid, (int64_t)((most + pieces - 1) / pieces));
+  h.quota = max(h.quota, (int64_t)1);
+  h.begin = min(h.total, h.quota * wg);
+  h.end = min(h.total, h.begin + h.quota);
+  return h;
+}
+
+// One unit of a share: where it is, and the part of its tiles that the share holds.
+struct AttnUnit {
+  AttnSeq s;
+  int b, head, t;
+  int tile0, tiles, k0, k1;
+  int from, to;         // tiles [from, to) of the unit are in the share
+  int64_t start;        // the unit's first tile in the sequence of all tiles
+};
+
+// The unit that holds tile `at` of the sequence of all tiles.  Uniform over the
+// workgroup; every wave finds it by itself.
+template <int R, int KT>
+__device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare& h, const int* prefix, int64_t at) {
+  const int lane = threadIdx.x & (kWave - 1);
+  AttnUnit u;
+  u.head = (int)(at / h.per_head);
+  const int rem = (int)(at - (int64_t)u.head * h.per_head);
+  // the last sequence with prefix <= rem (empty sequences have none of the tiles)
+  int b = 0;
+  for (int i = 0; i < a.seqs; i += kWave) {
+    const uint64_t le = __ballot(i + lane < a.seqs && prefix[i + lane] <= rem);
+    if (le == 0) break;
+    b = i + 63 - __builtin_clzll(le);
+  }
+  u.b = __builtin_amdgcn_readfirstlane(b);
+  u.s = attn_seq(a, u.b);
+  int left = rem - prefix[u.b];
+  const int units = attn_units(a, u.s, R);
+  int tile0, k0, k1, t = 0;
+  if (units > 1) {
+    int before = 0;
+    for (int i = 0; i < units; i += kWave) {
+      const int n = i + lane < units ? attn_tiles<R, KT>(a, u.s, i + lane, tile0, k0, k1) : 0;
+      const int incl = wave_scan(n) + before;
+      const uint64_t gt = __ballot(incl > left);
+      if (gt != 0) {
+        const int l = __builtin_ctzll(gt);
+        t = i + l;
+        before = l > 0 ? __shfl(incl, l - 1) : before;
+        break;
+      }
+      before = __shfl(incl, kWave - 1);
+    }
+    left -= before;
+  }
+  u.t = __builtin_amdgcn_readfirstlane(t);
+  u.tiles = attn_tiles<R, KT>(a, u.s, u.t, u.tile0, u.k0, u.k1);
+  u.from = __builtin_amdgcn_readfirstlane(left);
+  u.start = at - u.from;
+  u.to = (int)min((int64_t)u.tiles, (int64_t)u.from + (h.end - at));
+  return u;
+}
+
+// The page of key j of sequence b, kept inside the cache.
+__device__ __forceinline__ int attn_page(const AttnArgs& a, int b, int j) {
+  const int p = a.block_table[b * a.table_stride + (j >> a.page_shift)];
+  return min(max(p, 0), a.pages - 1);
+}
+
+// fp32 to the cache's type, two at a time, and the types' products.
+template <bool BF>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  if constexpr (BF) {
+    const b2_t r = {(__bf16)x, (__bf16)y};
+    return __builtin_bit_cast(uint32_t, r);
+  } else {
+    const h2_t r = {(_Float16)x, (_Float16)y};
+    return __builtin_bit_cast(uint32_t, r);
+  }
+}
+template <bool BF>
+__device__ __forceinline__ float low_of(uint32_t w) {
+  if constexpr (BF) return __builtin_bit_cast(float, w << 16);
+  return (float)as_h2(w)[0];
+}
+template <bool BF>
+__device__ __forceinline__ float high_of(uint32_t w) {
+  if constexpr (BF) return __builtin_bit_cast(float, w & 0xFFFF0000u);
+  return (float)as_h2(w)[1];
+}
+template <bool BF>
+__device__ __forceinline__ f4_t mfma16(const u32x4_t& x, const u32x4_t& y, const f4_t& c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, x), __builtin_bit_cast(b8_t, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, x), __builtin_bit_cast(h8_t, y), c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+template <bool BF>
+__device__ __forceinline__ f16_t mfma32(const u32x4_t& x, const u32x4_t& y, const f16_t& c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8_t, x), __builtin_bit_cast(b8_t, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8_t, x), __builtin_bit_cast(h8_t, y), c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// Factor of sums whose maximum rises by -x (log2).  Never 0, so that an infinite
+// sum stays what it is; finite ones vanish either way.
+__device__ __forceinline__ float rescale(float x) { return fmaxf(__builtin_amdgcn_exp2f(x), 1e-30f); }
+
+// Values that are not finite.  A masked key has weight 0, and 0 times an
+// infinite or NaN value would be NaN in rows that do not see the key.  Where some
+// row does not see some key of a tile, a tile with such values takes the values
+// as 0 in the product, and rows that do see one get it by another: the number
+// of +inf (or NaN) and of -inf (or NaN) values that a row sees, from 0/1 weights
+// and 0/1 values, exactly.
+template <bool BF>
+struct Bits16 {
+  static constexpr uint32_t kExp = BF ? 0x7F80u : 0x7C00u;
+  static constexpr uint32_t kOne = BF ? 0x3F80u : 0x3C00u;
+};
+// Bit 15 and bit 31: halves with all exponent bits set.
+template <bool BF>
+__device__ __forceinline__ uint32_t non_finite(uint32_t w) {
+  constexpr uint32_t e = Bits16<BF>::kExp, low = e & (~e + 1);
+  return ((w & (e * 0x10001u)) + low * 0x10001u) & 0x80008000u;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t non_finite_any(const u32x4_t& f) {
+  return non_finite<BF>(f[0]) | non_finite<BF>(f[1]) | non_finite<BF>(f[2]) | non_finite<BF>(f[3]);
+}
+template <bool BF>
+__device__ __forceinline__ u32x4_t finite_or_zero(const u32x4_t& f) {
+  u32x4_t r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) r[w] = f[w] & ~((non_finite<BF>(f[w]) >> 15) * 0xFFFFu);
+  return r;
+}
+// 1 for halves that are +inf or NaN (`sign` 0x10001: -inf or NaN), else 0.
+template <bool BF>
+__device__ __forceinline__ u32x4_t infinite_ones(const u32x4_t& f, uint32_t sign) {
+  constexpr uint32_t e = Bits16<BF>::kExp, mant = ~e & 0x7FFFu;
+  u32x4_t r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t odd = non_finite<BF>(f[w]) >> 15;
+    const uint32_t nan = (((f[w] & (mant * 0x10001u)) + mant * 0x10001u) / (mant + 1)) & 0x10001u;
+    r[w] = (odd & (nan | ~((f[w] >> 15) ^ sign))) * Bits16<BF>::kOne;
+  }
+  return r;
+}
+// Adds +inf where a row sees such values (counts nu), -inf likewise (nd).
+template <typename V>
+__device__ __forceinline__ void add_infinities(V& acc, const V& nu, const V& nd) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(V) / 4); ++i) {
+    acc[i] += nu[i] > 0.f ? INFINITY : 0.f;
+    acc[i] -= nd[i] > 0.f ? INFINITY : 0.f;
+  }
+}
+
+hipError_t launch_attention_step(const AttnArgs& a, bool bf, int grid, hipStream_t s);
+hipError_t launch_attention_chunk(const AttnArgs& a, bool bf, int grid, hipStream_t s);
+// The padded head size a kernel runs (64, 128 or 256), workgroups per launch and
+// floats of a workspace place.
+inline int attention_dim(int head_dim) { return head_dim <= 64 ? 64 : (head_dim <= 128 ? 128 : 256); }
+int attention_step_grid();
+int attention_chunk_grid(int head_dim);
+int64_t attention_step_place(int head_dim);
+int64_t attention_chunk_place(int head_dim);
+
+}  // namespace aqlm

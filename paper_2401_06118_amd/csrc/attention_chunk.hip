@@ -1,0 +1,473 @@
+// Attention over a paged cache for many rows per sequence: chunks of a prompt.
+//
+// Bound: 4 operations per row, key and element of the head against 4 bytes per key
+// and element, so a unit of 128 rows is bound by the matrix cores and by the
+// exponentials between their two products.  A workgroup of 4 waves holds a unit
+// of 128 rows, 32 a wave, and runs key tiles of 64 through two LDS stages:
+// keys and values go from the pages straight into LDS
+// (global_load_lds_dwordx4, a lane fetches 16 bytes of its row's page), a tile
+// ahead of the one being computed.
+//
+// Products, 32 x 32 x 16, rows as columns of the results, so that a lane holds
+// one row's weights and a row's maximum, denominator and factors need no
+// exchange of lanes but one between the wave's halves:
+//   S^T [key][row] = K Q^T      a lane holds 16 of 32 keys of its row
+//   O^T [d][row]  += V^T P^T    the lane's keys as they are: the order of the
+//                               keys inside a product is free, and V^T's
+//                               fragments (ds_read_b64_tr_b16, 4 keys of a
+//                               column) follow P's order
+// Stage rows hold their 16-byte chunks permuted by the key, so that the fragment
+// reads of 16 (keys) and 8 (values, two 32-byte blocks) rows cover all banks; the
+// loads apply the permutation on the memory side.
+//
+// The sums are rescaled only where a row's maximum rises by more than 2^8: until
+// then the old one stays in the exponents.  Weights are rounded once to the
+// cache's type (fp16: up to 2^15, so that small ones stay normal); the
+// denominator adds them up unrounded.
+#include "attention.h"
+#include "launch.h"
+#include "lds_sync.h"
+
+namespace aqlm {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kWaveRows = 32;
+constexpr int kRows = kWaves * kWaveRows;
+constexpr int kTile = 64;
+constexpr int kPieces = 16;  // whole shares of a split unit: its last workgroup reads all pieces
+constexpr float kLazy = 8.f;
+
+typedef __attribute__((address_space(3))) s4_t lds_s4_t;
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+template <int D>
+constexpr int chunk_place() { return kRows * D + 2 * kRows; }
+
+template <int D>
+struct ChunkLds {
+  static constexpr int kOperand = kTile * D;           // elements
+  static constexpr int kStage = 2 * kOperand;          // keys, values
+  static constexpr int kFixed = 2 * kStage * 2 + 64;   // bytes, with the scratch words
+};
+
+__device__ __forceinline__ void chunk_load_to_lds(const uint16_t* g, uint16_t* l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(g, (lds_void_t*)l, 16, 0, 0);
+#endif
+}
+__device__ __forceinline__ u32x2_t chunk_read_tr(const uint16_t* l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)l));
+#else
+  return u32x2_t{};
+#endif
+}
+
+// This wave's loads into LDS have landed; then every wave's have.
+__device__ __forceinline__ void stage_ready() {
+  __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Chunk position of 16-byte chunk c of stage row r.
+template <int D>
+__device__ __forceinline__ int k_swizzle(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
+template <int D>
+__device__ __forceinline__ int v_swizzle(int r) { return (D == 64 ? (r >> 1) & 3 : r & 7) * 2; }
+
+// Exchanges x's upper half of the wave with y's lower half.
+__device__ __forceinline__ void swap_halves(uint32_t& x, uint32_t& y) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+#endif
+}
+__device__ __forceinline__ float other_half_max(float v) {
+  uint32_t x = __builtin_bit_cast(uint32_t, v), y = x;
+  swap_halves(x, y);
+  return fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
+}
+__device__ __forceinline__ float both_halves_sum(float v) {
+  uint32_t x = __builtin_bit_cast(uint32_t, v), y = x;
+  swap_halves(x, y);
+  return __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+}
+
+// What a wave keeps of its rows.
+template <int D>
+struct ChunkRows {
+  u32x4_t q[D / 16];
+  f16_t acc[D / 32];
+  float m, l;
+  int lo, hi;                  // keys that this lane's row sees
+  int lo_min, lo_max, hi_min, hi_max;  // over the wave's rows
+};
+
+// Loads of a tile: this lane's chunks of the wave's rows of a stage.
+template <int D, bool EXACT>
+struct ChunkLoad {
+  static constexpr int CH = D / 8, PER = CH / kWaves, ROWS = kTile / kWaves, RPI = kWave / CH;
+  const uint16_t *k, *v;  // at the head
+  int row0;               // the wave's first stage row
+  int inst0;              // LDS elements before the wave's rows
+
+  __device__ __forceinline__ int page_id(const AttnArgs& a, const AttnUnit& u, int base, int lane) const {
+    return attn_page(a, u.b, min(max(base + row0 + (lane & (ROWS - 1)), u.k0), u.k1 - 1));
+  }
+  __device__ __forceinline__ void issue(const AttnArgs& a, const AttnUnit& u, uint16_t* stage, int base, int ids,
+                                        int lane) const {
+    const int pmask = (1 << a.page_shift) - 1;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int rl = i * RPI + lane / CH, row = row0 + rl, slot = lane % CH;
+      const int key = min(max(base + row, u.k0), u.k1 - 1);
+      const int id = __shfl(ids, rl), at = key & pmask;
+      const int ck = slot ^ k_swizzle<D>(row), cv = slot ^ v_swizzle<D>(row);
+      const uint16_t* pk = k + id * a.k_page + at * a.k_slot + ck * 8;
+      const uint16_t* pv = v + id * a.v_page + at * a.v_slot + cv * 8;
+      uint16_t* const l = stage + inst0 + i * (kWave * 8);
+      if (EXACT || ck * 8 < a.head_dim) chunk_load_to_lds(pk, l);
+      if (EXACT || cv * 8 < a.head_dim) chunk_load_to_lds(pv, l + ChunkLds<D>::kOperand);
+    }
+  }
+};
+
+// V^T of 32 columns (block db) and 16 keys (step s), in P's key order.
+template <int D>
+__device__ __forceinline__ u32x4_t read_vt(const uint16_t* v, int db, int s, int lane) {
+  const int kr = 16 * s + 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const int c = db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  const uint16_t* p = v + kr * D + (c ^ v_swizzle<D>(kr)) * 8 + (lane & 1) * 4;
+  const u32x2_t x = chunk_read_tr(p), y = chunk_read_tr(p + 8 * D);
+  return u32x4_t{x[0], x[1], y[0], y[1]};
+}
+
+// One tile: the next tile's loads go out, then this one is computed.  The two
+// stages are different memory (restrict): otherwise the compiler would wait for
+// the loads just issued before the first fragment read.
+template <bool BF, int D, bool EXACT>
+__device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u, const uint16_t* __restrict__ rd,
+                                           uint16_t* __restrict__ wr, const ChunkLoad<D, EXACT>& ld, int base,
+                                           bool more, int& ids, bool active, int unit_lo, int unit_hi, int* mark, int turn,
+                                           ChunkRows<D>& r) {
+  constexpr float kShift = BF ? 0.f : 7.f;
+  const int lane = threadIdx.x & 63, half = lane >> 5, r32 = lane & 31;
+  if (more) {
+    ld.issue(a, u, wr, base + kTile, ids, lane);
+    ids = ld.page_id(a, u, base + 2 * kTile, lane);
+  }
+  const uint16_t* const kst = rd;
+  const uint16_t* const vst = rd + ChunkLds<D>::kOperand;
+
+  // Values that are not finite, in tiles that some row of the unit does not see
+  // all of: each wave notes which of its rows' sums become infinite (bit i of
+  // `flags`: +inf, bit 16 + i: -inf), then the tile's are set to 0.  (Loops that
+  // are not unrolled: this path must not cost the others registers.)
+  uint32_t flags[D / 32] = {};
+  bool special = false;
+  if (base < unit_lo || base + kTile > unit_hi) {
+    uint16_t* const mine = const_cast<uint16_t*>(vst) + (threadIdx.x / kWave) * (kTile / kWaves) * D;
+    constexpr int PER = kTile * D / 8 / (kWaves * kWave);
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) odd |= non_finite_any<BF>(*(const u32x4_t*)(mine + (i * kWave + lane) * 8));
+    if (__ballot(odd != 0) != 0 && lane == 0) *mark = turn;
+    lds_barrier();
+    special = *mark == turn;
+    if (__builtin_expect(special, 0)) {
+#pragma unroll 1
+      for (int d = 0; d < D / 32; ++d) {
+        f16_t nu, nd;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) nu[i] = nd[i] = 0.f;
+#pragma unroll 1
+        for (int st = 0; st < 4; ++st) {
+          u32x4_t seen;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int key = base + st * 16 + 8 * (w / 2) + 4 * half + 2 * (w % 2);
+            seen[w] = (key >= r.lo && key < r.hi ? Bits16<BF>::kOne : 0u) |
+                      (key + 1 >= r.lo && key + 1 < r.hi ? Bits16<BF>::kOne << 16 : 0u);
+          }
+          const u32x4_t vf = read_vt<D>(vst, d, st, lane);
+          nu = mfma32<BF>(infinite_ones<BF>(vf, 0), seen, nu);
+          nd = mfma32<BF>(infinite_ones<BF>(vf, 0x10001u), seen, nd);
+        }
+        uint32_t f = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f |= (nu[i] > 0.f ? 1u << i : 0u) | (nd[i] > 0.f ? 0x10000u << i : 0u);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) flags[i] = i == d ? f : flags[i];
+      }
+      lds_barrier();
+#pragma unroll 1
+      for (int i = 0; i < PER; ++i) {
+        u32x4_t* const p = (u32x4_t*)(mine + (i * kWave + lane) * 8);
+        *p = finite_or_zero<BF>(*p);
+      }
+      lds_barrier();
+    }
+  }
+  if (!active || base >= r.hi_max || base + kTile <= r.lo_min) return;
+
+  f16_t s[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    const int row = b * 32 + r32;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const u32x4_t kf = *(const u32x4_t*)(kst + row * D + ((2 * i + half) ^ k_swizzle<D>(row)) * 8);
+      s[b] = mfma32<BF>(kf, r.q[i], s[b]);
+    }
+  }
+
+  const bool full = base >= r.lo_max && base + kTile <= r.hi_min;
+  if (!full) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = base + b * 32 + 8 * (i / 4) + 4 * half + i % 4;
+        const bool ok = key >= r.lo && key < r.hi;
+        s[b][i] = ok ? s[b][i] : -INFINITY;
+      }
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+  top = other_half_max(top) * a.scale_log2;
+  if (__ballot(top > r.m + kLazy) != 0) {
+    const float mn = fmaxf(r.m, top);
+    const float alpha = rescale(r.m - (mn == -INFINITY ? 0.f : mn));
+    r.m = mn;
+    r.l *= alpha;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) r.acc[d] *= alpha;
+  }
+  const float off = kShift - (r.m == -INFINITY ? 0.f : r.m);
+  u32x4_t pf[4];
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int st = 0; st < 4; ++st)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int i = (st % 2) * 8 + 2 * w;
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[st / 2][i], a.scale_log2, off));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[st / 2][i + 1], a.scale_log2, off));
+      sum[0] += p0;
+      sum[1] += p1;
+      pf[st][w] = pack2<BF>(p0, p1);
+    }
+  r.l += sum[0] + sum[1];
+
+#pragma unroll
+  for (int st = 0; st < 4; ++st)
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) r.acc[d] = mfma32<BF>(read_vt<D>(vst, d, st, lane), pf[st], r.acc[d]);
+  if (__builtin_expect(special, 0)) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        r.acc[d][i] += (flags[d] >> i) & 1 ? INFINITY : 0.f;
+        r.acc[d][i] -= (flags[d] >> (16 + i)) & 1 ? INFINITY : 0.f;
+      }
+  }
+}
+
+template <bool BF, int D, bool EXACT>
+__global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_chunk(AttnArgs a) {
+  constexpr float kShift = BF ? 0.f : 7.f;
+  extern __shared__ __align__(16) uint8_t lds[];
+  uint16_t* const stages = (uint16_t*)lds;
+  int* const scratch = (int*)(lds + ChunkLds<D>::kFixed - 64);
+  int* const prefix = scratch + 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r32 = lane & 31;
+  const int grid = gridDim.x;
+  const int wg = (grid & 7) == 0 ? (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+
+  if (!EXACT) {  // the padding of heads shorter than D is never loaded
+    for (int i = threadIdx.x; i < 2 * ChunkLds<D>::kStage / 8; i += kWaves * kWave)
+      *(u32x4_t*)(stages + i * 8) = u32x4_t{0, 0, 0, 0};
+  }
+  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces);
+
+  if (threadIdx.x == 0) scratch[9] = 0;  // (ordered by the barriers below)
+  int parity = 0, turn = 0;
+  for (int64_t at = h.begin; at < h.end;) {
+    const AttnUnit u = attn_find<kRows, kTile>(a, h, prefix, at);
+    at += u.to - u.from;
+    const int rows = min(kRows, u.s.count * a.group - u.t * kRows);
+    const int left = rows - wave * kWaveRows;  // rows of this wave
+    const bool active = left > 0;
+    const uint32_t first = (uint32_t)(u.t * kRows + (active ? wave * kWaveRows : 0));
+    const int mine = active ? min(left, kWaveRows) : 1;
+    const uint32_t rr = first + (uint32_t)min(r32, mine - 1);
+    const int token = (int)(rr / (uint32_t)a.group);
+    const int head = u.head * a.group + (int)(rr - (uint32_t)token * (uint32_t)a.group);
+
+    ChunkRows<D> r;
+    attn_visible(a, u.s, token, r.lo, r.hi);
+    attn_visible(a, u.s, (int)(first / (uint32_t)a.group), r.lo_min, r.hi_min);
+    attn_visible(a, u.s, (int)((first + (uint32_t)mine - 1) / (uint32_t)a.group), r.lo_max, r.hi_max);
+    int unit_lo, unit_hi, x;  // keys that all of the unit's rows see
+    attn_visible(a, u.s, (int)((uint32_t)(u.t * kRows) / (uint32_t)a.group), x, unit_hi);
+    attn_visible(a, u.s, (int)((uint32_t)(u.t * kRows + rows - 1) / (uint32_t)a.group), unit_lo, x);
+    r.m = -INFINITY;
+    r.l = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r.acc[d][i] = 0.f;
+
+    if (u.k1 > u.k0) {
+      ChunkLoad<D, EXACT> ld;
+      ld.k = a.k + u.head * a.k_head;
+      ld.v = a.v + u.head * a.v_head;
+      ld.row0 = wave * ld.ROWS;
+      ld.inst0 = wave * ld.ROWS * D;
+      int base = (u.tile0 + u.from) * kTile;
+      const int end = (u.tile0 + u.to) * kTile;
+      int ids = ld.page_id(a, u, base, lane);
+      ld.issue(a, u, stages + parity * ChunkLds<D>::kStage, base, ids, lane);
+      ids = ld.page_id(a, u, base + kTile, lane);
+      const uint16_t* qp = a.q + (u.s.first + token) * a.q_token + head * a.q_head;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const int c = 2 * i + half;
+        const bool in = EXACT || c * 8 < a.head_dim;
+        r.q[i] = attn_query(a, *(const u32x4_t*)(qp + (in ? c : 0) * 8));
+        if (!in) r.q[i] = u32x4_t{0, 0, 0, 0};
+      }
+      for (; base < end; base += kTile) {
+        stage_ready();
+        chunk_tile<BF, D, EXACT>(a, u, stages + parity * ChunkLds<D>::kStage,
+                                 stages + (parity ^ 1) * ChunkLds<D>::kStage, ld, base, base + kTile < end, ids,
+                                 active, unit_lo, unit_hi, scratch + 9, ++turn, r);
+        parity ^= 1;
+      }
+    }
+    r.l = both_halves_sum(r.l);
+
+    const bool whole = u.from == 0 && u.to == u.tiles;
+    bool write = whole;
+    if (!whole) {
+      const int w0 = (int)(u.start / h.quota), w1 = (int)((u.start + u.tiles - 1) / h.quota);
+      float* const place = a.parts + (int64_t)(2 * wg + (w0 == wg ? 1 : 0)) * chunk_place<D>();
+      if (active) {
+        float* const o = place + wave * kWaveRows * D;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *(f4_t*)(o + ((d * 4 + i) * kWave + lane) * 4) =
+                f4_t{r.acc[d][4 * i], r.acc[d][4 * i + 1], r.acc[d][4 * i + 2], r.acc[d][4 * i + 3]};
+        if (half == 0) {
+          place[kRows * D + wave * kWaveRows + r32] = r.m;
+          place[kRows * D + kRows + wave * kWaveRows + r32] = r.l;
+        }
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const uint32_t done = __hip_atomic_fetch_add(&a.counters[w0], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        scratch[8] = done == (uint32_t)(w1 - w0);
+      }
+      __syncthreads();
+      write = scratch[8] != 0;
+      if (write) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        const int n = w1 - w0 + 1;
+        auto piece = [&](int p) { return a.parts + (int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * chunk_place<D>(); };
+        if (active) {
+          const int row = wave * kWaveRows + r32;
+          float mm = -INFINITY;
+          for (int p = 0; p < n; ++p) mm = fmaxf(mm, piece(p)[kRows * D + row]);
+          r.m = mm;
+          r.l = 0.f;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r.acc[d][i] = 0.f;
+          for (int p = 0; p < n; ++p) {
+            const float* const pp = piece(p);
+            const float pm = pp[kRows * D + row];
+            const float w = pm == -INFINITY ? 0.f : rescale(pm - mm);
+            r.l += pm == -INFINITY ? 0.f : w * pp[kRows * D + kRows + row];
+            const float* const o = pp + wave * kWaveRows * D;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const f4_t x = *(const f4_t*)(o + ((d * 4 + i) * kWave + lane) * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r.acc[d][4 * i + j] += pm == -INFINITY ? 0.f : w * x[j];
+              }
+          }
+        }
+        if (threadIdx.x == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
+    if (write && active) {
+      const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+      uint16_t* const o = a.out + (u.s.first + token) * a.out_token + head * a.out_head;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {  // blocks i and i + 1 of 8 columns, half of each in a lane
+          u32x4_t w;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t x = pack2<BF>(r.acc[d][4 * i + 2 * j] * inv, r.acc[d][4 * i + 2 * j + 1] * inv);
+            uint32_t y = pack2<BF>(r.acc[d][4 * i + 4 + 2 * j] * inv, r.acc[d][4 * i + 4 + 2 * j + 1] * inv);
+            if (r.l == 0.f) x = y = 0;
+            swap_halves(x, y);
+            w[j] = x;
+            w[2 + j] = y;
+          }
+          const int c = d * 32 + 8 * (i + half);
+          if (r32 < mine && (EXACT || c < a.head_dim)) *(u32x4_t*)(o + c) = w;
+        }
+      if (a.lse && half == 0 && r32 < mine)
+        a.lse[(int64_t)(u.s.first + token) * (a.kv_heads * a.group) + head] =
+            r.l == 0.f ? -INFINITY : (r.m - kShift + log2f(r.l)) * 0.69314718055994531f;
+    }
+  }
+}
+
+template <bool BF, int D, bool EXACT>
+hipError_t launch(const AttnArgs& a, int grid, hipStream_t s) {
+  constexpr auto kern = k_attention_chunk<BF, D, EXACT>;
+  const hipError_t e = allow_dynamic_lds((const void*)kern, ChunkLds<D>::kFixed + (kAttnMaxSeqs + 1) * 4);
+  if (e != hipSuccess) return e;
+  kern<<<grid, kWaves * kWave, ChunkLds<D>::kFixed + (a.seqs + 1) * 4, s>>>(a);
+  return hipGetLastError();
+}
+
+template <bool BF, int D>
+hipError_t launch(const AttnArgs& a, int grid, hipStream_t s) {
+  return a.head_dim == D ? launch<BF, D, true>(a, grid, s) : launch<BF, D, false>(a, grid, s);
+}
+
+}  // namespace
+
+int attention_chunk_grid(int head_dim) { return (attention_dim(head_dim) == 256 ? 1 : 2) * num_cus(); }
+int64_t attention_chunk_place(int head_dim) { return (int64_t)kRows * (attention_dim(head_dim) + 2); }
+
+hipError_t launch_attention_chunk(const AttnArgs& a, bool bf, int grid, hipStream_t s) {
+  switch (attention_dim(a.head_dim)) {
+    case 64: return bf ? launch<true, 64>(a, grid, s) : launch<false, 64>(a, grid, s);
+    case 128: return bf ? launch<true, 128>(a, grid, s) : launch<false, 128>(a, grid, s);
+    default: return bf ? launch<true, 256>(a, grid, s) : launch<false, 256>(a, grid, s);
+  }
+}
+
+}  // namespace aqlm
