@@ -123,15 +123,30 @@ struct AttnShare {
   int per_head;    // tiles of one kv head over all sequences
   int64_t total;   // tiles of all heads
   int64_t quota;   // tiles of a workgroup's share
+  int64_t slack;   // how far an end of a share moves to an end of a unit
   int64_t begin, end;
+};
+
+struct AttnUnit;
+template <int R, int KT>
+__device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare& h, const int* prefix, int64_t at);
+
+// One unit of a share: where it is, and the part of its tiles that the share holds.
+struct AttnUnit {
+  AttnSeq s;
+  int b, head, t;
+  int tile0, tiles, k0, k1;
+  int from, to;         // tiles [from, to) of the unit are in the share
+  int64_t start;        // the unit's first tile in the sequence of all tiles
 };
 
 // Fills `prefix` (LDS, seqs + 1 ints: tiles of one kv head before each
 // sequence; `scratch`: 2 * waves ints) and returns this workgroup's share.
-// `pieces`: the most pieces that a unit is split into.
+// `pieces`: the most whole shares that a unit is split into; `least`: tiles that a
+// share has at least.
 template <int R, int KT, int WAVES>
 __device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, int* prefix, int* scratch, int wg, int grid,
-                                                int pieces) {
+                                                int pieces, int least) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   int most = 1;
   if (a.seqs <= WAVES) {  // few sequences, perhaps of many units: a wave for each
@@ -182,20 +197,68 @@ __device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, int* prefix, 
   h.per_head = prefix[a.seqs];
   h.total = (int64_t)h.per_head * a.kv_heads;
   h.quota = max((h.total + grid - 1) / grid, (int64_t)((most + pieces - 1) / pieces));
-  h.quota = max(h.quota, (int64_t)1);
+  h.quota = max(h.quota, (int64_t)least);
+  h.slack = h.quota / 8;
   h.begin = min(h.total, h.quota * wg);
   h.end = min(h.total, h.begin + h.quota);
+  if (h.slack > 0) {
+    const int64_t last = h.end;
+    auto moved = [&](int64_t x) {
+      if (x == 0 || x >= h.total) return x;
+      const AttnUnit u = attn_find<R, KT>(a, h, prefix, x);
+      if (u.from <= h.slack) return u.start;
+      return u.tiles - u.from <= h.slack ? u.start + u.tiles : x;
+    };
+    h.end = moved(last);
+    h.begin = h.begin < last ? moved(h.begin) : h.end;
+  }
   return h;
 }
 
-// One unit of a share: where it is, and the part of its tiles that the share holds.
-struct AttnUnit {
-  AttnSeq s;
-  int b, head, t;
-  int tile0, tiles, k0, k1;
-  int from, to;         // tiles [from, to) of the unit are in the share
-  int64_t start;        // the unit's first tile in the sequence of all tiles
-};
+// The workgroups that hold the first and the last piece of a unit.
+__device__ __forceinline__ void attn_holders(const AttnShare& h, const AttnUnit& u, int& w0, int& w1) {
+  w0 = (int)((u.start + h.slack) / h.quota);
+  w1 = max(w0, (int)((u.start + u.tiles - h.slack - 1) / h.quota));
+}
+
+// The place of piece p of a unit: of the unit that its workgroup begins (the
+// first piece) or continues.
+__device__ __forceinline__ float* attn_place(const AttnArgs& a, int w0, int p, int64_t floats) {
+  return a.parts + (2 * (int64_t)(w0 + p) + (p == 0 ? 1 : 0)) * floats;
+}
+
+// Written through to memory, and read from there.
+__device__ __forceinline__ void put2(float* p, float x, float y) {
+  const u32x2_t w = {__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+  __hip_atomic_store((uint64_t*)p, __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f2_t get2(const float* p) {
+  return __builtin_bit_cast(f2_t, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ void put4(float* p, const f4_t& v) {
+  put2(p, v[0], v[1]);
+  put2(p + 2, v[2], v[3]);
+}
+__device__ __forceinline__ f4_t get4(const float* p) {
+  const f2_t x = get2(p), y = get2(p + 2);
+  return f4_t{x[0], x[1], y[0], y[1]};
+}
+
+// After a workgroup's stores of a piece: true in the workgroup that wrote the last
+// of a unit's pieces (`count` of them).  Its stores have reached memory before the
+// counter moves.  `flag`: an LDS word.
+__device__ __forceinline__ bool attn_last(uint32_t* counter, int count, int* flag) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last =
+        __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(count - 1);
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag != 0;
+}
 
 // The unit that holds tile `at` of the sequence of all tiles.  Uniform over the
 // workgroup; every wave finds it by itself.
@@ -219,13 +282,14 @@ __device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare
   int tile0, k0, k1, t = 0;
   if (units > 1) {
     int before = 0;
+    auto unit_at = [&](int i) { return (i & 1) == 0 ? i / 2 : units - 1 - i / 2; };
     for (int i = 0; i < units; i += kWave) {
-      const int n = i + lane < units ? attn_tiles<R, KT>(a, u.s, i + lane, tile0, k0, k1) : 0;
+      const int n = i + lane < units ? attn_tiles<R, KT>(a, u.s, unit_at(i + lane), tile0, k0, k1) : 0;
       const int incl = wave_scan(n) + before;
       const uint64_t gt = __ballot(incl > left);
       if (gt != 0) {
         const int l = __builtin_ctzll(gt);
-        t = i + l;
+        t = unit_at(i + l);
         before = l > 0 ? __shfl(incl, l - 1) : before;
         break;
       }

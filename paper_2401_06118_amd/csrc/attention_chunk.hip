@@ -37,6 +37,7 @@ constexpr int kWaveRows = 32;
 constexpr int kRows = kWaves * kWaveRows;
 constexpr int kTile = 64;
 constexpr int kPieces = 16;  // whole shares of a split unit: its last workgroup reads all pieces
+constexpr int kLeast = 4;     // tiles of a share: below, a piece costs more than it computes
 constexpr float kLazy = 8.f;
 
 typedef __attribute__((address_space(3))) s4_t lds_s4_t;
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
     for (int i = threadIdx.x; i < 2 * ChunkLds<D>::kStage / 8; i += kWaves * kWave)
       *(u32x4_t*)(stages + i * 8) = u32x4_t{0, 0, 0, 0};
   }
-  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces);
+  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces, kLeast);
 
   if (threadIdx.x == 0) scratch[9] = 0;  // (ordered by the barriers below)
   int parity = 0, turn = 0;
@@ -361,36 +362,26 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
     const bool whole = u.from == 0 && u.to == u.tiles;
     bool write = whole;
     if (!whole) {
-      const int w0 = (int)(u.start / h.quota), w1 = (int)((u.start + u.tiles - 1) / h.quota);
-      float* const place = a.parts + (int64_t)(2 * wg + (w0 == wg ? 1 : 0)) * chunk_place<D>();
+      int w0, w1;
+      attn_holders(h, u, w0, w1);
+      const int n = w1 - w0 + 1;
+      float* const place = attn_place(a, w0, wg - w0, chunk_place<D>());
       if (active) {
         float* const o = place + wave * kWaveRows * D;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *(f4_t*)(o + ((d * 4 + i) * kWave + lane) * 4) =
-                f4_t{r.acc[d][4 * i], r.acc[d][4 * i + 1], r.acc[d][4 * i + 2], r.acc[d][4 * i + 3]};
-        if (half == 0) {
-          place[kRows * D + wave * kWaveRows + r32] = r.m;
-          place[kRows * D + kRows + wave * kWaveRows + r32] = r.l;
-        }
+            put4(o + ((d * 4 + i) * kWave + lane) * 4,
+                 f4_t{r.acc[d][4 * i], r.acc[d][4 * i + 1], r.acc[d][4 * i + 2], r.acc[d][4 * i + 3]});
+        if (half == 0) put2(place + kRows * D + 2 * (wave * kWaveRows + r32), r.m, r.l);
       }
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        const uint32_t done = __hip_atomic_fetch_add(&a.counters[w0], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        scratch[8] = done == (uint32_t)(w1 - w0);
-      }
-      __syncthreads();
-      write = scratch[8] != 0;
+      write = attn_last(&a.counters[w0], n, scratch + 8);
       if (write) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        const int n = w1 - w0 + 1;
-        auto piece = [&](int p) { return a.parts + (int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * chunk_place<D>(); };
         if (active) {
           const int row = wave * kWaveRows + r32;
           float mm = -INFINITY;
-          for (int p = 0; p < n; ++p) mm = fmaxf(mm, piece(p)[kRows * D + row]);
+          for (int p = 0; p < n; ++p) mm = fmaxf(mm, get2(attn_place(a, w0, p, chunk_place<D>()) + kRows * D + 2 * row)[0]);
           r.m = mm;
           r.l = 0.f;
 #pragma unroll
@@ -398,22 +389,22 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
 #pragma unroll
             for (int i = 0; i < 16; ++i) r.acc[d][i] = 0.f;
           for (int p = 0; p < n; ++p) {
-            const float* const pp = piece(p);
-            const float pm = pp[kRows * D + row];
-            const float w = pm == -INFINITY ? 0.f : rescale(pm - mm);
-            r.l += pm == -INFINITY ? 0.f : w * pp[kRows * D + kRows + row];
+            const float* const pp = attn_place(a, w0, p, chunk_place<D>());
+            const f2_t ml = get2(pp + kRows * D + 2 * row);
+            const bool some = ml[0] != -INFINITY;
+            const float w = some ? rescale(ml[0] - mm) : 0.f;
+            r.l += some ? w * ml[1] : 0.f;
             const float* const o = pp + wave * kWaveRows * D;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const f4_t x = *(const f4_t*)(o + ((d * 4 + i) * kWave + lane) * 4);
+                const f4_t x = get4(o + ((d * 4 + i) * kWave + lane) * 4);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r.acc[d][4 * i + j] += pm == -INFINITY ? 0.f : w * x[j];
+                for (int j = 0; j < 4; ++j) r.acc[d][4 * i + j] += some ? w * x[j] : 0.f;
               }
           }
         }
-        if (threadIdx.x == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
     if (write && active) {

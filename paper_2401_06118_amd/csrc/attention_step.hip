@@ -45,7 +45,7 @@ struct StepLds {
   static constexpr int kPitch = D + 4;  // floats per row of the joined sums
   static constexpr int kStage = kWaves * kWaveKeys * D * 2;
   static constexpr int kJoin = kWaves * kRows * (kPitch + 2) * 4;
-  static constexpr int kWeights = (kPieces + 2) * kRows * 4;
+  static constexpr int kWeights = (kPieces + 1) * kRows * 8;
   static constexpr int kMax0 = kStage > kJoin ? kStage : kJoin;
   static constexpr int kUnion = kMax0 > kWeights ? kMax0 : kWeights;
   static constexpr int kFixed = kUnion + 64;  // + scratch: waves' maxima, the "last" flag
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
   float* const join_m = join + kWaves * kRows * StepLds<D>::kPitch;  // [wave][row] maxima, then denominators
   const int pmask = (1 << a.page_shift) - 1;
 
-  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces);
+  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces, 1);
 
   for (int64_t at = h.begin; at < h.end;) {
     const AttnUnit u = attn_find<kRows, kTile>(a, h, prefix, at);
@@ -285,10 +285,6 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
       join_m[(kWaves + wave) * kRows + r16] = l;
     }
     __syncthreads();
-    const bool whole = u.from == 0 && u.to == u.tiles;
-    const int w0 = (int)(u.start / h.quota), w1 = (int)((u.start + u.tiles - 1) / h.quota);
-    float* const place = a.parts + (int64_t)(2 * wg + (w0 == wg ? 1 : 0)) * step_place<D>();
-
     auto write = [&](int row, int d, f4_t o, float mm, float ll) {
       const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
       const uint32_t ur = (uint32_t)(u.t * kRows + row);
@@ -304,77 +300,75 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
             ll == 0.f ? -INFINITY : (mm - kShift + log2f(ll)) * 0.69314718055994531f;
     };
 
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kWaves * kWave) {
-      const int row = i / (D / 4), d = (i % (D / 4)) * 4;
-      float mm = -INFINITY;
+    // 4 elements of a row per thread and turn
+    constexpr int kTurns = kRows * D / 4 / (kWaves * kWave);
+    f4_t o[kTurns];
+    float mm[kTurns], ll[kTurns];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, join_m[w * kRows + row]);
-      const float bm = mm == -INFINITY ? 0.f : mm;
-      f4_t o = {0, 0, 0, 0};
-      float ll = 0.f;
+    for (int t = 0; t < kTurns; ++t) {
+      const int i = t * (kWaves * kWave) + threadIdx.x, row = i / (D / 4), d = (i % (D / 4)) * 4;
+      mm[t] = -INFINITY;
+      ll[t] = 0.f;
+      o[t] = f4_t{0, 0, 0, 0};
+      if (row >= rows) continue;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) mm[t] = fmaxf(mm[t], join_m[w * kRows + row]);
+      const float bm = mm[t] == -INFINITY ? 0.f : mm[t];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float mw = join_m[w * kRows + row];
         if (mw == -INFINITY) continue;  // (a wave without keys of this row)
         const float e = rescale(mw - bm);
-        ll += e * join_m[(kWaves + w) * kRows + row];
-        o += e * *(const f4_t*)(join + (w * kRows + row) * StepLds<D>::kPitch + d);
+        ll[t] += e * join_m[(kWaves + w) * kRows + row];
+        o[t] += e * *(const f4_t*)(join + (w * kRows + row) * StepLds<D>::kPitch + d);
       }
-      if (whole) {
-        write(row, d, o, mm, ll);
-      } else {
-        *(f4_t*)(place + row * D + d) = o;
-        if (d == 0) {
-          place[kRows * D + row] = mm;
-          place[kRows * D + kRows + row] = ll;
+    }
+    bool done = true;
+    if (u.from != 0 || u.to != u.tiles) {
+      int w0, w1;
+      attn_holders(h, u, w0, w1);
+      const int n = w1 - w0 + 1;
+      float* const place = attn_place(a, w0, wg - w0, step_place<D>());
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        const int i = t * (kWaves * kWave) + threadIdx.x, row = i / (D / 4), d = (i % (D / 4)) * 4;
+        if (row >= rows) continue;
+        put4(place + row * D + d, o[t]);
+        if (d == 0) put2(place + kRows * D + 2 * row, mm[t], ll[t]);
+      }
+      done = attn_last(&a.counters[w0], n, scratch + 8);
+      if (done) {
+        float* const ml = (float*)lds;  // [piece][row]: maximum, denominator
+        for (int i = threadIdx.x; i < n * rows; i += kWaves * kWave) {
+          const int p = i / rows, row = i - p * rows;
+          *(f2_t*)(ml + 2 * (p * kRows + row)) = get2(attn_place(a, w0, p, step_place<D>()) + kRows * D + 2 * row);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+          const int i = t * (kWaves * kWave) + threadIdx.x, row = i / (D / 4), d = (i % (D / 4)) * 4;
+          if (row >= rows) continue;
+          mm[t] = -INFINITY;
+          for (int p = 0; p < n; ++p) mm[t] = fmaxf(mm[t], ml[2 * (p * kRows + row)]);
+          ll[t] = 0.f;
+          o[t] = f4_t{0, 0, 0, 0};
+#pragma unroll 8
+          for (int p = 0; p < n; ++p) {
+            const f4_t po = get4(attn_place(a, w0, p, step_place<D>()) + row * D + d);
+            const f2_t pm = *(const f2_t*)(ml + 2 * (p * kRows + row));
+            if (pm[0] == -INFINITY) continue;
+            const float w = rescale(pm[0] - mm[t]);
+            o[t] += w * po;
+            ll[t] += w * pm[1];
+          }
         }
       }
     }
-    if (!whole) {
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        const uint32_t done = __hip_atomic_fetch_add(&a.counters[w0], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        scratch[8] = done == (uint32_t)(w1 - w0);
-      }
-      __syncthreads();
-      if (scratch[8]) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        const int n = w1 - w0 + 1;
-        float* const wt = (float*)lds;  // [piece][row]
-        auto piece = [&](int p) { return a.parts + (int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * step_place<D>(); };
-        for (int i = threadIdx.x; i < n * rows; i += kWaves * kWave)
-          wt[(i / rows) * kRows + i % rows] = piece(i / rows)[kRows * D + i % rows];
-        __syncthreads();
-        float* const top = wt + (kPieces + 1) * kRows;  // [row]
-        if (threadIdx.x < rows) {
-          float mm = -INFINITY;
-          for (int p = 0; p < n; ++p) mm = fmaxf(mm, wt[p * kRows + threadIdx.x]);
-          top[threadIdx.x] = mm;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < n * rows; i += kWaves * kWave) {
-          float& w = wt[(i / rows) * kRows + i % rows];
-          w = w == -INFINITY ? 0.f : rescale(w - top[i % rows]);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < rows * (D / 4); i += kWaves * kWave) {
-          const int row = i / (D / 4), d = (i % (D / 4)) * 4;
-          f4_t o = {0, 0, 0, 0};
-          float ll = 0.f;
-#pragma unroll 4
-          for (int p = 0; p < n; ++p) {
-            const float* pp = piece(p);
-            const float w = wt[p * kRows + row];
-            const f4_t po = *(const f4_t*)(pp + row * D + d);
-            const float pl = pp[kRows * D + kRows + row];
-            if (w != 0.f) {
-              o += w * po;
-              ll += w * pl;
-            }
-          }
-          write(row, d, o, top[row], ll);
-        }
-        if (threadIdx.x == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (done) {
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        const int i = t * (kWaves * kWave) + threadIdx.x, row = i / (D / 4), d = (i % (D / 4)) * 4;
+        if (row < rows) write(row, d, o[t], mm[t], ll[t]);
       }
     }
     __syncthreads();
