@@ -56,6 +56,7 @@ struct AttnArgs {
   int32_t tokens, seqs, kv_heads, group, head_dim;
   int32_t pages, page_shift, table_width;
   int32_t causal, window;
+  int32_t whole_rows;  // 16 aligned keys share a page, their offsets in it fit 31 bits
   // |scale| * log2(e), above 0 (so that a masked score stays -inf under it); the
   // queries are read as (q & q_keep) ^ q_flip, which brings in the sign, and a
   // scale of 0 as queries of 0.

@@ -115,15 +115,40 @@ struct ChunkLoad {
   static constexpr int CH = D / 8, PER = CH / kWaves, ROWS = kTile / kWaves, RPI = kWave / CH;
   const uint16_t *k, *v;  // at the head
   int row0;               // the wave's first stage row
-  int inst0;              // LDS elements before the wave's rows
+  uint32_t at_k[PER], at_v[PER];  // bytes of the lane's chunks past the wave's first row
 
+  // Offsets within a page, for tiles whose rows of a wave share one.
+  __device__ __forceinline__ void set(const AttnArgs& a, int wave, int lane) {
+    row0 = wave * ROWS;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int rl = i * RPI + lane / CH, slot = lane % CH;
+      at_k[i] = (uint32_t)(rl * (int)a.k_slot + (slot ^ k_swizzle<D>(row0 + rl)) * 8) * 2;
+      at_v[i] = (uint32_t)(rl * (int)a.v_slot + (slot ^ v_swizzle<D>(row0 + rl)) * 8) * 2;
+    }
+  }
   __device__ __forceinline__ int page_id(const AttnArgs& a, const AttnUnit& u, int base, int lane) const {
     return attn_page(a, u.b, min(max(base + row0 + (lane & (ROWS - 1)), u.k0), u.k1 - 1));
   }
   __device__ __forceinline__ void issue(const AttnArgs& a, const AttnUnit& u, uint16_t* stage, int base, int ids,
                                         int lane) const {
     const int pmask = (1 << a.page_shift) - 1;
+    uint16_t* const to = stage + row0 * D;
+    if (a.whole_rows && base >= u.k0 && base + kTile <= u.k1) {  // the wave's rows are in one page
+      const int64_t id = __builtin_amdgcn_readfirstlane(ids), at = (base + row0) & pmask;
+      const uint8_t* const pk = (const uint8_t*)(k + id * a.k_page + at * a.k_slot);
+      const uint8_t* const pv = (const uint8_t*)(v + id * a.v_page + at * a.v_slot);
 #pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int row = row0 + i * RPI + lane / CH, slot = lane % CH;
+        uint16_t* const l = to + i * (kWave * 8);
+        if (EXACT || (slot ^ k_swizzle<D>(row)) * 8 < a.head_dim) chunk_load_to_lds((const uint16_t*)(pk + at_k[i]), l);
+        if (EXACT || (slot ^ v_swizzle<D>(row)) * 8 < a.head_dim)
+          chunk_load_to_lds((const uint16_t*)(pv + at_v[i]), l + ChunkLds<D>::kOperand);
+      }
+      return;
+    }
+#pragma unroll 1
     for (int i = 0; i < PER; ++i) {
       const int rl = i * RPI + lane / CH, row = row0 + rl, slot = lane % CH;
       const int key = min(max(base + row, u.k0), u.k1 - 1);
@@ -131,19 +156,24 @@ struct ChunkLoad {
       const int ck = slot ^ k_swizzle<D>(row), cv = slot ^ v_swizzle<D>(row);
       const uint16_t* pk = k + id * a.k_page + at * a.k_slot + ck * 8;
       const uint16_t* pv = v + id * a.v_page + at * a.v_slot + cv * 8;
-      uint16_t* const l = stage + inst0 + i * (kWave * 8);
+      uint16_t* const l = to + i * (kWave * 8);
       if (EXACT || ck * 8 < a.head_dim) chunk_load_to_lds(pk, l);
       if (EXACT || cv * 8 < a.head_dim) chunk_load_to_lds(pv, l + ChunkLds<D>::kOperand);
     }
   }
 };
 
-// V^T of 32 columns (block db) and 16 keys (step s), in P's key order.
+// V^T of 32 columns (block db) and 16 keys (step s), in P's key order; `at`:
+// vt_offset.
 template <int D>
-__device__ __forceinline__ u32x4_t read_vt(const uint16_t* v, int db, int s, int lane) {
-  const int kr = 16 * s + 4 * (lane >> 5) + ((lane & 15) >> 2);
-  const int c = db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-  const uint16_t* p = v + kr * D + (c ^ v_swizzle<D>(kr)) * 8 + (lane & 1) * 4;
+__device__ __forceinline__ int vt_offset(int lane) {
+  const int kr = 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const int c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  return kr * D + (c ^ v_swizzle<D>(kr)) * 8 + (lane & 1) * 4;
+}
+template <int D>
+__device__ __forceinline__ u32x4_t read_vt(const uint16_t* v, int db, int s, int at) {
+  const uint16_t* p = v + (at ^ (db * 32)) + 16 * s * D;
   const u32x2_t x = chunk_read_tr(p), y = chunk_read_tr(p + 8 * D);
   return u32x4_t{x[0], x[1], y[0], y[1]};
 }
@@ -195,7 +225,7 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
             seen[w] = (key >= r.lo && key < r.hi ? Bits16<BF>::kOne : 0u) |
                       (key + 1 >= r.lo && key + 1 < r.hi ? Bits16<BF>::kOne << 16 : 0u);
           }
-          const u32x4_t vf = read_vt<D>(vst, d, st, lane);
+          const u32x4_t vf = read_vt<D>(vst, d, st, vt_offset<D>(lane));
           nu = mfma32<BF>(infinite_ones<BF>(vf, 0), seen, nu);
           nd = mfma32<BF>(infinite_ones<BF>(vf, 0x10001u), seen, nd);
         }
@@ -216,17 +246,28 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
   }
   if (!active || base >= r.hi_max || base + kTile <= r.lo_min) return;
 
+  // Fragments are read kAhead products ahead: an LDS read takes about as long as
+  // four products.
+  constexpr int kAhead = 4, kSteps = D / 16;
   f16_t s[2];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-    const int row = b * 32 + r32;
+  // (offsets of the other steps and column blocks differ from the first's by an
+  // XOR; computed anew for each tile, they need no registers across tiles)
+  int k_at = r32 * D + (half ^ k_swizzle<D>(r32)) * 8, v_at = vt_offset<D>(lane);
+  asm volatile("" : "+v"(k_at), "+v"(v_at));
+  auto key_frag = [&](int n) {  // keys n % 2, step n / 2
+    return *(const u32x4_t*)(kst + (k_at ^ ((n / 2) * 16)) + (n % 2) * 32 * D);
+  };
+  u32x4_t kf[kAhead];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      const u32x4_t kf = *(const u32x4_t*)(kst + row * D + ((2 * i + half) ^ k_swizzle<D>(row)) * 8);
-      s[b] = mfma32<BF>(kf, r.q[i], s[b]);
-    }
+  for (int n = 0; n < kAhead; ++n) kf[n] = key_frag(n);
+#pragma unroll
+  for (int n = 0; n < 2 * kSteps; ++n) {
+    s[n % 2] = mfma32<BF>(kf[n % kAhead], r.q[n / 2], s[n % 2]);
+    if (n + kAhead < 2 * kSteps) kf[n % kAhead] = key_frag(n + kAhead);
   }
 
   const bool full = base >= r.lo_max && base + kTile <= r.hi_min;
@@ -254,6 +295,9 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) r.acc[d] *= alpha;
   }
+  u32x4_t vf[kAhead];
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) vf[n] = read_vt<D>(vst, n % (D / 32), n / (D / 32), v_at);
   const float off = kShift - (r.m == -INFINITY ? 0.f : r.m);
   u32x4_t pf[4];
   float sum[2] = {0.f, 0.f};
@@ -270,10 +314,13 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
     }
   r.l += sum[0] + sum[1];
 
+  constexpr int kBlocks = D / 32;
 #pragma unroll
-  for (int st = 0; st < 4; ++st)
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d) r.acc[d] = mfma32<BF>(read_vt<D>(vst, d, st, lane), pf[st], r.acc[d]);
+  for (int n = 0; n < 4 * kBlocks; ++n) {
+    r.acc[n % kBlocks] = mfma32<BF>(vf[n % kAhead], pf[n / kBlocks], r.acc[n % kBlocks]);
+    if (n + kAhead < 4 * kBlocks)
+      vf[n % kAhead] = read_vt<D>(vst, (n + kAhead) % kBlocks, (n + kAhead) / kBlocks, v_at);
+  }
   if (__builtin_expect(special, 0)) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -304,6 +351,8 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
 
   if (threadIdx.x == 0) scratch[9] = 0;  // (ordered by the barriers below)
   int parity = 0, turn = 0;
+  ChunkLoad<D, EXACT> ld;
+  ld.set(a, wave, lane);
   for (int64_t at = h.begin; at < h.end;) {
     const AttnUnit u = attn_find<kRows, kTile>(a, h, prefix, at);
     at += u.to - u.from;
@@ -331,11 +380,8 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
       for (int i = 0; i < 16; ++i) r.acc[d][i] = 0.f;
 
     if (u.k1 > u.k0) {
-      ChunkLoad<D, EXACT> ld;
       ld.k = a.k + u.head * a.k_head;
       ld.v = a.v + u.head * a.v_head;
-      ld.row0 = wave * ld.ROWS;
-      ld.inst0 = wave * ld.ROWS * D;
       int base = (u.tile0 + u.from) * kTile;
       const int end = (u.tile0 + u.to) * kTile;
       int ids = ld.page_id(a, u, base, lane);

@@ -300,6 +300,7 @@ int aqlm_paged_attention(const aqlm_heads* q, const aqlm_heads* out, float* lse,
   a.table_width = c->table_width;
   a.causal = causal != 0;
   a.window = window;
+  a.whole_rows = c->page_size >= 16 && std::max(c->k_slot_stride, c->v_slot_stride) < (1 << 25);
   const float scale_log2 = std::fabs(scale) * 1.44269504088896341f;
   a.scale_log2 = scale_log2 > 0.f ? scale_log2 : 1.f;
   a.q_keep = scale_log2 > 0.f ? 0xFFFFFFFFu : 0u;
