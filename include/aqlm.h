@@ -570,7 +570,7 @@ typedef struct aqlm_paged_cache {
   int32_t dtype;
 } aqlm_paged_cache;
 
-#define AQLM_MAX_SEQS 4096
+#define AQLM_MAX_SEQS 2032
 
 /* Norms and rotation as aqlm_rope on the way into the cache: q_out gets the
  * queries, the pages the keys and (unchanged) the values of the new tokens.  A

@@ -15,7 +15,8 @@
 // Division of the work.  Lengths live on the device (a captured launch serves
 // any lengths), so every workgroup adds up the tiles of all units by itself,
 // and takes an equal, contiguous share of the sequence (kv head, sequence,
-// unit, tile).  A share may hold many short units, or a piece of a long one.  A
+// unit, tile), where a unit counts as EXTRA tiles more than it has: what its
+// beginning and end cost.  A share may hold many short units, or a piece of a long one.  A
 // workgroup that holds a whole unit writes its rows.  The pieces of a split one
 // (unnormalised sums, maximum, denominator, all fp32) go to the workspace, where
 // a workgroup has two places: one for the unit that it continues, one for the
@@ -37,7 +38,7 @@ typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
 typedef float f2_t __attribute__((ext_vector_type(2)));
 typedef short s4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kAttnMaxSeqs = 4096;
+constexpr int kAttnMaxSeqs = 2032;  // (their entries and two stages of 256-element heads fill the LDS)
 
 struct AttnArgs {
   const uint16_t* q;
@@ -54,6 +55,7 @@ struct AttnArgs {
   int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
   int64_t table_stride;
   int32_t tokens, seqs, kv_heads, group, head_dim;
+  uint32_t group_mul, group_shift;  // row / group = hi32(row * group_mul) >> group_shift (group_mul 0: row)
   int32_t pages, page_shift, table_width;
   int32_t causal, window;
   int32_t whole_rows;  // 16 aligned keys share a page, their offsets in it fit 31 bits
@@ -85,6 +87,11 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int b) {
   return s;
 }
 
+// The token of a sequence's row (rows are below 2^31).
+__device__ __forceinline__ int attn_token(const AttnArgs& a, int row) {
+  return a.group_mul == 0 ? row : (int)(__umulhi((uint32_t)row, a.group_mul) >> a.group_shift);
+}
+
 // Keys [lo, hi) that token i of a sequence sees (hi <= lo: none).
 __device__ __forceinline__ void attn_visible(const AttnArgs& a, const AttnSeq& s, int i, int& lo, int& hi) {
   const int pos = s.keys - s.count + i;
@@ -97,8 +104,8 @@ __device__ __forceinline__ void attn_visible(const AttnArgs& a, const AttnSeq& s
 template <int R, int KT>
 __device__ __forceinline__ int attn_tiles(const AttnArgs& a, const AttnSeq& s, int t, int& tile0, int& k0, int& k1) {
   int lo, hi, x;
-  attn_visible(a, s, (int)((uint32_t)(t * R) / (uint32_t)a.group), lo, x);
-  attn_visible(a, s, min(s.count - 1, (int)((uint32_t)(t * R + R - 1) / (uint32_t)a.group)), x, hi);
+  attn_visible(a, s, attn_token(a, t * R), lo, x);
+  attn_visible(a, s, min(s.count - 1, attn_token(a, t * R + R - 1)), x, hi);
   k0 = lo;
   k1 = max(hi, lo);
   tile0 = lo / KT;
@@ -109,28 +116,47 @@ __device__ __forceinline__ int attn_units(const AttnArgs& a, const AttnSeq& s, i
   return (int)(((int64_t)s.count * a.group + R - 1) / R);
 }
 
-// Inclusive prefix sum over the wave.
+// Inclusive prefix sum over the wave, and its maximum of values above 0, by moves
+// between lanes (shuffles go through the LDS).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_0(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
 __device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
+  v += dpp_or_0<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += dpp_or_0<0x112, 0xF>(v);
+  v += dpp_or_0<0x114, 0xF>(v);
+  v += dpp_or_0<0x118, 0xF>(v);
+  v += dpp_or_0<0x142, 0xA>(v);  // row_bcast 15, 31
+  v += dpp_or_0<0x143, 0xC>(v);
   return v;
 }
+__device__ __forceinline__ int wave_most(int v) {
+  v = max(v, dpp_or_0<0x111, 0xF>(v));
+  v = max(v, dpp_or_0<0x112, 0xF>(v));
+  v = max(v, dpp_or_0<0x114, 0xF>(v));
+  v = max(v, dpp_or_0<0x118, 0xF>(v));
+  v = max(v, dpp_or_0<0x142, 0xA>(v));
+  v = max(v, dpp_or_0<0x143, 0xC>(v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// A sequence in LDS: the cost of one kv head before it, and what attn_seq says.
+struct __align__(16) AttnEntry {
+  int before, first, count, keys;
+};
 
 struct AttnShare {
-  int per_head;    // tiles of one kv head over all sequences
-  int64_t total;   // tiles of all heads
-  int64_t quota;   // tiles of a workgroup's share
+  int per_head;    // cost of one kv head over all sequences
+  int64_t total;   // cost of all heads
+  int64_t quota;   // cost of a workgroup's share
   int64_t slack;   // how far an end of a share moves to an end of a unit
   int64_t begin, end;
 };
 
 struct AttnUnit;
-template <int R, int KT>
-__device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare& h, const int* prefix, int64_t at);
+template <int R, int KT, int EXTRA>
+__device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare& h, const AttnEntry* list, int64_t at);
 
 // One unit of a share: where it is, and the part of its tiles that the share holds.
 struct AttnUnit {
@@ -138,77 +164,90 @@ struct AttnUnit {
   int b, head, t;
   int tile0, tiles, k0, k1;
   int from, to;         // tiles [from, to) of the unit are in the share
-  int64_t start;        // the unit's first tile in the sequence of all tiles
+  int64_t start, stop;  // where the unit's cost is in the sequence of all
 };
 
-// Fills `prefix` (LDS, seqs + 1 ints: tiles of one kv head before each
-// sequence; `scratch`: 2 * waves ints) and returns this workgroup's share.
-// `pieces`: the most whole shares that a unit is split into; `least`: tiles that a
-// share has at least.
-template <int R, int KT, int WAVES>
-__device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, int* prefix, int* scratch, int wg, int grid,
+// Unit i of a sequence in the order first, last, second, last but one, ...
+__device__ __forceinline__ int attn_folded(int i, int units) { return (i & 1) == 0 ? i / 2 : units - 1 - i / 2; }
+
+// Fills `list` (LDS, seqs + 1 entries; `scratch`: two ints per wave) and returns this
+// workgroup's share.  `pieces`: the most whole shares that a unit is split
+// into; `least`: the least cost of a share, if a unit has that much.
+template <int R, int KT, int EXTRA, int WAVES>
+__device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, AttnEntry* list, int* scratch, int wg, int grid,
                                                 int pieces, int least) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  int most = 1;
-  if (a.seqs <= WAVES) {  // few sequences, perhaps of many units: a wave for each
-    for (int b = wave; b < a.seqs; b += WAVES) {
-      const AttnSeq s = attn_seq(a, b);
-      const int units = attn_units(a, s, R);
-      int sum = 0, tile0, k0, k1;
-      for (int t = lane; t < units; t += kWave) {
-        const int n = attn_tiles<R, KT>(a, s, t, tile0, k0, k1);
-        sum += n;
-        most = max(most, n);
+  int most = 1, tile0, k0, k1;
+  // a thread per sequence; those of several units are left to a wave each
+  bool many = false;
+  for (int b = tid; b < a.seqs; b += WAVES * kWave) {
+    const AttnSeq s = attn_seq(a, b);
+    const int units = attn_units(a, s, R);
+    int cost = 0;
+    if (units == 1) cost = attn_tiles<R, KT>(a, s, 0, tile0, k0, k1) + EXTRA;
+    most = max(most, cost);
+    many |= units > 1;
+    list[b] = AttnEntry{units > 1 ? -1 : cost, s.first, s.count, s.keys};
+  }
+  const bool any = __ballot(many) != 0;
+  if (lane == 0) scratch[WAVES + wave] = any;
+  __syncthreads();
+  int marked = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) marked |= scratch[WAVES + w];
+  if (marked != 0) {
+    for (int i = 0; i < a.seqs; i += kWave) {
+      uint64_t left = __ballot(i + lane < a.seqs && list[i + lane].before == -1);
+      for (int n = 0; left != 0; ++n, left &= left - 1) {
+        if (n % WAVES != wave) continue;
+        const int b = i + __builtin_ctzll(left);
+        const AttnSeq s = {list[b].first, list[b].count, list[b].keys};
+        const int units = attn_units(a, s, R);
+        int sum = 0;
+        for (int t = lane; t < units; t += kWave) {
+          const int cost = attn_tiles<R, KT>(a, s, t, tile0, k0, k1) + EXTRA;
+          sum += cost;
+          most = max(most, cost);
+        }
+        sum = wave_scan(sum);
+        if (lane == kWave - 1) list[b].before = sum;
       }
-      sum = wave_scan(sum);
-      if (lane == kWave - 1) prefix[b + 1] = sum;
-    }
-  } else {
-    for (int b = tid; b < a.seqs; b += WAVES * kWave) {
-      const AttnSeq s = attn_seq(a, b);
-      const int units = attn_units(a, s, R);
-      int sum = 0, tile0, k0, k1;
-      for (int t = 0; t < units; ++t) {
-        const int n = attn_tiles<R, KT>(a, s, t, tile0, k0, k1);
-        sum += n;
-        most = max(most, n);
-      }
-      prefix[b + 1] = sum;
+      // (the marks of these 64 sequences are read before any is replaced only if the
+      // waves stay together)
+      __syncthreads();
     }
   }
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) most = max(most, __shfl_xor(most, d));
+  most = wave_most(most);
   if (lane == 0) scratch[wave] = most;
+  if (wave == 0) {  // costs to the costs before
+    int before = 0;
+    for (int b = 0; b < a.seqs; b += kWave) {
+      const int i = b + lane;
+      const int cost = i < a.seqs ? list[i].before : 0;
+      const int incl = wave_scan(cost) + before;
+      if (i < a.seqs) list[i].before = incl - cost;
+      before = __builtin_amdgcn_readlane(incl, kWave - 1);
+    }
+    if (lane == 0) list[a.seqs].before = before;
+  }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) most = max(most, scratch[w]);
-  // every wave scans the whole array in steps of 64; wave 0 writes it back
-  if (wave == 0) {
-    int before = 0;
-    if (lane == 0) prefix[0] = 0;
-    for (int b = 0; b < a.seqs; b += kWave) {
-      const int i = b + lane;
-      const int v = wave_scan(i < a.seqs ? prefix[i + 1] : 0) + before;
-      if (i < a.seqs) prefix[i + 1] = v;
-      before = __shfl(v, kWave - 1);
-    }
-  }
-  __syncthreads();
   AttnShare h;
-  h.per_head = prefix[a.seqs];
+  h.per_head = list[a.seqs].before;
   h.total = (int64_t)h.per_head * a.kv_heads;
   h.quota = max((h.total + grid - 1) / grid, (int64_t)((most + pieces - 1) / pieces));
-  h.quota = max(h.quota, (int64_t)least);
-  h.slack = h.quota / 8;
+  h.quota = max(h.quota, (int64_t)min(least, most));
+  h.slack = max(h.quota / 8, (int64_t)EXTRA);  // (a piece has a tile at least)
   h.begin = min(h.total, h.quota * wg);
   h.end = min(h.total, h.begin + h.quota);
   if (h.slack > 0) {
     const int64_t last = h.end;
     auto moved = [&](int64_t x) {
       if (x == 0 || x >= h.total) return x;
-      const AttnUnit u = attn_find<R, KT>(a, h, prefix, x);
-      if (u.from <= h.slack) return u.start;
-      return u.tiles - u.from <= h.slack ? u.start + u.tiles : x;
+      const AttnUnit u = attn_find<R, KT, EXTRA>(a, h, list, x);
+      if (x - u.start <= h.slack) return u.start;
+      return u.stop - x <= h.slack ? u.stop : x;
     };
     h.end = moved(last);
     h.begin = h.begin < last ? moved(h.begin) : h.end;
@@ -219,7 +258,7 @@ __device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, int* prefix, 
 // The workgroups that hold the first and the last piece of a unit.
 __device__ __forceinline__ void attn_holders(const AttnShare& h, const AttnUnit& u, int& w0, int& w1) {
   w0 = (int)((u.start + h.slack) / h.quota);
-  w1 = max(w0, (int)((u.start + u.tiles - h.slack - 1) / h.quota));
+  w1 = max(w0, (int)((u.stop - h.slack - 1) / h.quota));
 }
 
 // The place of piece p of a unit: of the unit that its workgroup begins (the
@@ -237,8 +276,11 @@ __device__ __forceinline__ f2_t get2(const float* p) {
   return __builtin_bit_cast(f2_t, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 __device__ __forceinline__ void put4(float* p, const f4_t& v) {
-  put2(p, v[0], v[1]);
-  put2(p + 2, v[2], v[3]);
+#if defined(__HIP_DEVICE_COMPILE__)
+  // one 16-byte store; the pause keeps its data registers as they are until it
+  // has read them (attn_last waits for it to reach memory)
+  asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(p), "v"(v) : "memory");
+#endif
 }
 __device__ __forceinline__ f4_t get4(const float* p) {
   const f2_t x = get2(p), y = get2(p + 2);
@@ -261,48 +303,53 @@ __device__ __forceinline__ bool attn_last(uint32_t* counter, int count, int* fla
   return *flag != 0;
 }
 
-// The unit that holds tile `at` of the sequence of all tiles.  Uniform over the
+// The unit that holds `at` of the sequence of all costs.  Uniform over the
 // workgroup; every wave finds it by itself.
-template <int R, int KT>
-__device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare& h, const int* prefix, int64_t at) {
+template <int R, int KT, int EXTRA>
+__device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare& h, const AttnEntry* list,
+                                              int64_t at) {
   const int lane = threadIdx.x & (kWave - 1);
   AttnUnit u;
-  u.head = (int)(at / h.per_head);
+  u.head = a.kv_heads == 1 ? 0 : (int)(at / h.per_head);
   const int rem = (int)(at - (int64_t)u.head * h.per_head);
-  // the last sequence with prefix <= rem (empty sequences have none of the tiles)
+  // the last sequence that begins at or before (empty ones have no cost)
   int b = 0;
   for (int i = 0; i < a.seqs; i += kWave) {
-    const uint64_t le = __ballot(i + lane < a.seqs && prefix[i + lane] <= rem);
+    const uint64_t le = __ballot(i + lane < a.seqs && list[i + lane].before <= rem);
     if (le == 0) break;
     b = i + 63 - __builtin_clzll(le);
   }
   u.b = __builtin_amdgcn_readfirstlane(b);
-  u.s = attn_seq(a, u.b);
-  int left = rem - prefix[u.b];
+  const AttnEntry e = list[u.b];
+  u.s.first = __builtin_amdgcn_readfirstlane(e.first);
+  u.s.count = __builtin_amdgcn_readfirstlane(e.count);
+  u.s.keys = __builtin_amdgcn_readfirstlane(e.keys);
+  int left = rem - e.before;
   const int units = attn_units(a, u.s, R);
   int tile0, k0, k1, t = 0;
   if (units > 1) {
     int before = 0;
-    auto unit_at = [&](int i) { return (i & 1) == 0 ? i / 2 : units - 1 - i / 2; };
     for (int i = 0; i < units; i += kWave) {
-      const int n = i + lane < units ? attn_tiles<R, KT>(a, u.s, unit_at(i + lane), tile0, k0, k1) : 0;
+      const int n = i + lane < units ? attn_tiles<R, KT>(a, u.s, attn_folded(i + lane, units), tile0, k0, k1) + EXTRA : 0;
       const int incl = wave_scan(n) + before;
       const uint64_t gt = __ballot(incl > left);
       if (gt != 0) {
         const int l = __builtin_ctzll(gt);
-        t = unit_at(i + l);
-        before = l > 0 ? __shfl(incl, l - 1) : before;
+        t = attn_folded(i + l, units);
+        before = l > 0 ? __builtin_amdgcn_readlane(incl, l - 1) : before;
         break;
       }
-      before = __shfl(incl, kWave - 1);
+      before = __builtin_amdgcn_readlane(incl, kWave - 1);
     }
     left -= before;
   }
   u.t = __builtin_amdgcn_readfirstlane(t);
   u.tiles = attn_tiles<R, KT>(a, u.s, u.t, u.tile0, u.k0, u.k1);
-  u.from = __builtin_amdgcn_readfirstlane(left);
-  u.start = at - u.from;
-  u.to = (int)min((int64_t)u.tiles, (int64_t)u.from + (h.end - at));
+  left = __builtin_amdgcn_readfirstlane(left);
+  u.start = at - left;
+  u.stop = u.start + u.tiles + EXTRA;
+  u.from = max(0, left - EXTRA);
+  u.to = (int)min((int64_t)u.tiles, h.end - u.start - EXTRA);
   return u;
 }
 

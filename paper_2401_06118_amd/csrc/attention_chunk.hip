@@ -37,7 +37,8 @@ constexpr int kWaveRows = 32;
 constexpr int kRows = kWaves * kWaveRows;
 constexpr int kTile = 64;
 constexpr int kPieces = 16;  // whole shares of a split unit: its last workgroup reads all pieces
-constexpr int kLeast = 4;     // tiles of a share: below, a piece costs more than it computes
+constexpr int kExtra = 2;
+constexpr int kLeast = 6;     // below, a piece costs more than it computes
 constexpr float kLazy = 8.f;
 
 typedef __attribute__((address_space(3))) s4_t lds_s4_t;
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
   extern __shared__ __align__(16) uint8_t lds[];
   uint16_t* const stages = (uint16_t*)lds;
   int* const scratch = (int*)(lds + ChunkLds<D>::kFixed - 64);
-  int* const prefix = scratch + 16;
+  AttnEntry* const list = (AttnEntry*)(scratch + 16);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r32 = lane & 31;
   const int grid = gridDim.x;
   const int wg = (grid & 7) == 0 ? (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3) : blockIdx.x;
@@ -347,31 +348,31 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
     for (int i = threadIdx.x; i < 2 * ChunkLds<D>::kStage / 8; i += kWaves * kWave)
       *(u32x4_t*)(stages + i * 8) = u32x4_t{0, 0, 0, 0};
   }
-  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces, kLeast);
+  const AttnShare h = attn_share<kRows, kTile, kExtra, kWaves>(a, list, scratch, wg, grid, kPieces, kLeast);
 
   if (threadIdx.x == 0) scratch[9] = 0;  // (ordered by the barriers below)
   int parity = 0, turn = 0;
   ChunkLoad<D, EXACT> ld;
   ld.set(a, wave, lane);
   for (int64_t at = h.begin; at < h.end;) {
-    const AttnUnit u = attn_find<kRows, kTile>(a, h, prefix, at);
-    at += u.to - u.from;
+    const AttnUnit u = attn_find<kRows, kTile, kExtra>(a, h, list, at);
+    at = min(u.stop, h.end);
     const int rows = min(kRows, u.s.count * a.group - u.t * kRows);
     const int left = rows - wave * kWaveRows;  // rows of this wave
     const bool active = left > 0;
     const uint32_t first = (uint32_t)(u.t * kRows + (active ? wave * kWaveRows : 0));
     const int mine = active ? min(left, kWaveRows) : 1;
     const uint32_t rr = first + (uint32_t)min(r32, mine - 1);
-    const int token = (int)(rr / (uint32_t)a.group);
+    const int token = attn_token(a, (int)rr);
     const int head = u.head * a.group + (int)(rr - (uint32_t)token * (uint32_t)a.group);
 
     ChunkRows<D> r;
     attn_visible(a, u.s, token, r.lo, r.hi);
-    attn_visible(a, u.s, (int)(first / (uint32_t)a.group), r.lo_min, r.hi_min);
-    attn_visible(a, u.s, (int)((first + (uint32_t)mine - 1) / (uint32_t)a.group), r.lo_max, r.hi_max);
+    attn_visible(a, u.s, attn_token(a, (int)first), r.lo_min, r.hi_min);
+    attn_visible(a, u.s, attn_token(a, (int)first + mine - 1), r.lo_max, r.hi_max);
     int unit_lo, unit_hi, x;  // keys that all of the unit's rows see
-    attn_visible(a, u.s, (int)((uint32_t)(u.t * kRows) / (uint32_t)a.group), x, unit_hi);
-    attn_visible(a, u.s, (int)((uint32_t)(u.t * kRows + rows - 1) / (uint32_t)a.group), unit_lo, x);
+    attn_visible(a, u.s, attn_token(a, u.t * kRows), x, unit_hi);
+    attn_visible(a, u.s, attn_token(a, u.t * kRows + rows - 1), unit_lo, x);
     r.m = -INFINITY;
     r.l = 0.f;
 #pragma unroll
@@ -425,29 +426,50 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
       write = attn_last(&a.counters[w0], n, scratch + 8);
       if (write) {
         if (active) {
+          // in the order of the keys, this workgroup's own piece from its registers
           const int row = wave * kWaveRows + r32;
-          float mm = -INFINITY;
-          for (int p = 0; p < n; ++p) mm = fmaxf(mm, get2(attn_place(a, w0, p, chunk_place<D>()) + kRows * D + 2 * row)[0]);
-          r.m = mm;
+          f16_t own[D / 32];
+          const float own_m = r.m, own_l = r.l;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) own[d] = r.acc[d];
+          r.m = -INFINITY;
           r.l = 0.f;
 #pragma unroll
           for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) r.acc[d][i] = 0.f;
+#pragma unroll 1
           for (int p = 0; p < n; ++p) {
-            const float* const pp = attn_place(a, w0, p, chunk_place<D>());
-            const f2_t ml = get2(pp + kRows * D + 2 * row);
-            const bool some = ml[0] != -INFINITY;
-            const float w = some ? rescale(ml[0] - mm) : 0.f;
-            r.l += some ? w * ml[1] : 0.f;
-            const float* const o = pp + wave * kWaveRows * D;
+            f4_t x[D / 8];
+            float pm, pl;
+            if (w0 + p == wg) {
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
+              for (int i = 0; i < D / 8; ++i)
+                x[i] = f4_t{own[i / 4][4 * (i % 4)], own[i / 4][4 * (i % 4) + 1], own[i / 4][4 * (i % 4) + 2],
+                            own[i / 4][4 * (i % 4) + 3]};
+              pm = own_m;
+              pl = own_l;
+            } else {
+              const float* const pp = attn_place(a, w0, p, chunk_place<D>());
+              const float* const o = pp + wave * kWaveRows * D + lane * 4;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const f4_t x = get4(o + ((d * 4 + i) * kWave + lane) * 4);
+              for (int i = 0; i < D / 8; ++i) x[i] = get4(o + i * kWave * 4);
+              const f2_t ml = get2(pp + kRows * D + 2 * row);
+              pm = ml[0];
+              pl = ml[1];
+            }
+            const float mn = fmaxf(r.m, pm);
+            const float base = mn == -INFINITY ? 0.f : mn;
+            const float wa = rescale(r.m - base), wb = rescale(pm - base);
+            const bool some = pm != -INFINITY;  // (a piece without keys of this row: nothing, whatever it holds)
+            r.m = mn;
+            r.l = r.l * wa + (some ? wb * pl : 0.f);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r.acc[d][4 * i + j] += some ? w * x[j] : 0.f;
+            for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float y = r.acc[i / 4][4 * (i % 4) + j];
+                r.acc[i / 4][4 * (i % 4) + j] = y * wa + (some ? wb * x[i][j] : 0.f);
               }
           }
         }
@@ -483,9 +505,9 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
 template <bool BF, int D, bool EXACT>
 hipError_t launch(const AttnArgs& a, int grid, hipStream_t s) {
   constexpr auto kern = k_attention_chunk<BF, D, EXACT>;
-  const hipError_t e = allow_dynamic_lds((const void*)kern, ChunkLds<D>::kFixed + (kAttnMaxSeqs + 1) * 4);
+  const hipError_t e = allow_dynamic_lds((const void*)kern, ChunkLds<D>::kFixed + (kAttnMaxSeqs + 1) * 16);
   if (e != hipSuccess) return e;
-  kern<<<grid, kWaves * kWave, ChunkLds<D>::kFixed + (a.seqs + 1) * 4, s>>>(a);
+  kern<<<grid, kWaves * kWave, ChunkLds<D>::kFixed + (a.seqs + 1) * 16, s>>>(a);
   return hipGetLastError();
 }
 

@@ -36,6 +36,8 @@ constexpr int kRows = 16;
 constexpr int kWaves = 4;
 constexpr int kWaveKeys = 32;
 constexpr int kTile = kWaves * kWaveKeys;
+constexpr int kExtra = 0;
+constexpr int kLeast = 1;
 constexpr int kPieces = 64;  // whole shares of a split unit (one piece more where it begins inside one)
 
 typedef __attribute__((address_space(3))) s4_t lds_s4_t;
@@ -45,9 +47,7 @@ struct StepLds {
   static constexpr int kPitch = D + 4;  // floats per row of the joined sums
   static constexpr int kStage = kWaves * kWaveKeys * D * 2;
   static constexpr int kJoin = kWaves * kRows * (kPitch + 2) * 4;
-  static constexpr int kWeights = (kPieces + 1) * kRows * 8;
-  static constexpr int kMax0 = kStage > kJoin ? kStage : kJoin;
-  static constexpr int kUnion = kMax0 > kWeights ? kMax0 : kWeights;
+  static constexpr int kUnion = kStage > kJoin ? kStage : kJoin;
   static constexpr int kFixed = kUnion + 64;  // + scratch: waves' maxima, the "last" flag
 };
 
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
   constexpr float kShift = BF ? 0.f : 14.f;  // fp16: weights up to 2^14, so that small ones stay normal
   extern __shared__ __align__(16) uint8_t lds[];
   int* const scratch = (int*)(lds + StepLds<D>::kUnion);
-  int* const prefix = scratch + 16;
+  AttnEntry* const list = (AttnEntry*)(scratch + 16);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int grid = gridDim.x;
   const int wg = (grid & 7) == 0 ? (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3) : blockIdx.x;
@@ -109,19 +109,19 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
   float* const join_m = join + kWaves * kRows * StepLds<D>::kPitch;  // [wave][row] maxima, then denominators
   const int pmask = (1 << a.page_shift) - 1;
 
-  const AttnShare h = attn_share<kRows, kTile, kWaves>(a, prefix, scratch, wg, grid, kPieces, 1);
+  const AttnShare h = attn_share<kRows, kTile, kExtra, kWaves>(a, list, scratch, wg, grid, kPieces, kLeast);
 
   for (int64_t at = h.begin; at < h.end;) {
-    const AttnUnit u = attn_find<kRows, kTile>(a, h, prefix, at);
-    at += u.to - u.from;
+    const AttnUnit u = attn_find<kRows, kTile, kExtra>(a, h, list, at);
+    at = min(u.stop, h.end);
     const int rows = min(kRows, u.s.count * a.group - u.t * kRows);
     const uint32_t rr = (uint32_t)(u.t * kRows + min(r16, rows - 1));
-    const int token = (int)(rr / (uint32_t)a.group);
+    const int token = attn_token(a, (int)rr);
     const int head = u.head * a.group + (int)(rr - (uint32_t)token * (uint32_t)a.group);
     int lo, hi, lo_max, hi_min, x;
     attn_visible(a, u.s, token, lo, hi);
-    attn_visible(a, u.s, (int)((uint32_t)(u.t * kRows) / (uint32_t)a.group), x, hi_min);
-    attn_visible(a, u.s, (int)((uint32_t)(u.t * kRows + rows - 1) / (uint32_t)a.group), lo_max, x);
+    attn_visible(a, u.s, attn_token(a, u.t * kRows), x, hi_min);
+    attn_visible(a, u.s, attn_token(a, u.t * kRows + rows - 1), lo_max, x);
 
     // elements past the head (its padding to D): zeros in q and k; v's only
     // reach sums that are not written
@@ -288,8 +288,8 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
     auto write = [&](int row, int d, f4_t o, float mm, float ll) {
       const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
       const uint32_t ur = (uint32_t)(u.t * kRows + row);
-      const int tok = u.s.first + (int)(ur / (uint32_t)a.group);
-      const int hd = u.head * a.group + (int)(ur % (uint32_t)a.group);
+      const int in_seq = attn_token(a, (int)ur), tok = u.s.first + in_seq;
+      const int hd = u.head * a.group + (int)ur - in_seq * a.group;
       if (d < a.head_dim) {
         if (ll == 0.f) o = f4_t{0, 0, 0, 0};
         u32x2_t w = {pack2<BF>(o[0] * inv, o[1] * inv), pack2<BF>(o[2] * inv, o[3] * inv)};
@@ -338,28 +338,40 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
       }
       done = attn_last(&a.counters[w0], n, scratch + 8);
       if (done) {
-        float* const ml = (float*)lds;  // [piece][row]: maximum, denominator
-        for (int i = threadIdx.x; i < n * rows; i += kWaves * kWave) {
-          const int p = i / rows, row = i - p * rows;
-          *(f2_t*)(ml + 2 * (p * kRows + row)) = get2(attn_place(a, w0, p, step_place<D>()) + kRows * D + 2 * row);
-        }
-        __syncthreads();
+        // in the order of the keys, four pieces' loads at a time, this
+        // workgroup's own from its registers
+        const int mine = wg - w0;
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
           const int i = t * (kWaves * kWave) + threadIdx.x, row = i / (D / 4), d = (i % (D / 4)) * 4;
           if (row >= rows) continue;
+          const f4_t own = o[t];
+          const float own_m = mm[t], own_l = ll[t];
           mm[t] = -INFINITY;
-          for (int p = 0; p < n; ++p) mm[t] = fmaxf(mm[t], ml[2 * (p * kRows + row)]);
           ll[t] = 0.f;
           o[t] = f4_t{0, 0, 0, 0};
-#pragma unroll 8
-          for (int p = 0; p < n; ++p) {
-            const f4_t po = get4(attn_place(a, w0, p, step_place<D>()) + row * D + d);
-            const f2_t pm = *(const f2_t*)(ml + 2 * (p * kRows + row));
-            if (pm[0] == -INFINITY) continue;
-            const float w = rescale(pm[0] - mm[t]);
-            o[t] += w * po;
-            ll[t] += w * pm[1];
+          for (int p0 = 0; p0 < n; p0 += 4) {
+            f4_t x[4];
+            f2_t ml[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              const float* const pp = attn_place(a, w0, min(p0 + p, n - 1), step_place<D>());
+              x[p] = get4(pp + row * D + d);
+              ml[p] = get2(pp + kRows * D + 2 * row);
+            }
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              if (p0 + p == mine) {
+                x[p] = own;
+                ml[p] = f2_t{own_m, own_l};
+              }
+              if (p0 + p >= n || ml[p][0] == -INFINITY) continue;  // (no keys of this row)
+              const float mn = fmaxf(mm[t], ml[p][0]);
+              const float wa = rescale(mm[t] - mn), wb = rescale(ml[p][0] - mn);
+              mm[t] = mn;
+              ll[t] = ll[t] * wa + wb * ml[p][1];
+              o[t] = o[t] * wa + wb * x[p];
+            }
           }
         }
       }
@@ -378,9 +390,9 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
 template <bool BF, int D, bool EXACT>
 hipError_t launch(const AttnArgs& a, int grid, hipStream_t s) {
   constexpr auto kern = k_attention_step<BF, D, EXACT>;
-  const hipError_t e = allow_dynamic_lds((const void*)kern, StepLds<D>::kFixed + (kAttnMaxSeqs + 1) * 4);
+  const hipError_t e = allow_dynamic_lds((const void*)kern, StepLds<D>::kFixed + (kAttnMaxSeqs + 1) * 16);
   if (e != hipSuccess) return e;
-  kern<<<grid, kWaves * kWave, StepLds<D>::kFixed + (a.seqs + 1) * 4, s>>>(a);
+  kern<<<grid, kWaves * kWave, StepLds<D>::kFixed + (a.seqs + 1) * 16, s>>>(a);
   return hipGetLastError();
 }
 

@@ -294,6 +294,11 @@ int aqlm_paged_attention(const aqlm_heads* q, const aqlm_heads* out, float* lse,
   a.seqs = c->seqs;
   a.kv_heads = c->kv_heads;
   a.group = (int32_t)group;
+  if (group > 1) {  // s = ceil(log2(group)): 2^(31 + s) / group, rounded up, divides rows below 2^31 exactly
+    const int s = 64 - __builtin_clzll((uint64_t)group - 1);
+    a.group_mul = (uint32_t)((uint64_t(1) << (31 + s)) / (uint64_t)group + 1);
+    a.group_shift = (uint32_t)(s - 1);
+  }
   a.head_dim = c->head_dim;
   a.pages = (int32_t)c->pages;
   a.page_shift = page_shift(c->page_size);
