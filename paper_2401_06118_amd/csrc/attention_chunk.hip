@@ -42,7 +42,6 @@ constexpr int kLeast = 6;     // below, a piece costs more than it computes
 constexpr float kLazy = 8.f;
 
 typedef __attribute__((address_space(3))) s4_t lds_s4_t;
-typedef __attribute__((address_space(3))) void lds_void_t;
 
 template <int D>
 constexpr int chunk_place() { return kRows * D + 2 * kRows; }
@@ -54,14 +53,34 @@ struct ChunkLds {
   static constexpr int kFixed = 2 * kStage * 2 + 64;   // bytes, with the scratch words
 };
 
-__device__ __forceinline__ void chunk_load_to_lds(const uint16_t* g, uint16_t* l) {
+typedef __attribute__((address_space(3))) const u32x4_t lds_v4;
+typedef __attribute__((address_space(3))) u32x4_t lds_w4;
+typedef const __attribute__((address_space(4))) int32_t const_i32;
+
+// (m0, named as clobbered, is one that the compiler never keeps a value in)
+#pragma clang diagnostic ignored "-Winline-asm"
+
+// 16 bytes per lane from base + offset (bytes) into LDS at `lds` + 16 * lane, without
+// a vector instruction for the address.  The compiler does not know of these
+// loads in flight: a stage is read after stage_ready only, and a wait of its
+// own for a vector load waits for these too, which is never too short.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const uint8_t* base) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_global_load_lds(g, (lds_void_t*)l, 16, 0, 0);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
+               : "memory", "m0");
 #endif
 }
-__device__ __forceinline__ u32x2_t chunk_read_tr(const uint16_t* l) {
+// The same from a lane's own address.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint16_t* from) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)l));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from)
+               : "memory", "m0");
+#endif
+}
+__device__ __forceinline__ u32x4_t chunk_read(uint32_t lds) { return *(lds_v4*)(uintptr_t)lds; }
+__device__ __forceinline__ u32x2_t chunk_read_tr(uint32_t lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(uintptr_t)lds));
 #else
   return u32x2_t{};
 #endif
@@ -128,27 +147,29 @@ struct ChunkLoad {
       at_v[i] = (uint32_t)(rl * (int)a.v_slot + (slot ^ v_swizzle<D>(row0 + rl)) * 8) * 2;
     }
   }
-  __device__ __forceinline__ int page_id(const AttnArgs& a, const AttnUnit& u, int base, int lane) const {
-    return attn_page(a, u.b, min(max(base + row0 + (lane & (ROWS - 1)), u.k0), u.k1 - 1));
+  // The page of the wave's rows of a tile (a scalar load; used a tile later).
+  __device__ __forceinline__ int page_id(const AttnArgs& a, const AttnUnit& u, int base) const {
+    const int key = min(max(base + row0, u.k0), u.k1 - 1);
+    return ((const_i32*)(uintptr_t)(a.block_table + u.b * a.table_stride))[key >> a.page_shift];
   }
-  __device__ __forceinline__ void issue(const AttnArgs& a, const AttnUnit& u, uint16_t* stage, int base, int ids,
+  __device__ __forceinline__ void issue(const AttnArgs& a, const AttnUnit& u, uint32_t stage, int base, int page,
                                         int lane) const {
     const int pmask = (1 << a.page_shift) - 1;
-    uint16_t* const to = stage + row0 * D;
+    const uint32_t to = stage + row0 * D * 2;
     if (a.whole_rows && base >= u.k0 && base + kTile <= u.k1) {  // the wave's rows are in one page
-      const int64_t id = __builtin_amdgcn_readfirstlane(ids), at = (base + row0) & pmask;
+      const int64_t id = min(max(page, 0), a.pages - 1), at = (base + row0) & pmask;
       const uint8_t* const pk = (const uint8_t*)(k + id * a.k_page + at * a.k_slot);
       const uint8_t* const pv = (const uint8_t*)(v + id * a.v_page + at * a.v_slot);
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int row = row0 + i * RPI + lane / CH, slot = lane % CH;
-        uint16_t* const l = to + i * (kWave * 8);
-        if (EXACT || (slot ^ k_swizzle<D>(row)) * 8 < a.head_dim) chunk_load_to_lds((const uint16_t*)(pk + at_k[i]), l);
-        if (EXACT || (slot ^ v_swizzle<D>(row)) * 8 < a.head_dim)
-          chunk_load_to_lds((const uint16_t*)(pv + at_v[i]), l + ChunkLds<D>::kOperand);
+        const uint32_t l = to + i * (kWave * 16);
+        if (EXACT || (slot ^ k_swizzle<D>(row)) * 8 < a.head_dim) load_to_lds(l, at_k[i], pk);
+        if (EXACT || (slot ^ v_swizzle<D>(row)) * 8 < a.head_dim) load_to_lds(l + ChunkLds<D>::kOperand * 2, at_v[i], pv);
       }
       return;
     }
+    const int ids = attn_page(a, u.b, min(max(base + row0 + (lane & (ROWS - 1)), u.k0), u.k1 - 1));
 #pragma unroll 1
     for (int i = 0; i < PER; ++i) {
       const int rl = i * RPI + lane / CH, row = row0 + rl, slot = lane % CH;
@@ -157,44 +178,41 @@ struct ChunkLoad {
       const int ck = slot ^ k_swizzle<D>(row), cv = slot ^ v_swizzle<D>(row);
       const uint16_t* pk = k + id * a.k_page + at * a.k_slot + ck * 8;
       const uint16_t* pv = v + id * a.v_page + at * a.v_slot + cv * 8;
-      uint16_t* const l = to + i * (kWave * 8);
-      if (EXACT || ck * 8 < a.head_dim) chunk_load_to_lds(pk, l);
-      if (EXACT || cv * 8 < a.head_dim) chunk_load_to_lds(pv, l + ChunkLds<D>::kOperand);
+      const uint32_t l = to + i * (kWave * 16);
+      if (EXACT || ck * 8 < a.head_dim) load_to_lds(l, pk);
+      if (EXACT || cv * 8 < a.head_dim) load_to_lds(l + ChunkLds<D>::kOperand * 2, pv);
     }
   }
 };
 
-// V^T of 32 columns (block db) and 16 keys (step s), in P's key order; `at`:
-// vt_offset.
+// V^T of 32 columns (block db) and 16 keys (step s), in P's key order; `at`: the
+// values' LDS address plus vt_offset.
 template <int D>
-__device__ __forceinline__ int vt_offset(int lane) {
+__device__ __forceinline__ uint32_t vt_offset(int lane) {
   const int kr = 4 * (lane >> 5) + ((lane & 15) >> 2);
   const int c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-  return kr * D + (c ^ v_swizzle<D>(kr)) * 8 + (lane & 1) * 4;
+  return (kr * D + (c ^ v_swizzle<D>(kr)) * 8 + (lane & 1) * 4) * 2;
 }
 template <int D>
-__device__ __forceinline__ u32x4_t read_vt(const uint16_t* v, int db, int s, int at) {
-  const uint16_t* p = v + (at ^ (db * 32)) + 16 * s * D;
-  const u32x2_t x = chunk_read_tr(p), y = chunk_read_tr(p + 8 * D);
+__device__ __forceinline__ u32x4_t read_vt(uint32_t at, int db, int s) {
+  const uint32_t p = (at ^ (db * 64)) + 32 * s * D;
+  const u32x2_t x = chunk_read_tr(p), y = chunk_read_tr(p + 16 * D);
   return u32x4_t{x[0], x[1], y[0], y[1]};
 }
 
-// One tile: the next tile's loads go out, then this one is computed.  The two
-// stages are different memory (restrict): otherwise the compiler would wait for
-// the loads just issued before the first fragment read.
+// One tile: the next tile's loads go out (into stage `wr`), then this one (stage
+// `rd`, LDS addresses) is computed.
 template <bool BF, int D, bool EXACT>
-__device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u, const uint16_t* __restrict__ rd,
-                                           uint16_t* __restrict__ wr, const ChunkLoad<D, EXACT>& ld, int base,
-                                           bool more, int& ids, bool active, int unit_lo, int unit_hi, int* mark, int turn,
-                                           ChunkRows<D>& r) {
+__device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u, uint32_t rd, uint32_t wr,
+                                           const ChunkLoad<D, EXACT>& ld, int base, bool more, int& page, bool active,
+                                           int unit_lo, int unit_hi, int* mark, int turn, ChunkRows<D>& r) {
   constexpr float kShift = BF ? 0.f : 7.f;
   const int lane = threadIdx.x & 63, half = lane >> 5, r32 = lane & 31;
   if (more) {
-    ld.issue(a, u, wr, base + kTile, ids, lane);
-    ids = ld.page_id(a, u, base + 2 * kTile, lane);
+    ld.issue(a, u, wr, base + kTile, page, lane);
+    page = ld.page_id(a, u, base + 2 * kTile);
   }
-  const uint16_t* const kst = rd;
-  const uint16_t* const vst = rd + ChunkLds<D>::kOperand;
+  const uint32_t vst = rd + ChunkLds<D>::kOperand * 2;
 
   // Values that are not finite, in tiles that some row of the unit does not see
   // all of: each wave notes which of its rows' sums become infinite (bit i of
@@ -203,11 +221,11 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
   uint32_t flags[D / 32] = {};
   bool special = false;
   if (base < unit_lo || base + kTile > unit_hi) {
-    uint16_t* const mine = const_cast<uint16_t*>(vst) + (threadIdx.x / kWave) * (kTile / kWaves) * D;
+    const uint32_t mine = vst + (threadIdx.x / kWave) * (kTile / kWaves) * D * 2 + lane * 16;
     constexpr int PER = kTile * D / 8 / (kWaves * kWave);
     uint32_t odd = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) odd |= non_finite_any<BF>(*(const u32x4_t*)(mine + (i * kWave + lane) * 8));
+    for (int i = 0; i < PER; ++i) odd |= non_finite_any<BF>(chunk_read(mine + i * kWave * 16));
     if (__ballot(odd != 0) != 0 && lane == 0) *mark = turn;
     lds_barrier();
     special = *mark == turn;
@@ -226,7 +244,7 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
             seen[w] = (key >= r.lo && key < r.hi ? Bits16<BF>::kOne : 0u) |
                       (key + 1 >= r.lo && key + 1 < r.hi ? Bits16<BF>::kOne << 16 : 0u);
           }
-          const u32x4_t vf = read_vt<D>(vst, d, st, vt_offset<D>(lane));
+          const u32x4_t vf = read_vt<D>(vst + vt_offset<D>(lane), d, st);
           nu = mfma32<BF>(infinite_ones<BF>(vf, 0), seen, nu);
           nd = mfma32<BF>(infinite_ones<BF>(vf, 0x10001u), seen, nd);
         }
@@ -239,8 +257,8 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
       lds_barrier();
 #pragma unroll 1
       for (int i = 0; i < PER; ++i) {
-        u32x4_t* const p = (u32x4_t*)(mine + (i * kWave + lane) * 8);
-        *p = finite_or_zero<BF>(*p);
+        const uint32_t p = mine + i * kWave * 16;
+        *(lds_w4*)(uintptr_t)p = finite_or_zero<BF>(chunk_read(p));
       }
       lds_barrier();
     }
@@ -255,12 +273,11 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-  // (offsets of the other steps and column blocks differ from the first's by an
-  // XOR; computed anew for each tile, they need no registers across tiles)
-  int k_at = r32 * D + (half ^ k_swizzle<D>(r32)) * 8, v_at = vt_offset<D>(lane);
-  asm volatile("" : "+v"(k_at), "+v"(v_at));
+  // (the addresses of the other steps and column blocks differ from the first's by an
+  // XOR, and from those of other rows by a constant of the instruction)
+  uint32_t k_at = rd + (r32 * D + (half ^ k_swizzle<D>(r32)) * 8) * 2, v_at = vst + vt_offset<D>(lane);
   auto key_frag = [&](int n) {  // keys n % 2, step n / 2
-    return *(const u32x4_t*)(kst + (k_at ^ ((n / 2) * 16)) + (n % 2) * 32 * D);
+    return chunk_read((k_at ^ ((n / 2) * 32)) + (n % 2) * 32 * D * 2);
   };
   u32x4_t kf[kAhead];
 #pragma unroll
@@ -298,7 +315,7 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
   }
   u32x4_t vf[kAhead];
 #pragma unroll
-  for (int n = 0; n < kAhead; ++n) vf[n] = read_vt<D>(vst, n % (D / 32), n / (D / 32), v_at);
+  for (int n = 0; n < kAhead; ++n) vf[n] = read_vt<D>(v_at, n % (D / 32), n / (D / 32));
   const float off = kShift - (r.m == -INFINITY ? 0.f : r.m);
   u32x4_t pf[4];
   float sum[2] = {0.f, 0.f};
@@ -320,7 +337,7 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
   for (int n = 0; n < 4 * kBlocks; ++n) {
     r.acc[n % kBlocks] = mfma32<BF>(vf[n % kAhead], pf[n / kBlocks], r.acc[n % kBlocks]);
     if (n + kAhead < 4 * kBlocks)
-      vf[n % kAhead] = read_vt<D>(vst, (n + kAhead) % kBlocks, (n + kAhead) / kBlocks, v_at);
+      vf[n % kAhead] = read_vt<D>(v_at, (n + kAhead) % kBlocks, (n + kAhead) / kBlocks);
   }
   if (__builtin_expect(special, 0)) {
 #pragma unroll
@@ -336,11 +353,14 @@ __device__ __forceinline__ void chunk_tile(const AttnArgs& a, const AttnUnit& u,
 template <bool BF, int D, bool EXACT>
 __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_chunk(AttnArgs a) {
   constexpr float kShift = BF ? 0.f : 7.f;
+  constexpr uint32_t kStageBytes = ChunkLds<D>::kStage * 2;
   extern __shared__ __align__(16) uint8_t lds[];
   uint16_t* const stages = (uint16_t*)lds;
+  const uint32_t stage0 = (uint32_t)(uintptr_t)(lds_s4_t*)lds;
   int* const scratch = (int*)(lds + ChunkLds<D>::kFixed - 64);
   AttnEntry* const list = (AttnEntry*)(scratch + 16);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r32 = lane & 31;
+  const int lane = threadIdx.x & 63, half = lane >> 5, r32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grid = gridDim.x;
   const int wg = (grid & 7) == 0 ? (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3) : blockIdx.x;
 
@@ -385,9 +405,9 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
       ld.v = a.v + u.head * a.v_head;
       int base = (u.tile0 + u.from) * kTile;
       const int end = (u.tile0 + u.to) * kTile;
-      int ids = ld.page_id(a, u, base, lane);
-      ld.issue(a, u, stages + parity * ChunkLds<D>::kStage, base, ids, lane);
-      ids = ld.page_id(a, u, base + kTile, lane);
+      int page = ld.page_id(a, u, base);
+      ld.issue(a, u, stage0 + parity * kStageBytes, base, page, lane);
+      page = ld.page_id(a, u, base + kTile);
       const uint16_t* qp = a.q + (u.s.first + token) * a.q_token + head * a.q_head;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
@@ -398,9 +418,8 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
       }
       for (; base < end; base += kTile) {
         stage_ready();
-        chunk_tile<BF, D, EXACT>(a, u, stages + parity * ChunkLds<D>::kStage,
-                                 stages + (parity ^ 1) * ChunkLds<D>::kStage, ld, base, base + kTile < end, ids,
-                                 active, unit_lo, unit_hi, scratch + 9, ++turn, r);
+        chunk_tile<BF, D, EXACT>(a, u, stage0 + parity * kStageBytes, stage0 + (parity ^ 1) * kStageBytes, ld, base,
+                                 base + kTile < end, page, active, unit_lo, unit_hi, scratch + 9, ++turn, r);
         parity ^= 1;
       }
     }
