@@ -16,60 +16,32 @@ rules); this module only marshals arguments and makes output tensors.
 """
 from __future__ import annotations
 
-import ctypes
 import math
+import os
+import threading
 
 import torch
 
 from . import _check, _lib, _stream_handle
 
-_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
-_byref = ctypes.byref
+_lock = threading.Lock()
+_ext = None
 
 
-def _heads(name, t, tokens=None, heads=None, like=None):
-    """``aqlm_heads`` of a [tokens, heads, head_dim] tensor."""
-    if t.dim() != 3 or not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor [tokens, heads, head_dim]")
-    shape = t.shape
-    st = t.stride()
-    if st[2] != 1 and shape[2] > 1:
-        raise ValueError(f"the elements of a head of {name} must be contiguous")
-    if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads):
-        raise ValueError(f"{name} must be [{tokens}, {heads}, head_dim], got {tuple(shape)}")
-    if like is not None and (t.dtype != like.dtype or shape[2] != like.shape[2] or t.device != like.device):
-        raise ValueError(f"{name} must have the type, head size and device of the other activations")
-    if t.dtype not in _DTYPES:
-        raise ValueError(f"{name} must be fp16, bf16 or fp32")
-    # (the stride of a dimension of one is never used, whatever it says)
-    return _lib.Heads(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, shape[1])
-
-
-def _vector(name, t, like, n, dtype):
-    if t.dtype != dtype or t.numel() != n or not t.is_cuda or t.device != like.device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of {n} elements")
-    return t.data_ptr()
-
-
-def _rotation(like, table, q_weight, k_weight, eps, interleaved):
-    dim = like.shape[2]
-    r = _lib.Rotation()
-    if table is not None:
-        if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_cuda \
-                or table.device != like.device or not table.is_contiguous():
-            raise ValueError("table must be a contiguous fp32 GPU tensor [positions, rot / 2, 2]")
-        rot = 2 * table.shape[1]
-        if rot > dim:
-            raise ValueError(f"the table rotates {rot} elements of heads of {dim}")
-        r.rot = rot
-        if rot:
-            r.table, r.rows = table.data_ptr(), table.shape[0]
-    r.interleaved, r.eps = bool(interleaved), eps
-    if q_weight is not None:
-        r.q_weight = _vector("q_weight", q_weight, like, dim, like.dtype)
-    if k_weight is not None:
-        r.k_weight = _vector("k_weight", k_weight, like, dim, like.dtype)
-    return r
+def _binding():
+    """The C++ binding (raises if it has not been built)."""
+    global _ext
+    if _ext is None:
+        with _lock:
+            if _ext is None:
+                if not os.path.exists(os.path.join(_lib.HERE, "_block.so")):
+                    raise RuntimeError("_block.so is missing: build it with `python -m paper_2401_06118_amd.build` "
+                                       "(hipcc, gfx950). There is no CPU fallback.")
+                _lib.load()
+                from . import _block
+                _block.set_check(_check)
+                _ext = _block
+    return _ext
 
 
 def _made(stream, *tensors):
@@ -138,15 +110,6 @@ def rotary_table(positions: int, rot: int, *, base: float = 10000.0, scaling=Non
     return out
 
 
-def _like(t, out, name):
-    """A caller's output, checked, or a new contiguous one of t's shape."""
-    if out is None:
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device), True
-    if out.shape != t.shape or out.dtype != t.dtype or out.device != t.device:
-        raise ValueError(f"{name} must have the shape, type and device of its input")
-    return out, False
-
-
 def rope(q, k, table, positions, *, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
          out=None, stream=None):
     """Queries [tokens, heads, head_dim] and keys [tokens, kv heads, head_dim] with
@@ -155,18 +118,12 @@ def rope(q, k, table, positions, *, q_weight=None, k_weight=None, eps: float = 1
     :func:`rotary_table` makes it (it may rotate the first part of the head only);
     ``positions`` int32 [tokens].  Pairs are (i, i + rot / 2), or (2i, 2i + 1) with
     ``interleaved``.  ``out``: a (q', k') to write, which may be (q, k) itself."""
-    tokens = q.shape[0]
-    hq, hk = _heads("q", q), _heads("k", k, tokens, None, q)
-    r = _rotation(q, table, q_weight, k_weight, eps, interleaved)
-    oq, oq_new = _like(q, None if out is None else out[0], "out")
-    ok, ok_new = _like(k, None if out is None else out[1], "out")
-    if stream is not None:
-        _made(stream, oq if oq_new else None, ok if ok_new else None)
-    pos = _vector("positions", positions, q, tokens, torch.int32)
-    st = _lib.load().aqlm_rope(_byref(hq), _byref(hk), _byref(_heads("out", oq)), _byref(_heads("out", ok)),
-                               _DTYPES[q.dtype], tokens, q.shape[2], pos, _byref(r), _stream_handle(stream))
-    _check(st, "aqlm_rope")
-    return oq, ok
+    oq, ok = (None, None) if out is None else out
+    r = (_ext or _binding()).rope(q, k, table, positions, q_weight, k_weight, eps, interleaved, oq, ok,
+                                  _stream_handle(stream))
+    if stream is not None and out is None:
+        _made(stream, *r)
+    return r
 
 
 def rope_backward(dq, dk, table, positions, *, q=None, k=None, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -174,64 +131,12 @@ def rope_backward(dq, dk, table, positions, *, q=None, k=None, q_weight=None, k_
     """Gradients of :func:`rope`: ``dq``, ``dk`` are those of its outputs; returns
     those of q, k and (fp32 [head_dim], or None) of the two weights.  ``q`` and
     ``k``, what the forward read, are needed where there is a weight."""
-    tokens, dim = dq.shape[0], dq.shape[2] if dq.dim() == 3 else 0
-    hdq, hdk = _heads("dq", dq), _heads("dk", dk, tokens, None, dq)
-    r = _rotation(dq, table, q_weight, k_weight, eps, interleaved)
-    pos = _vector("positions", positions, dq, tokens, torch.int32)
-    gq, gq_new = _like(dq, None if out is None else out[0], "out")
-    gk, gk_new = _like(dk, None if out is None else out[1], "out")
-    if (q_weight is not None and q is None) or (k_weight is not None and k is None):
-        raise ValueError("q and k are needed where their norm has a weight")
-    hq = _byref(_heads("q", q, tokens, dq.shape[1], dq)) if q_weight is not None else None
-    hk = _byref(_heads("k", k, tokens, dk.shape[1], dq)) if k_weight is not None else None
-    wq = wk = ws = None
-    ws_bytes = 0
-    lib = _lib.load()
-    if hq or hk:
-        ws_bytes = int(lib.aqlm_rope_backward_workspace_bytes(dim))
-        both = torch.empty((2, dim), dtype=torch.float32, device=dq.device)
-        ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=dq.device)
-        wq = both[0] if hq else None
-        wk = both[1] if hk else None
-        if stream is not None:
-            _made(stream, both, ws)
+    oq, ok = (None, None) if out is None else out
+    r = (_ext or _binding()).rope_backward(dq, dk, table, positions, q, k, q_weight, k_weight, eps, interleaved, oq,
+                                           ok, _stream_handle(stream))
     if stream is not None:
-        _made(stream, gq if gq_new else None, gk if gk_new else None)
-    if tokens == 0:  # (nothing to sum over)
-        for w in (wq, wk):
-            if w is not None:
-                w.zero_()
-        return gq, gk, wq, wk
-    st = lib.aqlm_rope_backward(
-        _byref(hdq), _byref(hdk), hq, hk, _byref(_heads("out", gq)), _byref(_heads("out", gk)),
-        wq.data_ptr() if wq is not None else None, wk.data_ptr() if wk is not None else None, _DTYPES[dq.dtype],
-        tokens, dim, pos, _byref(r), ws.data_ptr() if ws is not None else None, ws_bytes, _stream_handle(stream))
-    _check(st, "aqlm_rope_backward")
-    return gq, gk, wq, wk
-
-
-def _cache(k_cache, v_cache, block_table, kv_lens, cu_new):
-    """``aqlm_paged_cache`` of the cache's tensors and the batch's integers."""
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if t.dim() != 4 or not t.is_cuda or t.dtype not in _DTYPES:
-            raise ValueError(f"{name} must be a GPU tensor [pages, page_size, kv heads, head_dim]")
-        if t.stride(3) != 1 and t.shape[3] > 1:
-            raise ValueError(f"the elements of a head of {name} must be contiguous")
-    if k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.device != v_cache.device:
-        raise ValueError("k_cache and v_cache must have one shape, type and device")
-    pages, page_size, kv_heads, dim = k_cache.shape
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.device != k_cache.device \
-            or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
-        raise ValueError("block_table must be an int32 tensor [sequences, pages] on the cache's device")
-    seqs, width = block_table.shape
-    ks, vs = k_cache.stride(), v_cache.stride()
-    if pages == 1 or page_size == 1 or kv_heads == 1:  # (such strides are never used, whatever they say)
-        ks, vs = ([s if n > 1 else 0 for s, n in zip(st, k_cache.shape)] for st in (ks, vs))
-    return _lib.PagedCache(
-        k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages,
-        block_table.data_ptr(), block_table.stride(0), _vector("kv_lens", kv_lens, k_cache, seqs, torch.int32),
-        _vector("cu_new", cu_new, k_cache, seqs + 1, torch.int32), width, seqs, page_size, kv_heads, dim,
-        _DTYPES[k_cache.dtype])
+        _made(stream, *(r if out is None else r[2:]))
+    return r[:4]
 
 
 def paged_append(q, k, v, k_cache, v_cache, block_table, kv_lens, cu_new, *, table=None, q_weight=None, k_weight=None,
@@ -244,23 +149,11 @@ def paged_append(q, k, v, k_cache, v_cache, block_table, kv_lens, cu_new, *, tab
     ``cu_new`` int32 [sequences + 1], where each sequence's new tokens begin among
     the activations.  Positions follow from these.  Without ``table`` nothing is
     rotated."""
-    c = _cache(k_cache, v_cache, block_table, kv_lens, cu_new)
-    tokens = k.shape[0]
-    hk, hv = _heads("k", k, tokens, c.kv_heads, k), _heads("v", v, tokens, c.kv_heads, k)
-    if k.dtype != k_cache.dtype or k.shape[2] != c.head_dim or k.device != k_cache.device:
-        raise ValueError("the activations must have the cache's type, head size and device")
-    r = _rotation(k, table, q_weight, k_weight, eps, interleaved)
-    hq = ho = oq = None
-    if q is not None:
-        hq = _byref(_heads("q", q, tokens, None, k))
-        oq, new = _like(q, out, "out")
-        ho = _byref(_heads("out", oq))
-        if new and stream is not None:
-            _made(stream, oq)
-    st = _lib.load().aqlm_paged_append(hq, _byref(hk), _byref(hv), ho, _byref(c), tokens, _byref(r),
-                                       _stream_handle(stream))
-    _check(st, "aqlm_paged_append")
-    return oq
+    r = (_ext or _binding()).paged_append(q, k, v, k_cache, v_cache, block_table, kv_lens, cu_new, table, q_weight,
+                                          k_weight, eps, interleaved, out, _stream_handle(stream))
+    if stream is not None and out is None:
+        _made(stream, r)
+    return r
 
 
 def attention_workspace(head_dim: int, device="cuda") -> torch.Tensor:
@@ -278,6 +171,8 @@ _workspaces = {}
 
 
 def _workspace(device, head_dim, stream_handle):
+    if head_dim % 8 or not 0 < head_dim <= 256 or device.type != "cuda":
+        raise ValueError("paged_attention takes GPU tensors and a head_dim that is a multiple of 8 up to 256")
     if torch.cuda.is_current_stream_capturing():
         # a graph's launches may run beside this stream's later ones: it gets its own
         return attention_workspace(head_dim, device)
@@ -304,37 +199,14 @@ def paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, *, scale=
     ``max_new``: the most new tokens of a sequence, if known (it chooses the kernel,
     not the result).  ``workspace``: as :func:`attention_workspace` makes it;
     without one, one per stream is kept."""
-    c = _cache(k_cache, v_cache, block_table, kv_lens, cu_new)
-    hq = _heads("q", q)
-    tokens, heads, dim = q.shape
-    if q.dtype != k_cache.dtype or dim != c.head_dim or q.device != k_cache.device:
-        raise ValueError("q must have the cache's type, head size and device")
-    if heads % c.kv_heads:
-        raise ValueError("the query heads must be a multiple of the kv heads")
     handle = _stream_handle(stream)
-    out, new = _like(q, out, "out")
-    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
     if workspace is None:
-        if dim % 8 or dim > 256:
-            raise ValueError("head_dim must be a multiple of 8 up to 256")
-        workspace = _workspace(q.device, dim, handle)
-    elif not workspace.is_cuda or workspace.device != q.device or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous GPU tensor on q's device")
+        workspace = _workspace(q.device, q.shape[-1], handle)
+    r = (_ext or _binding()).paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, scale, causal, window,
+                                             max_new, return_lse, out, workspace, handle)
     if stream is not None:
-        _made(stream, out if new else None, lse)
-    st = _lib.load().aqlm_paged_attention(
-        _byref(hq), _byref(_heads("out", out)), lse.data_ptr() if return_lse else None, _byref(c), tokens,
-        int(max_new), dim ** -0.5 if scale is None else scale, bool(causal), int(window), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), handle)
-    _check(st, "aqlm_paged_attention")
-    return (out, lse) if return_lse else out
-
-
-def _table2(name, t, rows, dtype, like):
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or not t.is_cuda or t.device != like.device \
-            or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name} must be a {dtype} GPU tensor [{rows}, n], its rows contiguous")
-    return t.data_ptr()
+        _made(stream, *(r if return_lse else (r,)))
+    return r
 
 
 def process_logits(logits, *, tokens=None, token_lens=None, prompt_lens=None, repetition=None, frequency=None,
@@ -349,52 +221,8 @@ def process_logits(logits, *, tokens=None, token_lens=None, prompt_lens=None, re
     [rows]; ``bias_ids`` int32 [rows, n] (negative: no entry) with ``bias_values`` fp32
     [rows, n]; ``mask`` int32 [rows, ceil(vocab / 32)], bit token % 32 of word token //
     32 set where the token is allowed.  ``out`` may be ``logits`` itself."""
-    if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in _DTYPES \
-            or (logits.stride(1) != 1 and logits.shape[1] > 1):
-        raise ValueError("logits must be an fp16, bf16 or fp32 GPU tensor [rows, vocab], its rows contiguous")
-    rows, vocab = logits.shape
-    r = _lib.LogitRules()
-    if tokens is not None:
-        if token_lens is None:
-            raise ValueError("tokens need token_lens")
-        r.tokens = _table2("tokens", tokens, rows, torch.int32, logits)
-        r.history, r.token_stride = tokens.shape[1], tokens.stride(0)
-        r.token_lens = _vector("token_lens", token_lens, logits, rows, torch.int32)
-        if prompt_lens is not None:
-            r.prompt_lens = _vector("prompt_lens", prompt_lens, logits, rows, torch.int32)
-    elif repetition is not None or frequency is not None or presence is not None:
-        raise ValueError("penalties need tokens")
-    if tokens is not None and tokens.shape[1] == 0:  # (nothing to penalise)
-        tokens = repetition = frequency = presence = None
-        r.tokens = r.token_lens = r.prompt_lens = None
-    if repetition is not None:
-        r.repetition = _vector("repetition", repetition, logits, rows, torch.float32)
-    if frequency is not None:
-        r.frequency = _vector("frequency", frequency, logits, rows, torch.float32)
-    if presence is not None:
-        r.presence = _vector("presence", presence, logits, rows, torch.float32)
-    if (bias_ids is None) != (bias_values is None):
-        raise ValueError("bias_ids and bias_values go together")
-    if bias_ids is not None:
-        if bias_ids.shape != bias_values.shape or bias_ids.stride() != bias_values.stride():
-            raise ValueError("bias_ids and bias_values must have one shape and layout")
-        r.bias_ids = _table2("bias_ids", bias_ids, rows, torch.int32, logits)
-        r.bias_values = _table2("bias_values", bias_values, rows, torch.float32, logits)
-        r.biases, r.bias_stride = bias_ids.shape[1], bias_ids.stride(0)
-    if mask is not None:
-        r.mask = _table2("mask", mask, rows, torch.int32, logits)
-        r.mask_stride = mask.stride(0)
-        if mask.shape[1] < (vocab + 31) // 32:
-            raise ValueError(f"mask must have {(vocab + 31) // 32} words per row")
-    if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-        if stream is not None:
-            _made(stream, out)
-    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device \
-            or (out.stride(1) != 1 and vocab > 1):
-        raise ValueError("out must have the shape, type and device of logits, its rows contiguous")
-    in_row, out_row = (logits.stride(0), out.stride(0)) if rows > 1 else (0, 0)
-    st = _lib.load().aqlm_process_logits(logits.data_ptr(), in_row, out.data_ptr(), out_row, _DTYPES[logits.dtype],
-                                         rows, vocab, _byref(r), _stream_handle(stream))
-    _check(st, "aqlm_process_logits")
-    return out
+    r = (_ext or _binding()).process_logits(logits, tokens, token_lens, prompt_lens, repetition, frequency, presence,
+                                            bias_ids, bias_values, mask, out, _stream_handle(stream))
+    if stream is not None and out is None:
+        _made(stream, r)
+    return r

@@ -1,7 +1,8 @@
 """Build the HIP library ``libaqlm_mi355x.so`` for gfx950 with hipcc.
 
 Each ``csrc/*.hip`` file compiles to an object in ``_build/`` (in parallel),
-then one shared library is linked next to this file.  Packed fp32 VALU ops
+then one shared library is linked next to this file, and the C++ binding of
+``block.py`` (``_block.so``) against it.  Packed fp32 VALU ops
 are switched off for the device code (``-packed-fp32-ops``); hipcc's host
 pass warns that it does not know that feature, which is harmless.
 """
@@ -20,6 +21,9 @@ LIB = os.path.join(HERE, "libaqlm_mi355x.so")
 # Measurement-only microbenchmarks (bench.py --floors), a library of their own.
 FLOORS_SRC = os.path.join(HERE, "floors", "floors.hip")
 FLOORS_LIB = os.path.join(HERE, "libaqlm_floors.so")
+# Python binding of the operators in block.py (host code, against torch's headers).
+BIND_SRC = os.path.join(CSRC, "block_bind.cpp")
+BIND_LIB = os.path.join(HERE, "_block.so")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -50,6 +54,29 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _bind(verbose: bool) -> None:
+    import sysconfig
+
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           sysconfig.get_paths()["include"]]
+    lib = os.path.join(root, "lib")
+    tmp = BIND_LIB + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-DUSE_ROCM",
+           "-D__HIP_PLATFORM_AMD__=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[a for i in inc for a in ("-isystem", i)], BIND_SRC, "-o", tmp, "-L", HERE,
+           "-l:" + os.path.basename(LIB), "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10",
+           "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed on {BIND_SRC}:\n{r.stdout}{r.stderr}")
+    os.replace(tmp, BIND_LIB)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
@@ -61,6 +88,7 @@ def build(verbose: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
+    _bind(verbose)
     tmp = FLOORS_LIB + ".tmp"
     cmd = [HIPCC, *FLAGS, "-shared", "-o", tmp, FLOORS_SRC]
     if verbose:

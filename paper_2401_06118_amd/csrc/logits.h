@@ -19,6 +19,7 @@ struct LogitsArgs {
   const uint32_t* mask;
   int64_t in_row, out_row, token_row, bias_row, mask_row;
   int32_t rows, vocab, history, biases;
+  int32_t slices_log2;
 };
 
 hipError_t launch_logits(const LogitsArgs& a, int dtype, hipStream_t s);

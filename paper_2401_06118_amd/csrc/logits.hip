@@ -12,7 +12,9 @@
 // words are integers, so the order of the atomics does not matter.  The slice's
 // logits are loaded into registers before the row's history is walked, which hides
 // the one under the other.  Every workgroup of a row walks the whole history
-// (4 bytes a token, from the L2 after the first).
+// (4 bytes a token, from the L2 after the first).  A slice is every 2^n-th block of
+// 64 tokens, not a range: frequent tokens have neighbouring numbers, and their
+// atomics would all be one workgroup's.
 #include "logits.h"
 
 #include "common.h"
@@ -55,14 +57,22 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
   int32_t* const ids = (int32_t*)(bias + a.biases);
   int32_t* const twice = ids + a.biases;         // a token has several biases
   const int tid = threadIdx.x, row = blockIdx.y;
-  const int base = blockIdx.x * kSlice;
+  const int turn = blockIdx.x, lg = a.slices_log2;
+  // place l of the slice holds token token_at(l)
+  auto token_at = [&](int l) { return ((((l >> 6) << lg) + turn) << 6) + (l & 63); };
+  // place of a token, or kSlice and more (ids outside the vocabulary too)
+  auto place_of = [&](int id) -> uint32_t {
+    const uint32_t block = (uint32_t)id >> 6;
+    if ((uint32_t)id >= (uint32_t)a.vocab || (int)(block & ((1u << lg) - 1)) != turn) return ~0u;
+    return ((block >> lg) << 6) + (id & 63);
+  };
   const T* const in = (const T*)a.in + row * a.in_row;
   T* const out = (T*)a.out + row * a.out_row;
 
   V4 x[PER / 4];
 #pragma unroll
   for (int j = 0; j < PER / 4; ++j) {
-    const int v = base + (j * kThreads + tid) * 4;
+    const int v = token_at((j * kThreads + tid) * 4);
     if (ALIGNED && v + 4 <= a.vocab) {
       x[j] = *(const V4*)(in + v);
     } else {
@@ -75,12 +85,10 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
   if (tid == 0) *twice = 0;
   lds_barrier();
 
-  const uint32_t slice = (uint32_t)min(kSlice, a.vocab - base);
   if (a.biases > 0) {
     for (int i = tid; i < a.biases; i += kThreads) {
-      const int id = a.bias_ids[row * a.bias_row + i];
-      const uint32_t at = (uint32_t)id - (uint32_t)base;
-      const bool here = id >= 0 && at < slice;
+      const uint32_t at = place_of(a.bias_ids[row * a.bias_row + i]);
+      const bool here = at < (uint32_t)kSlice;
       ids[i] = here ? (int)at : -1;
       bias[i] = here ? a.bias_values[row * a.bias_row + i] : 0.f;
       if (here) {  // the first bias of a token has the largest number here
@@ -104,12 +112,18 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
     const int n = min(max(a.token_lens[row], 0), a.history);
     const int p = a.prompt_lens != nullptr ? min(max(a.prompt_lens[row], 0), n) : 0;
     const int32_t* t = a.tokens + row * a.token_row;
-#pragma unroll 4
-    for (int i = tid; i < n; i += kThreads) {
-      const uint32_t at = (uint32_t)t[i] - (uint32_t)base;
-      if (at < slice) {
-        if (i < p) atomicOr(&word[at], kPrompt);
-        else atomicAdd(&word[at], 1u);
+    constexpr int kBatch = 8;  // loads in flight
+    for (int i0 = tid; i0 < n; i0 += kBatch * kThreads) {
+      int id[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) id[j] = i0 + j * kThreads < n ? t[i0 + j * kThreads] : -1;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const uint32_t at = place_of(id[j]);
+        if (at < (uint32_t)kSlice) {
+          if (i0 + j * kThreads < p) atomicOr(&word[at], kPrompt);
+          else atomicAdd(&word[at], 1u);
+        }
       }
     }
   }
@@ -120,7 +134,7 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
   const float pres = a.presence != nullptr ? a.presence[row] : 0.f;
 #pragma unroll
   for (int j = 0; j < PER / 4; ++j) {
-    const int l = (j * kThreads + tid) * 4, v = base + l;
+    const int l = (j * kThreads + tid) * 4, v = token_at(l);
     if (v >= a.vocab) continue;
     const u32x4_t w = *(const u32x4_t*)(word + l);
     uint32_t allowed = 0xFu;
@@ -148,9 +162,11 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
 }
 
 template <int TY, int PER>
-hipError_t launch(const LogitsArgs& a, bool aligned, hipStream_t s) {
+hipError_t launch(LogitsArgs a, bool aligned, hipStream_t s) {
   const size_t lds = (size_t)kThreads * PER * 4 + (size_t)a.biases * 8 + 16;
-  const dim3 grid((unsigned)((a.vocab + kThreads * PER - 1) / (kThreads * PER)), (unsigned)a.rows);
+  a.slices_log2 = 0;
+  while ((int64_t)kThreads * PER << a.slices_log2 < a.vocab) ++a.slices_log2;
+  const dim3 grid(1u << a.slices_log2, (unsigned)a.rows);
   if (aligned) k_logits<TY, PER, true><<<grid, kThreads, lds, s>>>(a);
   else k_logits<TY, PER, false><<<grid, kThreads, lds, s>>>(a);
   return hipGetLastError();

@@ -85,33 +85,37 @@ __device__ __forceinline__ int paged_page(const RopeArgs& a, int seq, int pos) {
   return p >= 0 && p < a.pages ? p : -1;
 }
 
-// A lane's two pieces of a head (in units of 8 elements); `on`: it has any.
+// A lane's two pieces of a head (in units of 8 elements), whether the head has
+// them, and the first of the 4 pairs of each half of the lane's 8.
 struct Pieces {
   int c[2];
   bool on[2];
-  int pair;  // its first pair; 8 pairs
+  int pair[2];
 };
 template <bool INTER>
-__device__ __forceinline__ Pieces pieces_of(const RopeArgs& a, int i) {
+__device__ __forceinline__ Pieces pieces_of(const RopeArgs& a, int i, int lanes) {
   Pieces p;
   const int ch = a.head_dim / 8;
-  if (INTER || i >= a.rot / 16) {
-    const int c0 = INTER ? 2 * i : a.rot / 8 + 2 * (i - a.rot / 16);
-    p.c[0] = c0;
-    p.c[1] = c0 + 1;
-  } else {
+  if (INTER) {  // pairs lie within a piece: neighbouring lanes take neighbouring ones
+    p.c[0] = i;
+    p.c[1] = i + lanes;
+  } else if (i < a.rot / 16) {
     p.c[0] = i;
     p.c[1] = i + a.rot / 16;
+  } else {
+    p.c[0] = a.rot / 8 + 2 * (i - a.rot / 16);
+    p.c[1] = p.c[0] + 1;
   }
   p.on[0] = p.c[0] < ch;
   p.on[1] = p.c[1] < ch;
-  p.pair = 8 * i;
+  p.pair[0] = INTER ? 4 * p.c[0] : 8 * i;
+  p.pair[1] = INTER ? 4 * p.c[1] : 8 * i + 4;
   return p;
 }
 
 // cos and sin of a lane's 8 pairs; pairs past the rotated part are left as they
 // are.  False for a position that the table does not have.
-__device__ __forceinline__ bool load_turn(const RopeArgs& a, int pos, int pair, float (&c)[8], float (&s)[8]) {
+__device__ __forceinline__ bool load_turn(const RopeArgs& a, int pos, const Pieces& p, float (&c)[8], float (&s)[8]) {
   const int half = a.rot / 2;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -120,24 +124,27 @@ __device__ __forceinline__ bool load_turn(const RopeArgs& a, int pos, int pair, 
   }
   if (half == 0) return true;
   if (pos < 0 || pos >= a.rows) return false;
-  const float* t = a.table + ((int64_t)pos * half + pair) * 2;
-  if (pair + 8 <= half) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 v = *(const float4*)(t + 4 * i);
-      c[2 * i] = v.x;
-      s[2 * i] = v.y;
-      c[2 * i + 1] = v.z;
-      s[2 * i + 1] = v.w;
-    }
-  } else {
+  for (int e = 0; e < 2; ++e) {
+    const float* t = a.table + ((int64_t)pos * half + p.pair[e]) * 2;
+    if (p.pair[e] + 4 <= half) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (pair + i < half) {
-        const float2 v = *(const float2*)(t + 2 * i);
-        c[i] = v.x;
-        s[i] = v.y;
+      for (int i = 0; i < 2; ++i) {
+        const float4 v = *(const float4*)(t + 4 * i);
+        c[4 * e + 2 * i] = v.x;
+        s[4 * e + 2 * i] = v.y;
+        c[4 * e + 2 * i + 1] = v.z;
+        s[4 * e + 2 * i + 1] = v.w;
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (p.pair[e] + i < half) {
+          const float2 v = *(const float2*)(t + 2 * i);
+          c[4 * e + i] = v.x;
+          s[4 * e + i] = v.y;
+        }
+    }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) s[i] *= a.sign;
@@ -183,7 +190,7 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int lanes, int per_tok
   const int token = live ? (int)(item / per_token) : 0;
   const int h0 = live ? (int)(item - (int64_t)token * per_token) * HPT : 0;
   const int nq = a.side[0].heads, nk = a.side[1].heads, all = nq + nk + (PAGED ? a.side[2].heads : 0);
-  const Pieces p = pieces_of<INTER>(a, i);
+  const Pieces p = pieces_of<INTER>(a, i, lanes);
 
   V x[HPT][2];
 #pragma unroll
@@ -199,7 +206,7 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int lanes, int per_tok
   const int pos = PAGED ? paged_position(a, token, seq) : a.positions[token];
   if (PAGED) page = paged_page(a, seq, pos);
   float c[8], s[8];
-  const bool inside = load_turn(a, pos, p.pair, c, s);
+  const bool inside = load_turn(a, pos, p, c, s);
   const bool rotates = INTER ? true : i < a.rot / 16;
 
 #pragma unroll
@@ -257,7 +264,7 @@ __global__ void __launch_bounds__(256) k_rope_grad(RopeArgs a, int lanes) {
   const int w = (int)blockIdx.x < a.blocks[0] ? 0 : 1;
   const int block = (int)blockIdx.x - (w ? a.blocks[0] : 0), blocks = a.blocks[w];
   const RopeSide& sd = a.side[w];
-  const Pieces p = pieces_of<INTER>(a, i);
+  const Pieces p = pieces_of<INTER>(a, i, lanes);
   const bool rotates = INTER ? true : i < a.rot / 16;
   float wt[16], dw[16];
 #pragma unroll
@@ -285,7 +292,7 @@ __global__ void __launch_bounds__(256) k_rope_grad(RopeArgs a, int lanes) {
       xv[e] = load8<TY>(sd.x, xo + p.c[e] * 8, live && p.on[e]);
     }
     float c[8], s[8];
-    const bool inside = load_turn(a, a.positions[token], p.pair, c, s);
+    const bool inside = load_turn(a, a.positions[token], p, c, s);
     float g[16], x[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -576,7 +583,7 @@ hipError_t launch_grad(const RopeArgs& a, bool vec, hipStream_t s) {
 bool rope_vector(const RopeArgs& a, int dtype, bool paged, bool grad) {
   const int64_t unit = 16 / dtype_bytes(dtype);
   if (a.head_dim % 8 != 0 || a.head_dim > 512 || (!a.interleaved && a.rot % 16 != 0)) return false;
-  if (((uintptr_t)a.table & 15) != 0 || (a.rot % 4 != 0 && a.rot >= 16)) return false;
+  if (((uintptr_t)a.table & 15) != 0 || (a.rot % 4 != 0 && a.rot >= 8)) return false;
   uintptr_t p = 0;
   int64_t st = 0;
   for (int i = 0; i < (paged ? 3 : 2); ++i) {
