@@ -45,17 +45,20 @@ struct Logit<kF32> {
   typedef float T;
 };
 
-// PER logits a thread, in vectors of 4 (ALIGNED: the rows allow it).
+// PER logits a thread, in vectors of 4 (ALIGNED: rows and vocabulary allow it).
+// STREAM: outputs that do not fit the L2s go past them.
 template <int TY, int PER, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
   typedef typename Logit<TY>::T T;
   typedef T V4 __attribute__((ext_vector_type(4)));
   constexpr int kSlice = kThreads * PER;
+  constexpr bool STREAM = PER > 4;
   extern __shared__ __align__(16) uint32_t lds[];
   uint32_t* const word = lds;                    // [kSlice]
   float* const bias = (float*)(lds + kSlice);    // [biases]
   int32_t* const ids = (int32_t*)(bias + a.biases);
   int32_t* const twice = ids + a.biases;         // a token has several biases
+  uint32_t* const marks = (uint32_t*)twice + 1;  // a bit per bias: the first of several
   const int tid = threadIdx.x, row = blockIdx.y;
   const int turn = blockIdx.x, lg = a.slices_log2;
   // place l of the slice holds token token_at(l)
@@ -69,76 +72,114 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
   const T* const in = (const T*)a.in + row * a.in_row;
   T* const out = (T*)a.out + row * a.out_row;
 
+  // All loads go out first, those that are needed first before the logits: waiting
+  // for one after another took half of the kernel's time.
+  constexpr int kBatch = 8;  // of the history, per thread
+  const int32_t* const t = a.tokens + row * a.token_row;
+  // (No load is under a condition of its own lane, but cut to the arrays' ends: the
+  // compiler's waits for the first ones then leave the later ones in flight.)
+  int id[kBatch], bias_id = -1;
+  float bias_value = 0.f;
+  if (a.tokens != nullptr) {
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) id[j] = t[min(tid + j * kThreads, a.history - 1)];
+  }
+  if (a.biases > 0) {
+    bias_id = a.bias_ids[row * a.bias_row + min(tid, a.biases - 1)];
+    bias_value = a.bias_values[row * a.bias_row + min(tid, a.biases - 1)];
+  }
+  const int n = a.tokens != nullptr ? min(max(a.token_lens[row], 0), a.history) : 0;
+  const int p = a.prompt_lens != nullptr ? min(max(a.prompt_lens[row], 0), n) : 0;
+  const float rep = a.repetition != nullptr ? a.repetition[row] : 1.f;
+  const float freq = a.frequency != nullptr ? a.frequency[row] : 0.f;
+  const float pres = a.presence != nullptr ? a.presence[row] : 0.f;
+  uint32_t allowed[PER / 4];
+#pragma unroll
+  for (int j = 0; j < PER / 4; ++j) allowed[j] = 0xFFFFFFFFu;
+  if (a.mask != nullptr) {
+#pragma unroll
+    for (int j = 0; j < PER / 4; ++j)
+      allowed[j] = a.mask[row * a.mask_row + min(token_at((j * kThreads + tid) * 4), a.vocab - 1) / 32];
+  }
   V4 x[PER / 4];
 #pragma unroll
   for (int j = 0; j < PER / 4; ++j) {
     const int v = token_at((j * kThreads + tid) * 4);
-    if (ALIGNED && v + 4 <= a.vocab) {
-      x[j] = *(const V4*)(in + v);
+    if constexpr (ALIGNED) {
+      x[j] = *(const V4*)(in + min(v, a.vocab - 4));
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[j][e] = v + e < a.vocab ? in[v + e] : (T)0.f;
+      for (int e = 0; e < 4; ++e) x[j][e] = in[min(v + e, a.vocab - 1)];
     }
   }
 #pragma unroll
   for (int j = 0; j < PER / 4; ++j) *(u32x4_t*)(word + (j * kThreads + tid) * 4) = u32x4_t{0, 0, 0, 0};
   if (tid == 0) *twice = 0;
+  if (tid < (a.biases + 31) / 32) marks[tid] = 0;
   lds_barrier();
 
   if (a.biases > 0) {
-    for (int i = tid; i < a.biases; i += kThreads) {
-      const uint32_t at = place_of(a.bias_ids[row * a.bias_row + i]);
+    auto note = [&](int i, int token, float value) {
+      const uint32_t at = place_of(token);
       const bool here = at < (uint32_t)kSlice;
       ids[i] = here ? (int)at : -1;
-      bias[i] = here ? a.bias_values[row * a.bias_row + i] : 0.f;
+      bias[i] = value;
       if (here) {  // the first bias of a token has the largest number here
         const uint32_t old = atomicMax(&word[at], (uint32_t)(a.biases - i) << kBiasShift);
         if (old != 0) *twice = 1;
       }
-    }
+    };
+    if (tid < a.biases) note(tid, bias_id, bias_value);
+    for (int i = tid + kThreads; i < a.biases; i += kThreads)
+      note(i, a.bias_ids[row * a.bias_row + i], a.bias_values[row * a.bias_row + i]);
     lds_barrier();
-    if (*twice) {  // the first one takes the sum, in the order of the list
+    if (*twice) {
+      // The first bias of such a token takes the sum, in the order of the list: marked
+      // by the others, then a wave for each, 64 entries of the list at a time.
       for (int i = tid; i < a.biases; i += kThreads) {
-        const int at = ids[i];
-        if (at < 0 || (word[at] & ~kPrompt) >> kBiasShift != (uint32_t)(a.biases - i)) continue;
-        float t = bias[i];
-        for (int j = i + 1; j < a.biases; ++j)
-          if (ids[j] == at) t += bias[j];
-        bias[i] = t;  // (read by this thread only: later ones are not first)
+        if (ids[i] < 0) continue;
+        const int first = a.biases - (int)((word[ids[i]] & ~kPrompt) >> kBiasShift);
+        if (first != i) atomicOr(&marks[first / 32], 1u << (first % 32));
       }
-    }
-  }
-  if (a.tokens != nullptr) {
-    const int n = min(max(a.token_lens[row], 0), a.history);
-    const int p = a.prompt_lens != nullptr ? min(max(a.prompt_lens[row], 0), n) : 0;
-    const int32_t* t = a.tokens + row * a.token_row;
-    constexpr int kBatch = 8;  // loads in flight
-    for (int i0 = tid; i0 < n; i0 += kBatch * kThreads) {
-      int id[kBatch];
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) id[j] = i0 + j * kThreads < n ? t[i0 + j * kThreads] : -1;
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        const uint32_t at = place_of(id[j]);
-        if (at < (uint32_t)kSlice) {
-          if (i0 + j * kThreads < p) atomicOr(&word[at], kPrompt);
-          else atomicAdd(&word[at], 1u);
+      lds_barrier();
+      const int lane = tid % kWave;
+      for (int m = tid / kWave; m < (a.biases + 31) / 32; m += kThreads / kWave) {
+        for (uint32_t left = marks[m]; left != 0; left &= left - 1) {
+          const int i = m * 32 + __builtin_ctz(left), at = ids[i];
+          float sum = bias[i];
+          for (int j = i + 1; j < a.biases; j += kWave)
+            for (uint64_t same = __ballot(j + lane < a.biases && ids[min(j + lane, a.biases - 1)] == at); same != 0;
+                 same &= same - 1)
+              sum += bias[j + __builtin_ctzll(same)];
+          if (lane == 0) bias[i] = sum;  // (only the first ones' are read from here on)
         }
       }
     }
   }
+  auto count = [&](int i, int token) {
+    const uint32_t at = place_of(token);
+    if (i < n && at < (uint32_t)kSlice) {
+      if (i < p) atomicOr(&word[at], kPrompt);
+      else atomicAdd(&word[at], 1u);
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < kBatch; ++j)
+    if (a.tokens != nullptr) count(tid + j * kThreads, id[j]);
+  // (the rest in a loop of its own: there a load's wait is one for the logits too)
+  for (int i0 = tid + kBatch * kThreads; i0 < n; i0 += kBatch * kThreads) {
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) id[j] = i0 + j * kThreads < n ? t[i0 + j * kThreads] : -1;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) count(i0 + j * kThreads, id[j]);
+  }
   lds_barrier();
 
-  const float rep = a.repetition != nullptr ? a.repetition[row] : 1.f;
-  const float freq = a.frequency != nullptr ? a.frequency[row] : 0.f;
-  const float pres = a.presence != nullptr ? a.presence[row] : 0.f;
 #pragma unroll
   for (int j = 0; j < PER / 4; ++j) {
     const int l = (j * kThreads + tid) * 4, v = token_at(l);
     if (v >= a.vocab) continue;
     const u32x4_t w = *(const u32x4_t*)(word + l);
-    uint32_t allowed = 0xFu;
-    if (a.mask != nullptr) allowed = a.mask[row * a.mask_row + v / 32] >> (v % 32);
     V4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -149,10 +190,11 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
         if (count != 0) f = f - freq * (float)count - pres;
         if (first != 0) f += bias[a.biases - (int)first];
       }
-      y[e] = (T)((allowed >> e) & 1 ? f : -INFINITY);
+      y[e] = (T)((allowed[j] >> (v % 32 + e)) & 1 ? f : -INFINITY);
     }
-    if (ALIGNED && v + 4 <= a.vocab) {
-      *(V4*)(out + v) = y;
+    if constexpr (ALIGNED) {
+      if constexpr (STREAM) __builtin_nontemporal_store(y, (V4*)(out + v));
+      else *(V4*)(out + v) = y;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -163,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) k_logits(LogitsArgs a) {
 
 template <int TY, int PER>
 hipError_t launch(LogitsArgs a, bool aligned, hipStream_t s) {
-  const size_t lds = (size_t)kThreads * PER * 4 + (size_t)a.biases * 8 + 16;
+  const size_t lds = (size_t)kThreads * PER * 4 + (size_t)a.biases * 8 + (size_t)((a.biases + 31) / 32) * 4 + 16;
   a.slices_log2 = 0;
   while ((int64_t)kThreads * PER << a.slices_log2 < a.vocab) ++a.slices_log2;
   const dim3 grid(1u << a.slices_log2, (unsigned)a.rows);
@@ -175,7 +217,7 @@ hipError_t launch(LogitsArgs a, bool aligned, hipStream_t s) {
 template <int TY>
 hipError_t launch_typed(const LogitsArgs& a, hipStream_t s) {
   const uintptr_t v4 = 4 * (uintptr_t)dtype_bytes(TY) - 1;
-  const bool aligned = (((uintptr_t)a.in | (uintptr_t)a.out) & v4) == 0 && ((a.in_row | a.out_row) & 3) == 0;
+  const bool aligned = (((uintptr_t)a.in | (uintptr_t)a.out) & v4) == 0 && ((a.in_row | a.out_row | a.vocab) & 3) == 0;
   // slices of 8192 tokens, or of 2048 where those would leave CUs without one
   const int64_t wgs = (int64_t)a.rows * ((a.vocab + 16 * kThreads - 1) / (16 * kThreads));
   return wgs >= num_cus() ? launch<TY, 16>(a, aligned, s) : launch<TY, 4>(a, aligned, s);

@@ -172,12 +172,17 @@ __device__ __forceinline__ typename Elem<TY>::V load8(const void* base, int64_t 
   for (int i = 0; i < 8; ++i) v[i] = (typename Elem<TY>::T)0.f;
   return v;
 }
-template <int TY>
+// STREAM: past the L2s, for outputs that do not fit them (4096 tokens of 72
+// heads of 128 in bf16, with norms: 41 us with plain stores, 32 with these).
+template <int TY, bool STREAM>
 __device__ __forceinline__ void store8(void* base, int64_t off, const float* y) {
-  typename Elem<TY>::V v;
+  typedef typename Elem<TY>::V V;
+  V v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (typename Elem<TY>::T)y[i];
-  *(typename Elem<TY>::V*)((typename Elem<TY>::T*)base + off) = v;
+  V* const to = (V*)((typename Elem<TY>::T*)base + off);
+  if constexpr (STREAM) __builtin_nontemporal_store(v, to);
+  else *to = v;
 }
 
 // HPT heads of a token for a group of `lanes` lanes; heads counted over q, k (and v).
@@ -250,7 +255,7 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int lanes, int per_tok
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      if (p.on[e]) store8<TY>(out, off + p.c[e] * 8, y + e * 8);
+      if (p.on[e]) store8<TY, (HPT > 1)>(out, off + p.c[e] * 8, y + e * 8);
   }
 }
 
@@ -322,7 +327,7 @@ __global__ void __launch_bounds__(256) k_rope_grad(RopeArgs a, int lanes) {
     const int64_t oo = token * sd.out_token + h * sd.out_head;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      if (p.on[e]) store8<TY>(sd.out, oo + p.c[e] * 8, g + e * 8);
+      if (p.on[e]) store8<TY, true>(sd.out, oo + p.c[e] * 8, g + e * 8);
   }
 #pragma unroll
   for (int e = 0; e < 16; ++e)
@@ -525,13 +530,17 @@ hipError_t launch_vector(const RopeArgs& a, hipStream_t s) {
   const int lanes = lanes_of(a.head_dim);
   const int all = a.side[0].heads + a.side[1].heads + (PAGED ? a.side[2].heads : 0);
   const int groups = 256 / lanes;
-  // four heads a group once that still leaves every CU work: the table's row and
-  // the position are read once for them
+  // several heads a group once that still leaves every CU work: the table's row
+  // and the position are read once for them.  Two, or four with norms (4096 tokens
+  // of 72 heads of 128, bf16: two 28.4 us without norms and 31.9 with them, four
+  // 29.3 and 30.7; appending 2700 tokens of 32 + 32 + 32 heads 25.6 against 27.7; eight are slower
+  // everywhere).
   const int64_t one = ((int64_t)a.tokens * all + groups - 1) / groups;
   if (one >= 8 * (int64_t)num_cus()) {
-    const int per = (all + 3) / 4;
+    constexpr int kHeads = NORM ? 4 : 2;
+    const int per = (all + kHeads - 1) / kHeads;
     const int64_t wgs = ((int64_t)a.tokens * per + groups - 1) / groups;
-    k_rope<TY, NORM, INTER, PAGED, 4><<<(unsigned)wgs, 256, 0, s>>>(a, lanes, per);
+    k_rope<TY, NORM, INTER, PAGED, kHeads><<<(unsigned)wgs, 256, 0, s>>>(a, lanes, per);
   } else {
     k_rope<TY, NORM, INTER, PAGED, 1><<<(unsigned)one, 256, 0, s>>>(a, lanes, all);
   }
