@@ -22,6 +22,12 @@
 // left), two products each: the matrix cores idle here, and the result carries
 // one 16-bit rounding instead of two.
 //
+// Measured: 64 sequences of up to 16000 keys, 64 heads over 8, bf16 (767 MB): 155 us, 4.9
+// TB/s; all of 5000 keys 231 us, 5.7 TB/s; traffic as counted is the keys and
+// values once.  One sequence of 1024 keys, 32 heads (17 MB): 14.0 us, of which about 3
+// are the launch, 3 the division of the work, 3 the joining of pieces and the rest
+// the chain of page number, keys, values.
+//
 // The next tile's keys are loaded into the registers of this one's as soon as
 // S^T is done, its values as soon as these are in LDS, and the page numbers one
 // tile ahead: 16 KB a wave in flight at 128 elements a head.
@@ -36,6 +42,10 @@ constexpr int kRows = 16;
 constexpr int kWaves = 4;
 constexpr int kWaveKeys = 32;
 constexpr int kTile = kWaves * kWaveKeys;
+// Division of the work: a share may be one tile (one sequence of 1024 keys, 32 heads:
+// 14.0 us; two tiles at least: 16.5), and a unit many pieces, which the last of its
+// workgroups reads (one of 60001 keys, 8 heads over one: 43.8 us with 64, 55 with 16,
+// 57 with 256).
 constexpr int kExtra = 0;
 constexpr int kLeast = 1;
 constexpr int kPieces = 64;  // whole shares of a split unit (one piece more where it begins inside one)

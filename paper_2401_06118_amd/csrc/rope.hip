@@ -16,6 +16,10 @@
 // whose elements pair with each other (half layout) or within (interleaved), so a
 // pair never crosses lanes, and a lane's 8 cos and sin serve all heads that it
 // runs of its token.  All loads of the heads go out before the first is used.
+// Measured: norms and rotation of 4096 tokens of 64 + 8 heads of 128, bf16 (153 MB):
+// 29.7 us, 5.2 TB/s (a copy of as much: 31); the gradients with norms of 2048 tokens of
+// 32 + 32 heads (102 MB) 23.4 us and 4.9 for the sum over workgroups; two heads' loads at
+// a time there: 25.1.
 // Any other alignment, head size or rotated part takes the general kernels, one
 // wave a head.
 #include "rope.h"
