@@ -81,7 +81,7 @@ enum aqlm_status {
   AQLM_OK = 0,
   AQLM_ERR_NULL = 1,        /* a required pointer is NULL */
   AQLM_ERR_SHAPE = 2,       /* non-positive or too large size, or d_in % g != 0 */
-  AQLM_ERR_UNSUPPORTED = 3, /* (M, B, g) outside the supported set */
+  AQLM_ERR_UNSUPPORTED = 3, /* (M, B, g), a type or a head size outside the supported set */
   AQLM_ERR_ALIGN = 4,       /* a pointer breaks the alignment rule above */
   AQLM_ERR_HIP = 5,         /* the HIP runtime reported an error */
   AQLM_ERR_WORKSPACE = 6,   /* workspace smaller than the entry point's *_workspace_bytes */
