@@ -24,6 +24,7 @@ import torch
 
 from . import _check, _lib, _stream_handle
 
+_COUNTER_BYTES = 16384  # AQLM_ATTENTION_COUNTER_BYTES
 _lock = threading.Lock()
 _ext = None
 
@@ -162,7 +163,9 @@ def attention_workspace(head_dim: int, device="cuda") -> torch.Tensor:
     need = int(_lib.load().aqlm_paged_attention_workspace_bytes(int(head_dim)))
     if need <= 0:
         raise ValueError("head_dim must be a multiple of 8 up to 256")
-    return torch.zeros((need,), dtype=torch.uint8, device=device)
+    ws = torch.empty((need,), dtype=torch.uint8, device=device)
+    ws[:_COUNTER_BYTES].zero_()
+    return ws
 
 
 # Workspaces of calls that bring none, one per device, stream and padded head

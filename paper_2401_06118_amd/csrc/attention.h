@@ -198,6 +198,7 @@ __device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, AttnEntry* li
   if (marked != 0) {
     for (int i = 0; i < a.seqs; i += kWave) {
       uint64_t left = __ballot(i + lane < a.seqs && list[i + lane].before == -1);
+      __syncthreads();  // (every wave has read the marks before one is replaced)
       for (int n = 0; left != 0; ++n, left &= left - 1) {
         if (n % WAVES != wave) continue;
         const int b = i + __builtin_ctzll(left);
@@ -212,13 +213,11 @@ __device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, AttnEntry* li
         sum = wave_scan(sum);
         if (lane == kWave - 1) list[b].before = sum;
       }
-      // (the marks of these 64 sequences are read before any is replaced only if the
-      // waves stay together)
-      __syncthreads();
     }
   }
   most = wave_most(most);
   if (lane == 0) scratch[wave] = most;
+  if (marked != 0) __syncthreads();
   if (wave == 0) {  // costs to the costs before
     int before = 0;
     for (int b = 0; b < a.seqs; b += kWave) {

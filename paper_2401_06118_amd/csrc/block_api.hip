@@ -346,7 +346,7 @@ int aqlm_process_logits(const void* logits, int64_t logits_stride, void* out, in
   a.out_row = out_stride;
   a.rows = (int32_t)rows;
   a.vocab = (int32_t)vocab;
-  if (r->tokens) {
+  if (r->tokens && r->history > 0) {  // (without history there is nothing to penalise)
     a.tokens = r->tokens;
     a.token_lens = r->token_lens;
     a.prompt_lens = r->prompt_lens;
@@ -356,7 +356,7 @@ int aqlm_process_logits(const void* logits, int64_t logits_stride, void* out, in
     a.frequency = r->frequency;
     a.presence = r->presence;
   }
-  if (r->bias_ids) {
+  if (r->bias_ids && r->biases > 0) {
     a.bias_ids = r->bias_ids;
     a.bias_values = r->bias_values;
     a.bias_row = r->bias_stride;

@@ -398,6 +398,16 @@ def test_attention_split(aq, lens, new, heads, kv):
     assert all(torch.equal(o[0], outs[0][0]) and torch.equal(o[1], outs[0][1]) for o in outs)
 
 
+@pytest.mark.parametrize("count,most", [(70, 90), (150, 40), (9, 200)])
+def test_attention_many_sequences(aq, count, most):
+    """Sequences of one unit and of several, in any order, more than a wave has lanes."""
+    new = [1 + (37 * i) % most for i in range(count)]
+    lens = [n + (53 * i) % 130 for i, n in enumerate(new)]
+    bt, q = attend_case(lens, new, 4, 1, 64, 16, torch.float16)
+    outs = [check_attention(aq, bt, q, True, 0, max_new=most)[0] for _ in range(2)]
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
 @pytest.mark.parametrize("stale", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("new", [[1, 1, 1], [3, 2, 1], [60, 40, 77]])
 def test_attention_stale_slots(aq, stale, new):
@@ -570,6 +580,20 @@ def test_process_logits_parts(aq):
     assert torch.equal(got.double(), want)
     empty = torch.zeros(3, 0, dtype=torch.int32, device=DEV)
     assert torch.equal(aq.process_logits(d(x), tokens=empty, token_lens=d(lens * 0), repetition=d(r)).cpu(), x)
+
+
+def test_process_logits_without_history(aq):
+    """Token lists of no entries through the C ABI: nothing is read from them."""
+    import ctypes
+
+    x = rand(1, 2, 100, dtype=torch.float32).to(DEV)
+    ints, ones = torch.zeros(2, dtype=torch.int32, device=DEV), torch.full((2,), 3.0, device=DEV)
+    out = torch.empty_like(x)
+    rules = aq._lib.LogitRules(tokens=ints.data_ptr(), token_lens=ints.data_ptr(), history=0,
+                               repetition=ones.data_ptr(), bias_ids=ints.data_ptr(), bias_values=ones.data_ptr())
+    st = aq._lib.load().aqlm_process_logits(x.data_ptr(), 100, out.data_ptr(), 100, 2, 2, 100, ctypes.byref(rules),
+                                            torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and torch.equal(out, x)
 
 
 def test_process_logits_special_values(aq):
