@@ -499,7 +499,9 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
             const float mn = fmaxf(r.m, pm);
             const float base = mn == -INFINITY ? 0.f : mn;
             const float wa = rescale(r.m - base), wb = rescale(pm - base);
-            const bool some = pm != -INFINITY;  // (a piece without keys of this row: nothing, whatever it holds)
+            // (a piece without keys of this row: nothing, whatever it holds; NaN scores leave
+            // the maximum where it was, but not the denominator)
+            const bool some = pm != -INFINITY || pl != 0.f;
             r.m = mn;
             r.l = r.l * wa + (some ? wb * pl : 0.f);
 #pragma unroll

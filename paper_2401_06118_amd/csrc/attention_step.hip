@@ -326,10 +326,12 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
       const float bm = mm[t] == -INFINITY ? 0.f : mm[t];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float mw = join_m[w * kRows + row];
-        if (mw == -INFINITY) continue;  // (a wave without keys of this row)
+        // (a wave without keys of this row; NaN scores leave the maximum where it was,
+        // but not the denominator)
+        const float mw = join_m[w * kRows + row], lw = join_m[(kWaves + w) * kRows + row];
+        if (mw == -INFINITY && lw == 0.f) continue;
         const float e = rescale(mw - bm);
-        ll[t] += e * join_m[(kWaves + w) * kRows + row];
+        ll[t] += e * lw;
         o[t] += e * *(const f4_t*)(join + (w * kRows + row) * StepLds<D>::kPitch + d);
       }
     }
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
                 x[p] = own;
                 ml[p] = f2_t{own_m, own_l};
               }
-              if (p0 + p >= n || ml[p][0] == -INFINITY) continue;  // (no keys of this row)
+              if (p0 + p >= n || (ml[p][0] == -INFINITY && ml[p][1] == 0.f)) continue;  // (no keys of this row)
               const float mn = fmaxf(mm[t], ml[p][0]);
               const float wa = rescale(mm[t] - mn), wb = rescale(ml[p][0] - mn);
               mm[t] = mn;

@@ -1,0 +1,51 @@
+"""NaN and infinities through the operators of ``block.py``, against their definitions in 64 bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import block_reference as ref  # noqa: E402
+from test_gpu_block import DEV, attend_case, aq, check_attention, rand  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+
+def both_kernels(aq, bt, q, causal=True, window=0, scale=None):
+    """A hint of one new token takes the kernel of a few rows, none the one of many (more than 16 rows)."""
+    for most in (1, 0):
+        check_attention(aq, bt, q, causal, window, scale=scale, max_new=most)
+
+
+NAN_QUERIES = [([1], [1]), ([40], [1]), ([300, 90], [1, 1]), ([20000], [1]), ([300, 90], [30, 8]), ([6000], [40])]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("lens,new", NAN_QUERIES)
+def test_nan_query(aq, lens, new, dtype):
+    """Rows whose query holds a NaN are NaN, their lse too, however the keys are divided; the others are theirs."""
+    bt, q = attend_case(lens, new, 4, 2, 128, 16, dtype)
+    q[0, 1, 5] = math.nan
+    q[-1, 2] = math.nan
+    both_kernels(aq, bt, q)
+
+
+NAN_KEYS = [
+    # lens, new, first and last NaN key, window
+    ([64], [1], 0, 64, 0),             # all keys
+    ([300], [1], 32, 64, 0),           # all of a wave's
+    ([20000, 50], [1, 1], 4000, 9000, 0),
+    ([6000], [40], 1000, 3000, 0),
+    ([6000], [40], 0, 6000, 0),
+    ([300], [40], 250, 262, 50),       # seen by some rows
+    ([300], [40], 290, 300, 0),
+]
+
+
+@pytest.mark.parametrize("lens,new,begin,end,window", NAN_KEYS)
+def test_nan_keys(aq, lens, new, begin, end, window):
+    """A run of NaN keys makes the rows that see one of them NaN, and no others."""
+    bt, q = attend_case(lens, new, 4, 2, 64, 16, torch.bfloat16)
+    for j in range(begin, end):
+        bt.k[int(bt.table[0, j // 16]), j % 16] = math.nan
+    both_kernels(aq, bt, q, window=window)
