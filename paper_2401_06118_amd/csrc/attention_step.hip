@@ -58,7 +58,7 @@ struct StepLds {
   static constexpr int kStage = kWaves * kWaveKeys * D * 2;
   static constexpr int kJoin = kWaves * kRows * (kPitch + 2) * 4;
   static constexpr int kUnion = kStage > kJoin ? kStage : kJoin;
-  static constexpr int kFixed = kUnion + 64;  // + scratch: waves' maxima, the "last" flag
+  static constexpr int kFixed = kUnion + 64;  // + scratch: waves' maxima, the "last" flag, waves' sums that are not finite
 };
 
 template <int D>
@@ -121,9 +121,13 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
 
   const AttnShare h = attn_share<kRows, kTile, kExtra, kWaves>(a, list, scratch, wg, grid, kPieces, kLeast);
 
+  // A weight's second part is 0 or below for some keys, and a weight may be 0 in 16
+  // bits: times an infinite value either gives a NaN that the definition has not.
+  // Tiles that all rows see are not searched for such values, whose sums tell of
+  // them: a unit (or piece) with one that is not finite is run again, with care.
+  bool care = false;
   for (int64_t at = h.begin; at < h.end;) {
     const AttnUnit u = attn_find<kRows, kTile, kExtra>(a, h, list, at);
-    at = min(u.stop, h.end);
     const int rows = min(kRows, u.s.count * a.group - u.t * kRows);
     const uint32_t rr = (uint32_t)(u.t * kRows + min(r16, rows - 1));
     const int token = attn_token(a, (int)rr);
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
         for (int d = 0; d < ND; ++d) acc[d] *= alpha;
 
         bool special = false;
-        if (!full) {
+        if (!full || care) {
           // values of keys outside the unit's range count as zeros
           uint32_t odd = 0;
 #pragma unroll
@@ -246,7 +250,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
             if (key < u.k0 || key >= u.k1) vt[i] = u32x4_t{0, 0, 0, 0};
             odd |= non_finite_any<BF>(vt[i]);
           }
-          if (lo_max <= u.k0 && hi_min >= u.k1) odd = 0;  // all rows see the same keys
+          if (!care && lo_max <= u.k0 && hi_min >= u.k1) odd = 0;  // all rows see the same keys
           special = __ballot(odd != 0) != 0;
         }
 #pragma unroll
@@ -286,6 +290,12 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
     l += __shfl_xor(l, 32);
 
     // join the waves
+    float z = 0.f;  // NaN if a sum is not finite
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z = fmaf(acc[d][i], 0.f, z);
+    const bool bad = __ballot(z != z) != 0;
     __syncthreads();
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -294,7 +304,15 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
       join_m[wave * kRows + r16] = m;
       join_m[(kWaves + wave) * kRows + r16] = l;
     }
+    if (lane == 0) scratch[12 + wave] = bad;
     __syncthreads();
+    int again = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) again |= scratch[12 + w];
+    if (__builtin_expect(!care && again != 0, 0)) {
+      care = true;
+      continue;
+    }
     auto write = [&](int row, int d, f4_t o, float mm, float ll) {
       const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
       const uint32_t ur = (uint32_t)(u.t * kRows + row);
@@ -396,6 +414,8 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
       }
     }
     __syncthreads();
+    care = false;
+    at = min(u.stop, h.end);
   }
 }
 

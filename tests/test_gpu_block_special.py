@@ -49,3 +49,25 @@ def test_nan_keys(aq, lens, new, begin, end, window):
     for j in range(begin, end):
         bt.k[int(bt.table[0, j // 16]), j % 16] = math.nan
     both_kernels(aq, bt, q, window=window)
+
+
+INF_VALUES = [([1], [1]), ([40], [1]), ([300, 90], [1, 1]), ([20000], [1]), ([300, 90], [30, 8]), ([6000], [40])]
+
+
+def put_infinities(bt):
+    """Of the first sequence's first kv head: +inf, -inf and both in columns of their own."""
+    n = bt.lens[0]
+    for j, d, v in ((5, 3, math.inf), (7, 3, math.inf), (9, 8, -math.inf), (11, 20, math.inf), (2 * n // 3, 20, -math.inf),
+                    (n - 2, 40, -math.inf)):
+        j = min(max(j, 0), n - 1)
+        bt.v[int(bt.table[0, j // 16]), j % 16, 0, d] = v
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,new", INF_VALUES)
+def test_infinite_values(aq, lens, new, causal, dtype):
+    """Infinite values of keys that all rows see: an infinite element, NaN where both signs meet."""
+    bt, q = attend_case(lens, new, 4, 2, 64, 16, dtype)
+    put_infinities(bt)
+    both_kernels(aq, bt, q, causal=causal)
