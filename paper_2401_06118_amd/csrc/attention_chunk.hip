@@ -393,9 +393,13 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
   int parity = 0, turn = 0;
   ChunkLoad<D, EXACT> ld;
   ld.set(a, wave, lane);
+  // A weight that is 0 in 16 bits, times an infinite value, is a NaN that the
+  // definition has not.  Tiles that all rows see are not searched for such values,
+  // whose sums tell of them: a unit (or piece) with a NaN among them is run again,
+  // with care.
+  bool care = false;
   for (int64_t at = h.begin; at < h.end;) {
     const AttnUnit u = attn_find<kRows, kTile, kExtra>(a, h, list, at);
-    at = min(u.stop, h.end);
     const int rows = min(kRows, u.s.count * a.group - u.t * kRows);
     const int left = rows - wave * kWaveRows;  // rows of this wave
     const bool active = left > 0;
@@ -412,6 +416,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
     int unit_lo, unit_hi, x;  // keys that all of the unit's rows see
     attn_visible(a, u.s, attn_token(a, u.t * kRows), x, unit_hi);
     attn_visible(a, u.s, attn_token(a, u.t * kRows + rows - 1), unit_lo, x);
+    if (care) unit_lo = INT_MAX;  // search every tile
     r.m = -INFINITY;
     r.l = 0.f;
 #pragma unroll
@@ -440,6 +445,25 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
         chunk_tile<BF, D, EXACT>(a, u, stage0 + parity * kStageBytes, stage0 + (parity ^ 1) * kStageBytes, ld, base,
                                  base + kTile < end, page, active, unit_lo, unit_hi, scratch + 9, ++turn, r);
         parity ^= 1;
+      }
+      float z0 = 0.f, z1 = 0.f;  // NaN if a sum is (or if one is infinite: run again in vain)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          z0 = fmaf(r.acc[d][i], r.acc[d][i + 1], z0);
+          z1 = fmaf(r.acc[d][i + 2], r.acc[d][i + 3], z1);
+        }
+      const float z = z0 + z1;
+      const bool bad = __ballot(z != z) != 0;
+      if (lane == 0) scratch[12 + wave] = bad;
+      lds_barrier();
+      int again = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) again |= scratch[12 + w];
+      if (__builtin_expect(!care && again != 0, 0)) {
+        care = true;
+        continue;
       }
     }
     r.l = both_halves_sum(r.l);
@@ -539,6 +563,8 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
         a.lse[(int64_t)(u.s.first + token) * (a.kv_heads * a.group) + head] =
             r.l == 0.f ? -INFINITY : (r.m - kShift + log2f(r.l)) * 0.69314718055994531f;
     }
+    care = false;
+    at = min(u.stop, h.end);
   }
 }
 

@@ -71,3 +71,15 @@ def test_infinite_values(aq, lens, new, causal, dtype):
     bt, q = attend_case(lens, new, 4, 2, 64, 16, dtype)
     put_infinities(bt)
     both_kernels(aq, bt, q, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim", [64, 128, 200, 256])
+@pytest.mark.parametrize("lens,new", [([300], [1]), ([300, 90], [30, 8]), ([2000], [40])])
+def test_infinite_values_of_small_weight(aq, lens, new, dim, dtype):
+    """However small a weight is, times an infinite value it is infinite."""
+    bt, q = attend_case(lens, new, 4, 2, dim, 16, dtype)
+    for i in range(40):
+        j = i * (lens[0] - new[0] - 1) // 40
+        bt.v[int(bt.table[0, j // 16]), j % 16, i % 2, i] = math.inf if i % 3 else -math.inf
+    both_kernels(aq, bt, q, scale=0.75 * (64 / dim) ** 0.5)
