@@ -155,15 +155,19 @@ __device__ __forceinline__ bool load_turn(const RopeArgs& a, int pos, const Piec
   return true;
 }
 
+// Pairs past the rotated part stay as they are (a turn by cos 1, sin 0 would carry an
+// infinite or NaN element to its neighbour).
 template <bool INTER>
-__device__ __forceinline__ void turn(float (&y)[16], const float (&c)[8], const float (&s)[8], bool rotates) {
-  if (!rotates) return;
+__device__ __forceinline__ void turn(const RopeArgs& a, int lane, const Pieces& p, float (&y)[16], const float (&c)[8],
+                                     const float (&s)[8]) {
+  if (!INTER && lane >= a.rot / 16) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
+    const bool rotates = !INTER || p.pair[i / 4] + i % 4 < a.rot / 2;
     const float ya = y[ia], yb = y[ib];
-    y[ia] = ya * c[i] - yb * s[i];
-    y[ib] = yb * c[i] + ya * s[i];
+    y[ia] = rotates ? ya * c[i] - yb * s[i] : ya;
+    y[ib] = rotates ? yb * c[i] + ya * s[i] : yb;
   }
 }
 
@@ -216,7 +220,6 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int lanes, int per_tok
   if (PAGED) page = paged_page(a, seq, pos);
   float c[8], s[8];
   const bool inside = load_turn(a, pos, p, c, s);
-  const bool rotates = INTER ? true : i < a.rot / 16;
 
 #pragma unroll
   for (int j = 0; j < HPT; ++j) {
@@ -240,7 +243,7 @@ __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int lanes, int per_tok
       }
     }
     if (w != 2) {
-      turn<INTER>(y, c, s, rotates);
+      turn<INTER>(a, i, p, y, c, s);
       if (!inside)
 #pragma unroll
         for (int e = 0; e < 16; ++e) y[e] = __builtin_nanf("");
@@ -274,7 +277,6 @@ __global__ void __launch_bounds__(256) k_rope_grad(RopeArgs a, int lanes) {
   const int block = (int)blockIdx.x - (w ? a.blocks[0] : 0), blocks = a.blocks[w];
   const RopeSide& sd = a.side[w];
   const Pieces p = pieces_of<INTER>(a, i, lanes);
-  const bool rotates = INTER ? true : i < a.rot / 16;
   float wt[16], dw[16];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(256) k_rope_grad(RopeArgs a, int lanes) {
       g[e] = inside ? (float)gv[e / 8][e % 8] : __builtin_nanf("");
       x[e] = (float)xv[e / 8][e % 8];
     }
-    turn<INTER>(g, c, s, rotates);
+    turn<INTER>(a, i, p, g, c, s);
     float ss = 0.f, dot = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {

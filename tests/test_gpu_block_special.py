@@ -83,3 +83,44 @@ def test_infinite_values_of_small_weight(aq, lens, new, dim, dtype):
         j = i * (lens[0] - new[0] - 1) // 40
         bt.v[int(bt.table[0, j // 16]), j % 16, i % 2, i] = math.inf if i % 3 else -math.inf
     both_kernels(aq, bt, q, scale=0.75 * (64 / dim) ** 0.5)
+
+
+UNROTATED = [(64, 32), (64, 4), (64, 6), (128, 64), (80, 40), (256, 252)]
+
+
+def put_outside(x, rot, dim):
+    """Infinities and NaN in the part that is not rotated, each beside a number of its pair."""
+    for t, d, v in ((0, rot, math.inf), (1, dim - 1, -math.inf), (2, rot + 2, math.nan), (3, rot + 1, math.inf)):
+        x[t, t % x.shape[1], d] = v
+
+
+def same_bits(got, want):
+    kind = torch.int32 if want.dtype == torch.float32 else torch.int16
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), nan)
+    assert torch.equal(got.contiguous().view(kind)[~nan], want.contiguous().view(kind)[~nan])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim,rot", UNROTATED)
+def test_interleaved_rotation_leaves_the_rest(aq, dim, rot, dtype):
+    """Elements past the rotated part come back as they are, and reach no others: forward, gradient and cache."""
+    a = rand(5, 4, 4, dim, dtype=dtype)
+    put_outside(a, rot, dim)
+    t = ref.table64(50, rot).float()
+    pos = torch.tensor([0, 3, 49, 7], dtype=torch.int32)
+    d, dt = a.to(DEV), t.to(DEV)
+    q, k = aq.rope(d[:, :2], d[:, 2:], dt, pos.to(DEV), interleaved=True)
+    g = aq.rope_backward(d[:, :2], d[:, 2:], dt, pos.to(DEV), interleaved=True)
+    for got in (torch.cat([q, k], 1), torch.cat(g[:2], 1)):
+        same_bits(got.cpu()[..., rot:], a[..., rot:])
+        assert torch.isfinite(got[..., :rot]).all()
+    kc, vc = (torch.zeros(2, 16, 2, dim, dtype=dtype, device=DEV) for _ in range(2))
+    where = (kc, vc, *(torch.tensor(v, dtype=torch.int32, device=DEV) for v in ([[1]], [4], [0, 4])))
+    for table in (dt, None):
+        first = rot if table is not None else 0
+        q = aq.paged_append(d[:, :2], d[:, 2:], d[:, 2:], *where, table=table, interleaved=True)
+        same_bits(q.cpu()[..., first:], a[:, :2, first:])
+        same_bits(kc[1, :4].cpu()[..., first:], a[:, 2:, first:])
+        same_bits(vc[1, :4].cpu(), a[:, 2:])
+        assert torch.isfinite(q[..., :first]).all() and torch.isfinite(kc[1, :4, :, :first]).all()
