@@ -551,7 +551,9 @@ int aqlm_rope_backward(const aqlm_heads* dq, const aqlm_heads* dk, const aqlm_he
  * sequence's keys WITH its new tokens, which are the tokens cu_new[b] ..
  * cu_new[b + 1] of the activations (cu_new[0] = 0, cu_new[seqs] = tokens) and its
  * last positions; a sequence may have no new tokens, and one without keys
- * (kv_lens 0) is an idle slot of a batch of fixed size.  Strides in elements. */
+ * (kv_lens 0) is an idle slot of a batch of fixed size.  Strides in elements.
+ * (cu_new ascends.  Where it falls all the same, attention takes a token as that of
+ * the first sequence that claims it, append as that of any or none.) */
 typedef struct aqlm_paged_cache {
   void* k;
   void* v;

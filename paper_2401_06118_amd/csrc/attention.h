@@ -28,6 +28,7 @@
 
 #include <limits.h>
 
+#include "attention_rows.h"
 #include "common.h"
 
 namespace aqlm {
@@ -73,18 +74,11 @@ __device__ __forceinline__ u32x4_t attn_query(const AttnArgs& a, const u32x4_t& 
   return r;
 }
 
-// A sequence's new tokens and keys, whatever the device arrays hold: no read
-// goes past the arrays.
-struct AttnSeq {
-  int first, count, keys;
-};
-__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int b) {
-  AttnSeq s;
-  s.first = min(max(a.cu_new[b], 0), a.tokens);
-  s.count = min(max(a.cu_new[b + 1], s.first), a.tokens) - s.first;
-  const int64_t room = (int64_t)a.table_width << a.page_shift;
-  s.keys = (int)min((int64_t)max(a.kv_lens[b], 0), room);
-  return s;
+// Sequence b by itself; `falls` is set where its offsets do.
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int b, bool& falls) {
+  const int cu0 = a.cu_new[b], cu1 = a.cu_new[b + 1];
+  falls |= cu1 < cu0;
+  return attn_cut(cu0, cu1, a.kv_lens[b], a.tokens, (int64_t)a.table_width << a.page_shift);
 }
 
 // The token of a sequence's row (rows are below 2^31).
@@ -116,7 +110,7 @@ __device__ __forceinline__ int attn_units(const AttnArgs& a, const AttnSeq& s, i
   return (int)(((int64_t)s.count * a.group + R - 1) / R);
 }
 
-// Inclusive prefix sum over the wave, and its maximum of values above 0, by moves
+// Inclusive prefix sums over the wave, and maxima of values of 0 and more, by moves
 // between lanes (shuffles go through the LDS).
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int dpp_or_0(int v) {
@@ -131,20 +125,41 @@ __device__ __forceinline__ int wave_scan(int v) {
   v += dpp_or_0<0x143, 0xC>(v);
   return v;
 }
-__device__ __forceinline__ int wave_most(int v) {
+__device__ __forceinline__ int wave_scan_most(int v) {
   v = max(v, dpp_or_0<0x111, 0xF>(v));
   v = max(v, dpp_or_0<0x112, 0xF>(v));
   v = max(v, dpp_or_0<0x114, 0xF>(v));
   v = max(v, dpp_or_0<0x118, 0xF>(v));
   v = max(v, dpp_or_0<0x142, 0xA>(v));
   v = max(v, dpp_or_0<0x143, 0xC>(v));
-  return __builtin_amdgcn_readlane(v, 63);
+  return v;
 }
+__device__ __forceinline__ int wave_most(int v) { return __builtin_amdgcn_readlane(wave_scan_most(v), kWave - 1); }
 
-// A sequence in LDS: the cost of one kv head before it, and what attn_seq says.
+// A sequence in LDS: the cost of one kv head before it, and what it holds.
 struct __align__(16) AttnEntry {
   int before, first, count, keys;
 };
+
+// Entries whose offsets fall somewhere: each keeps what those before it leave
+// (attn_after).  One wave runs it.
+__device__ __forceinline__ void attn_apart(const AttnArgs& a, AttnEntry* list) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int end = 0;
+  for (int b = 0; b < a.seqs; b += kWave) {
+    const int i = b + lane;
+    AttnSeq s = {0, 0, 0};
+    if (i < a.seqs) s = {list[i].first, list[i].count, list[i].keys};
+    const int ends = wave_scan_most(s.first + s.count);
+    const int others = __shfl_up(ends, 1);
+    s = attn_after(s, lane > 0 ? max(end, others) : end);
+    if (i < a.seqs) {
+      list[i].first = s.first;
+      list[i].count = s.count;
+    }
+    end = max(end, __builtin_amdgcn_readlane(ends, kWave - 1));
+  }
+}
 
 struct AttnShare {
   int per_head;    // cost of one kv head over all sequences
@@ -179,22 +194,36 @@ __device__ __forceinline__ AttnShare attn_share(const AttnArgs& a, AttnEntry* li
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   int most = 1, tile0, k0, k1;
   // a thread per sequence; those of several units are left to a wave each
-  bool many = false;
-  for (int b = tid; b < a.seqs; b += WAVES * kWave) {
-    const AttnSeq s = attn_seq(a, b);
+  bool many = false, falls = false;
+  auto enter = [&](int b, const AttnSeq& s) {
     const int units = attn_units(a, s, R);
     int cost = 0;
     if (units == 1) cost = attn_tiles<R, KT>(a, s, 0, tile0, k0, k1) + EXTRA;
     most = max(most, cost);
     many |= units > 1;
     list[b] = AttnEntry{units > 1 ? -1 : cost, s.first, s.count, s.keys};
-  }
-  const bool any = __ballot(many) != 0;
-  if (lane == 0) scratch[WAVES + wave] = any;
-  __syncthreads();
-  int marked = 0;
+  };
+  // what any thread found: 1 sequences of several units, 2 offsets that fall
+  auto found = [&]() {
+    const int mine = (__ballot(many) != 0 ? 1 : 0) | (__ballot(falls) != 0 ? 2 : 0);
+    if (lane == 0) scratch[WAVES + wave] = mine;
+    __syncthreads();
+    int all = 0;
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) marked |= scratch[WAVES + w];
+    for (int w = 0; w < WAVES; ++w) all |= scratch[WAVES + w];
+    return all;
+  };
+  for (int b = tid; b < a.seqs; b += WAVES * kWave) enter(b, attn_seq(a, b, falls));
+  int marked = found();
+  if (__builtin_expect((marked & 2) != 0, 0)) {
+    if (wave == 0) attn_apart(a, list);
+    __syncthreads();
+    most = 1;
+    many = falls = false;
+    for (int b = tid; b < a.seqs; b += WAVES * kWave)
+      enter(b, AttnSeq{list[b].first, list[b].count, list[b].keys});
+    marked = found();
+  }
   if (marked != 0) {
     for (int i = 0; i < a.seqs; i += kWave) {
       uint64_t left = __ballot(i + lane < a.seqs && list[i + lane].before == -1);
