@@ -588,9 +588,9 @@ int aqlm_paged_append(const aqlm_heads* q, const aqlm_heads* k, const aqlm_heads
  * token's sequence, query head e reading kv head e / (heads / kv_heads).  causal:
  * keys up to the token's own position only; window > 0: only the last `window`
  * positions up to the token's own (those after it, without causal, are not
- * limited).  A row without keys gives zeros.  Keys that a row does not see
+ * limited).  A row without keys, or of a token that no sequence holds, gives zeros.  Keys that a row does not see
  * take no part in it, whatever they hold.  lse (NULL or fp32 [tokens][heads]): the
- * logarithm of the softmax's denominator, -inf for a row without keys.
+ * logarithm of the softmax's denominator, -inf where the row is zeros for want of keys.
  *   max_new: the most new tokens of a sequence, if known (0: unknown); it
  *   chooses the kernel, not the result: up to 16 rows (new tokens x heads per kv
  *   head) of a sequence are bound by the cache's bytes, more by the products.

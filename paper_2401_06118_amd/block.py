@@ -198,7 +198,7 @@ def paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, *, scale=
     of each row's softmax denominator (fp32 [tokens, heads]).  Query head e reads kv
     head e // (heads / kv heads).  ``scale``: 1 / sqrt(head_dim) if not given.
     ``causal``: a token sees keys up to its own position; ``window`` above 0: only that
-    many positions up to its own.  A row that sees no key is 0, its lse -inf.
+    many positions up to its own.  A row that sees no key, or whose token no sequence holds, is 0, its lse -inf.
     ``max_new``: the most new tokens of a sequence, if known (it chooses the kernel,
     not the result).  ``workspace``: as :func:`attention_workspace` makes it;
     without one, one per stream is kept."""

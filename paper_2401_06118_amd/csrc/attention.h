@@ -381,6 +381,23 @@ __device__ __forceinline__ AttnUnit attn_find(const AttnArgs& a, const AttnShare
   return u;
 }
 
+// Rows of tokens that no sequence holds (the sequences' tokens are one run): zeros, as
+// rows without keys.
+template <int THREADS>
+__device__ __forceinline__ void attn_unheld(const AttnArgs& a, const AttnEntry* list, int wg, int grid) {
+  const int begin = list[0].first, end = list[a.seqs - 1].first + list[a.seqs - 1].count;
+  if (end - begin == a.tokens) return;
+  const int heads = a.kv_heads * a.group, pieces = a.head_dim / 8;
+  const int64_t rows = (int64_t)(a.tokens - (end - begin)) * heads;
+  for (int64_t i = (int64_t)wg * THREADS + threadIdx.x; i < rows * pieces; i += (int64_t)grid * THREADS) {
+    const int64_t row = i / pieces;
+    const int t = (int)(row / heads), head = (int)(row - (int64_t)t * heads), piece = (int)(i - row * pieces);
+    const int token = t < begin ? t : t + (end - begin);
+    *(u32x4_t*)(a.out + token * a.out_token + head * a.out_head + piece * 8) = u32x4_t{0, 0, 0, 0};
+    if (piece == 0 && a.lse) a.lse[(int64_t)token * heads + head] = -INFINITY;
+  }
+}
+
 // The page of key j of sequence b, kept inside the cache.
 __device__ __forceinline__ int attn_page(const AttnArgs& a, int b, int j) {
   const int p = a.block_table[b * a.table_stride + (j >> a.page_shift)];

@@ -566,6 +566,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_c
     care = false;
     at = min(u.stop, h.end);
   }
+  attn_unheld<kWaves * kWave>(a, list, wg, grid);
 }
 
 template <bool BF, int D, bool EXACT>

@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(kWaves* kWave, D == 256 ? 1 : 2) k_attention_s
     care = false;
     at = min(u.stop, h.end);
   }
+  attn_unheld<kWaves * kWave>(a, list, wg, grid);
 }
 
 template <bool BF, int D, bool EXACT>

@@ -65,3 +65,50 @@ def test_attention_falling_offsets(aq, cu, lens, tokens):
         within(got[held.to(DEV)], want[held], bound[held], "out")
         within(got_lse[held.to(DEV)], lse[held],
                (2.0 ** -19 * (score[..., 0] + lse.abs().nan_to_num(0.0, 0.0, 0.0) + 2))[held], "lse")
+
+
+UNHELD = [
+    ([0, 3, 5], [40, 90], 9),              # a padded batch: tokens behind the last sequence's
+    ([2, 6, 8], [40, 90], 10),             # and before the first one's
+    ([0, 0], [50], 4),                     # none held
+    ([9, 9, 9], [50, 20], 20),
+    ([0, 60, 100], [300, 90], 131),
+    ([5, 1, -7], [50, 20], 12),
+]
+
+
+@pytest.mark.parametrize("cu,lens,tokens,dim", [(*c, 64) for c in UNHELD + FALLING] + [(*c, 200) for c in UNHELD])
+def test_attention_tokens_of_no_sequence(aq, cu, lens, tokens, dim):
+    """Rows that no sequence holds are zeros, their lse -inf, whatever was there before."""
+    # (freed memory that new outputs may come from holds NaN)
+    junk = [torch.full((tokens, 4, dim), float("nan"), dtype=torch.float16, device=DEV) for _ in range(4)]
+    del junk
+    gots, want, bound, lse, score, held = call_with(aq, cu, lens, tokens, dim=dim)
+    tol = 2.0 ** -19 * (score[..., 0] + lse.abs().nan_to_num(0.0, 0.0, 0.0) + 2)
+    for got, got_lse in gots:
+        assert (got[~held.to(DEV)] == 0).all() and (got_lse[~held.to(DEV)] == -float("inf")).all()
+        within(got, want, bound, "out")
+        within(got_lse, lse, tol, "lse")
+
+
+def test_padded_batch_in_a_graph(aq):
+    """One captured call for up to 6 tokens serves fewer: the others' rows are zeros in every replay."""
+    bt = Batch([40, 90, 33], [1, 1, 4], 2, 64, 16, torch.float16)
+    q = rand(2, 6, 4, 64).to(DEV)
+    k, v, table, lens, cu = bt.gpu()
+    out = torch.empty(6, 4, 64, dtype=torch.float16, device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        aq.paged_attention(q, k, v, table, lens, cu, out=out)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        aq.paged_attention(q, k, v, table, lens, cu, out=out)
+    for ends in ((1, 2, 6), (1, 2, 3), (0, 0, 0), (2, 2, 5)):
+        cu.copy_(torch.tensor((0,) + ends, dtype=torch.int32))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out[ends[-1]:] == 0).all() and torch.isfinite(out).all()
+        assert torch.equal(out, aq.paged_attention(q, k, v, table, lens, cu))
