@@ -173,20 +173,25 @@ def attention_workspace(head_dim: int, device="cuda") -> torch.Tensor:
 _workspaces = {}
 
 
-def _workspace(device, head_dim, stream_handle):
+def _workspace(device, head_dim, stream, handle):
     if head_dim % 8 or not 0 < head_dim <= 256 or device.type != "cuda":
         raise ValueError("paged_attention takes GPU tensors and a head_dim that is a multiple of 8 up to 256")
-    if torch.cuda.is_current_stream_capturing():
+    if (_ext or _binding()).capturing(handle):
         # a graph's launches may run beside this stream's later ones: it gets its own
-        return attention_workspace(head_dim, device)
-    key = (device, stream_handle, 64 if head_dim <= 64 else 128 if head_dim <= 128 else 256)
+        return _workspace_on(stream, device, head_dim)
+    key = (device, handle, 64 if head_dim <= 64 else 128 if head_dim <= 128 else 256)
     ws = _workspaces.get(key)
     if ws is None:
-        ws = attention_workspace(key[2], device)
-        if stream_handle != _stream_handle(None):
-            torch.cuda.current_stream(device).synchronize()  # (zeroed on the current stream, used on another)
-        _workspaces[key] = ws
+        ws = _workspaces[key] = _workspace_on(stream, device, key[2])
     return ws
+
+
+def _workspace_on(stream, device, head_dim):
+    """Made and zeroed on the stream that launches: in its order, its graph and its memory."""
+    if stream is None:
+        return attention_workspace(head_dim, device)
+    with torch.cuda.stream(stream):
+        return attention_workspace(head_dim, device)
 
 
 def paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, *, scale=None, causal: bool = True,
@@ -204,7 +209,7 @@ def paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, *, scale=
     without one, one per stream is kept."""
     handle = _stream_handle(stream)
     if workspace is None:
-        workspace = _workspace(q.device, q.shape[-1], handle)
+        workspace = _workspace(q.device, q.shape[-1], stream, handle)
     r = (_ext or _binding()).paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, scale, causal, window,
                                              max_new, return_lse, out, workspace, handle)
     if stream is not None:

@@ -6,6 +6,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <hip/hip_runtime_api.h>
 
 #include <stdexcept>
 #include <string>
@@ -348,6 +349,14 @@ PyObject* process_logits(PyObject* const* a) {
   return wrap(out);
 }
 
+// Whether a stream (its handle) is recording a graph.
+PyObject* capturing(PyObject* const* a) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing((hipStream_t)stream_of(a[0]), &status);
+  if (e != hipSuccess) throw std::runtime_error(std::string("hipStreamIsCapturing: ") + hipGetErrorString(e));
+  return PyBool_FromLong(status != hipStreamCaptureStatusNone);
+}
+
 PyObject* set_check(PyObject* const* a) {
   Py_INCREF(a[0]);
   Py_XDECREF(g_check);
@@ -358,7 +367,8 @@ PyObject* set_check(PyObject* const* a) {
 #define AQLM_ENTRY(F, N) \
   { #F, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {AQLM_ENTRY(rope, 11),           AQLM_ENTRY(rope_backward, 13),   AQLM_ENTRY(paged_append, 15),
-                         AQLM_ENTRY(paged_attention, 14), AQLM_ENTRY(process_logits, 12), AQLM_ENTRY(set_check, 1),
+                         AQLM_ENTRY(paged_attention, 14), AQLM_ENTRY(process_logits, 12), AQLM_ENTRY(capturing, 1),
+                         AQLM_ENTRY(set_check, 1),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
