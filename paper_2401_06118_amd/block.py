@@ -159,7 +159,8 @@ def paged_append(q, k, v, k_cache, v_cache, block_table, kv_lens, cu_new, *, tab
 
 def attention_workspace(head_dim: int, device="cuda") -> torch.Tensor:
     """A workspace for :func:`paged_attention` with heads of up to ``head_dim``
-    elements, ready for use.  One serves any calls on one stream, one after another."""
+    elements, ready for use (heads of up to 64, 128 and 256 elements: 35, 68 and 68 MB).  One
+    serves any calls on one stream, one after another."""
     need = int(_lib.load().aqlm_paged_attention_workspace_bytes(int(head_dim)))
     if need <= 0:
         raise ValueError("head_dim must be a multiple of 8 up to 256")
@@ -169,8 +170,10 @@ def attention_workspace(head_dim: int, device="cuda") -> torch.Tensor:
 
 
 # Workspaces of calls that bring none, one per device, stream and padded head
-# size: calls on one stream run one after another.
+# size: calls on one stream run one after another.  Kept for good, as a stream's
+# later calls may come at any time.
 _workspaces = {}
+_workspaces_lock = threading.Lock()
 
 
 def _workspace(device, head_dim, stream, handle):
@@ -182,7 +185,10 @@ def _workspace(device, head_dim, stream, handle):
     key = (device, handle, 64 if head_dim <= 64 else 128 if head_dim <= 128 else 256)
     ws = _workspaces.get(key)
     if ws is None:
-        ws = _workspaces[key] = _workspace_on(stream, device, key[2])
+        with _workspaces_lock:  # (of threads that come together, one makes it)
+            ws = _workspaces.get(key)
+            if ws is None:
+                ws = _workspaces[key] = _workspace_on(stream, device, key[2])
     return ws
 
 
@@ -206,7 +212,7 @@ def paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, *, scale=
     many positions up to its own.  A row that sees no key, or whose token no sequence holds, is 0, its lse -inf.
     ``max_new``: the most new tokens of a sequence, if known (it chooses the kernel,
     not the result).  ``workspace``: as :func:`attention_workspace` makes it;
-    without one, one per stream is kept."""
+    without one, one per stream and size of heads is kept for good."""
     handle = _stream_handle(stream)
     if workspace is None:
         workspace = _workspace(q.device, q.shape[-1], stream, handle)

@@ -86,3 +86,27 @@ def test_workspace_of_another_stream(aq, made):
     s.synchronize()
     assert made == [(s.cuda_stream, False)]
     assert all(torch.equal(o, aq.paged_attention(q, *gpu)) for o in outs)
+
+
+def test_workspace_of_threads(aq, made, monkeypatch):
+    """Threads that make the first calls on one stream together share one workspace."""
+    import threading
+    import time
+
+    from paper_2401_06118_amd import block
+
+    make = block.attention_workspace
+    monkeypatch.setattr(block, "attention_workspace", lambda *a, **k: (time.sleep(0.2), make(*a, **k))[1])
+    device, s = torch.device("cuda", torch.cuda.current_device()), torch.cuda.Stream()
+    got, start = [], threading.Barrier(4)
+
+    def first():
+        start.wait()
+        got.append(block._workspace(device, 128, s, s.cuda_stream))
+
+    threads = [threading.Thread(target=first) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(made) == 1 and all(w is got[0] for w in got) and len(got) == 4
