@@ -12,7 +12,10 @@ a decode step, on torch tensors that live on the GPU:
 Activations are [tokens, heads, head_dim] with any token and head strides (views
 of a fused projection's output), the elements of a head contiguous.  Every
 computation runs in the library's kernels (``include/aqlm.h`` states their
-rules); this module only marshals arguments and makes output tensors.
+rules); this module only marshals arguments and makes output tensors.  As
+elsewhere in this package no autograd graph is recorded: gradients are calls of
+their own.  Tensors that a call writes (``out``, caches) count as modified in place, so
+autograd refuses to use what it saved of them.
 """
 from __future__ import annotations
 

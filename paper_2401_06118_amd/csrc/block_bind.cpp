@@ -112,6 +112,15 @@ at::Tensor output(PyObject* out, const at::Tensor& t) {
   return o;
 }
 
+// A tensor of the caller's that a call has written: autograd's check of saved tensors
+// goes by their version.
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(PyObject* out) {
+  if (given(out)) written(tensor(out, "out"));
+}
+
 aqlm_paged_cache cache(const at::Tensor& k, const at::Tensor& v, const at::Tensor& table, const at::Tensor& lens,
                        const at::Tensor& cu) {
   aqlm_paged_cache c{};
@@ -202,6 +211,8 @@ PyObject* rope(PyObject* const* a) {
   done(aqlm_rope(&hq, &hk, &hoq, &hok, dtype_of(q, "q"), q.size(0), int32_or(q.size(2), "head_dim"),
                  (const int32_t*)pos, &r, stream_of(a[10])),
        "aqlm_rope");
+  written(a[8]);
+  written(a[9]);
   return Py_BuildValue("NN", wrap(oq), wrap(ok));
 }
 
@@ -238,6 +249,8 @@ PyObject* rope_backward(PyObject* const* a) {
     if (nq) wq.zero_();
     if (nk) wk.zero_();
   }
+  written(a[10]);
+  written(a[11]);
   return Py_BuildValue("NNNNN", wrap(gq), wrap(gk), nq ? wrap(wq) : none(), nk ? wrap(wk) : none(),
                        bytes ? wrap(ws) : none());
 }
@@ -262,6 +275,9 @@ PyObject* paged_append(PyObject* const* a) {
   done(aqlm_paged_append(given(a[0]) ? &hq : nullptr, &hk, &hv, given(a[0]) ? &ho : nullptr, &c, k.size(0), &r,
                          stream_of(a[14])),
        "aqlm_paged_append");
+  written(kc);
+  written(tensor(a[4], "v_cache"));
+  if (given(a[0])) written(a[13]);
   return given(a[0]) ? wrap(out) : none();
 }
 
@@ -286,6 +302,7 @@ PyObject* paged_attention(PyObject* const* a) {
                             scale, truth(a[7]), int32_or(integer(a[8]), "window"), ws.data_ptr(), ws.nbytes(),
                             stream_of(a[13])),
        "aqlm_paged_attention");
+  written(a[11]);
   return lse.defined() ? Py_BuildValue("NN", wrap(out), wrap(lse)) : wrap(out);
 }
 
@@ -346,6 +363,7 @@ PyObject* process_logits(PyObject* const* a) {
   done(aqlm_process_logits(x.data_ptr(), rows > 1 ? x.stride(0) : 0, out.data_ptr(), rows > 1 ? out.stride(0) : 0,
                            dtype, rows, vocab, &r, stream_of(a[11])),
        "aqlm_process_logits");
+  written(a[10]);
   return wrap(out);
 }
 
