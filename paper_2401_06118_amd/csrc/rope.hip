@@ -55,6 +55,15 @@ struct Elem<kF32> {
   typedef f8_t V;
 };
 
+// Workgroups of 256 threads, one after another along x and then y: a launch may
+// not have 2^32 threads along one axis, which one wave a head reaches at 2^26 heads.
+constexpr int64_t kMostAlongX = 1 << 22;
+dim3 grid_of(int64_t wgs) {
+  return wgs <= kMostAlongX ? dim3((unsigned)wgs)
+                            : dim3((unsigned)kMostAlongX, (unsigned)((wgs + kMostAlongX - 1) / kMostAlongX));
+}
+__device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Sum over groups of n neighbouring lanes (a power of two).
 __device__ __forceinline__ float group_sum(float v, int n) {
   for (int d = 1; d < n; d *= 2) v += __shfl_xor(v, d);
@@ -198,7 +207,7 @@ template <int TY, bool NORM, bool INTER, bool PAGED, int HPT>
 __global__ void __launch_bounds__(256) k_rope(RopeArgs a, int lanes, int per_token) {
   typedef typename Elem<TY>::V V;
   const int group = threadIdx.x / lanes, i = threadIdx.x % lanes;
-  const int64_t item = (int64_t)blockIdx.x * (256 / lanes) + group;
+  const int64_t item = workgroup() * (256 / lanes) + group;
   const bool live = item < (int64_t)a.tokens * per_token;
   const int token = live ? (int)(item / per_token) : 0;
   const int h0 = live ? (int)(item - (int64_t)token * per_token) * HPT : 0;
@@ -384,7 +393,7 @@ __device__ __forceinline__ void item_at(const RopeArgs& a, int i, int& ia, int& 
 template <int TY, bool PAGED, int ITEMS>
 __global__ void __launch_bounds__(256) k_rope_general(RopeArgs a, int64_t total, int all) {
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t item = workgroup() * 4 + (threadIdx.x >> 6);
   if (item >= total) return;
   const int token = (int)(item / all), h = (int)(item - (int64_t)token * all);
   const int nq = a.side[0].heads, nk = a.side[1].heads;
@@ -516,7 +525,7 @@ __global__ void __launch_bounds__(256) k_rope_grad_general(RopeArgs a) {
 
 __global__ void __launch_bounds__(256) k_rotary_table(const double* inv_freq, int64_t rows, int half, double scale,
                                                       float* table) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = workgroup() * 256 + threadIdx.x;
   if (i >= rows * half) return;
   const int64_t pos = i / half;
   double s, c;
@@ -546,9 +555,9 @@ hipError_t launch_vector(const RopeArgs& a, hipStream_t s) {
     constexpr int kHeads = NORM ? 4 : 2;
     const int per = (all + kHeads - 1) / kHeads;
     const int64_t wgs = ((int64_t)a.tokens * per + groups - 1) / groups;
-    k_rope<TY, NORM, INTER, PAGED, kHeads><<<(unsigned)wgs, 256, 0, s>>>(a, lanes, per);
+    k_rope<TY, NORM, INTER, PAGED, kHeads><<<grid_of(wgs), 256, 0, s>>>(a, lanes, per);
   } else {
-    k_rope<TY, NORM, INTER, PAGED, 1><<<(unsigned)one, 256, 0, s>>>(a, lanes, all);
+    k_rope<TY, NORM, INTER, PAGED, 1><<<grid_of(one), 256, 0, s>>>(a, lanes, all);
   }
   return hipGetLastError();
 }
@@ -563,7 +572,7 @@ hipError_t launch_typed(const RopeArgs& a, bool vec, hipStream_t s) {
   }
   const int all = a.side[0].heads + a.side[1].heads + (PAGED ? a.side[2].heads : 0);
   const int64_t total = (int64_t)a.tokens * all;
-  const unsigned wgs = (unsigned)((total + 3) / 4);
+  const dim3 wgs = grid_of((total + 3) / 4);
   if (a.head_dim - a.rot / 2 <= 4 * kWave)
     k_rope_general<TY, PAGED, 4><<<wgs, 256, 0, s>>>(a, total, all);
   else
@@ -647,7 +656,7 @@ hipError_t launch_rope_grad_norm(RopeArgs a, int dtype, hipStream_t s) {
 
 hipError_t launch_rotary_table(const double* inv_freq, int64_t rows, int half, double scale, float* table,
                                hipStream_t s) {
-  k_rotary_table<<<(unsigned)((rows * half + 255) / 256), 256, 0, s>>>(inv_freq, rows, half, scale, table);
+  k_rotary_table<<<grid_of((rows * half + 255) / 256), 256, 0, s>>>(inv_freq, rows, half, scale, table);
   return hipGetLastError();
 }
 
