@@ -139,6 +139,8 @@ def rope_backward(dq, dk, table, positions, *, q=None, k=None, q_weight=None, k_
     r = (_ext or _binding()).rope_backward(dq, dk, table, positions, q, k, q_weight, k_weight, eps, interleaved, oq,
                                            ok, _stream_handle(stream))
     if stream is not None:
+        if dq.shape[0] == 0:  # (the weights' gradients are zeros, written on the current stream)
+            stream.wait_stream(torch.cuda.current_stream())
         _made(stream, *(r if out is None else r[2:]))
     return r[:4]
 

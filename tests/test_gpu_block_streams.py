@@ -110,3 +110,19 @@ def test_workspace_of_threads(aq, made, monkeypatch):
     for t in threads:
         t.join()
     assert len(made) == 1 and all(w is got[0] for w in got) and len(got) == 4
+
+
+def test_gradients_of_no_tokens_on_another_stream(aq):
+    """The zeros that rope_backward returns for no tokens are there for the stream that it was given."""
+    z = lambda *s: torch.zeros(*s, dtype=torch.float16, device=DEV)  # noqa: E731
+    q, k, w = z(0, 4, 64), z(0, 2, 64), torch.ones(64, dtype=torch.float16, device=DEV)
+    table, pos = aq.rotary_table(4, 64), torch.zeros(0, dtype=torch.int32, device=DEV)
+    s = torch.cuda.Stream()
+    junk = [torch.full((64,), 7.0, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    torch.cuda._sleep(200_000_000)  # the current stream has something to do
+    got = aq.rope_backward(q, k, table, pos, q=q, k=k, q_weight=w, k_weight=w, stream=s)
+    with torch.cuda.stream(s):
+        seen = [g.cpu() for g in got[2:]]
+    assert all((g == 0).all() for g in seen)
