@@ -493,8 +493,8 @@ int aqlm_gemv_sorted_grouped(const aqlm_sorted_problem* problems, int32_t count,
  * Activations are [tokens][heads][head_dim] with strides in elements, the
  * elements of a head contiguous (views of a fused projection's output need no
  * copy).  Types: AQLM_F16, AQLM_BF16 and, where stated, AQLM_F32; sums, norms and
- * softmax statistics are fp32, results are rounded once.  `tokens` of 0 is a
- * call without work.  Values in device arrays (positions, lengths, page numbers)
+ * softmax statistics are fp32, results are rounded once (attention of many rows
+ * rounds its weights too, see there).  `tokens` of 0 is a call without work.  Values in device arrays (positions, lengths, page numbers)
  * cannot be checked on the host: whatever they hold, nothing is read or
  * written outside the arrays, and the text says what the results then are. */
 
@@ -591,9 +591,13 @@ int aqlm_paged_append(const aqlm_heads* q, const aqlm_heads* k, const aqlm_heads
  * limited).  A row without keys, or of a token that no sequence holds, gives zeros.  Keys that a row does not see
  * take no part in it, whatever they hold.  lse (NULL or fp32 [tokens][heads]): the
  * logarithm of the softmax's denominator, -inf where the row is zeros for want of keys.
- *   max_new: the most new tokens of a sequence, if known (0: unknown); it
- *   chooses the kernel, not the result: up to 16 rows (new tokens x heads per kv
- *   head) of a sequence are bound by the cache's bytes, more by the products.
+ *   max_new: the most new tokens of a sequence, if known (0: unknown, the call's
+ *   tokens are taken).  It chooses the kernel, any value is right: up to 16 rows
+ *   (new tokens x heads per kv head) of a sequence are bound by the cache's bytes,
+ *   more by the products.  The first kernel carries the weights exp(...) in two parts of
+ *   the cache's type; the second rounds them to it before the product with the
+ *   values, and its results are 1.3 to 1.4 times as far from exact ones as one rounding
+ *   is.
  *   Pages outside the cache are read as its first or last page; lengths past the
  *   block table's are cut to it.
  *   workspace: aqlm_paged_attention_workspace_bytes(head_dim) bytes, 16-byte

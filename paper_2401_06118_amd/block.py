@@ -10,7 +10,10 @@ a decode step, on torch tensors that live on the GPU:
 - :func:`process_logits` - penalties for repeated tokens, biases, grammar masks.
 
 Activations are [tokens, heads, head_dim] with any token and head strides (views
-of a fused projection's output), the elements of a head contiguous.  Every
+of a fused projection's output), the elements of a head contiguous.  ``stream``: where
+the launches go, the current stream if not given; another one has to wait for the
+current one first (``stream.wait_stream``), whose work may still use the inputs and the
+memory that outputs are made of.  Every
 computation runs in the library's kernels (``include/aqlm.h`` states their
 rules); this module only marshals arguments and makes output tensors.  As
 elsewhere in this package no autograd graph is recorded: gradients are calls of
@@ -215,8 +218,10 @@ def paged_attention(q, k_cache, v_cache, block_table, kv_lens, cu_new, *, scale=
     head e // (heads / kv heads).  ``scale``: 1 / sqrt(head_dim) if not given.
     ``causal``: a token sees keys up to its own position; ``window`` above 0: only that
     many positions up to its own.  A row that sees no key, or whose token no sequence holds, is 0, its lse -inf.
-    ``max_new``: the most new tokens of a sequence, if known (it chooses the kernel,
-    not the result).  ``workspace``: as :func:`attention_workspace` makes it;
+    ``max_new``: the most new tokens of a sequence, if known.  It chooses the kernel, any
+    value is right; without it a call of more than 16 rows (tokens times heads per kv
+    head) takes the kernel for many rows, which is up to twice as slow for single tokens
+    and rounds the weights once more.  ``workspace``: as :func:`attention_workspace` makes it;
     without one, one per stream and size of heads is kept for good."""
     handle = _stream_handle(stream)
     if workspace is None:

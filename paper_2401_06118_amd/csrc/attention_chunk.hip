@@ -8,8 +8,8 @@
 // (global_load_lds_dwordx4, a lane fetches 16 bytes of its row's page), a tile
 // ahead of the one being computed.  Pages of 16 slots and more give each wave's 16
 // rows of a tile one page: its address is scalar, and the loads take no vector
-// instruction (594 -> 549 us); smaller pages, and the first and last tile of a
-// unit, look each row's page up (pages of 8 slots: 640 us).
+// instruction (594 -> 549 us in a kernel trace of the case below); smaller pages, and
+// the first and last tile of a unit, look each row's page up (pages of 8 slots: 640 us).
 //
 // Products, 32 x 32 x 16, rows as columns of the results, so that a lane holds
 // one row's weights and a row's maximum, denominator and factors need no
@@ -23,19 +23,25 @@
 // reads of 16 (keys) and 8 (values, two 32-byte blocks) rows cover all banks; the
 // loads apply the permutation on the memory side.
 //
-// Measured: 2048 new tokens over 8192 keys, 64 heads over 8, bf16: 468 us, 1027 TFLOP/s
-// (a library product of 8192^3 random values: 1450 here); 2048 tokens without earlier
-// keys 93 us.  The matrix cores are busy 48 % of the cycles and the vector units
+// Measured: 2048 new tokens over 8192 keys, 64 heads over 8, bf16, calls back to back: 462
+// to 472 us, 1020 to 1040 TFLOP/s (a library product of 8192^3 random values: 1450 here); 2048
+// tokens without earlier keys 93 us.  Figures from a kernel trace are of single launches
+// with a synchronize between them, which cost this case some clock: 505 to 554 us.  Heads of
+// 80 and 96 elements run the form for 128: 1024 tokens over 4097 keys, 32 heads over 8: 83, 84
+// and, of 128 elements, 82 us.  The matrix cores are busy 48 % of the cycles and the vector units
 // most of the others; the clock gives way under the load (1.7 to 2 GHz), and
 // neither priorities that set the two workgroups of a CU against each other nor more
 // fragments in flight changed the time.  Running a tile's scores beside the
 // exponentials of the tile before needs 32 more registers than there are
-// (770 us, spilled).
+// (trace: 770 us, spilled).
 //
 // The sums are rescaled only where a row's maximum rises by more than 2^8: until
 // then the old one stays in the exponents.  Weights are rounded once to the
-// cache's type (fp16: up to 2^15, so that small ones stay normal); the
-// denominator adds them up unrounded.
+// cache's type (fp16: up to 2^15, so that small ones stay normal), as the second
+// product takes them; the denominator adds them up unrounded.  The error against 64
+// bits grows from one rounding's 0.0017 to 0.0023 (bf16; fp16 0.00021 to 0.00027).  Weights
+// in two parts, as attention_step.hip has them, would take half as many products again
+// and registers that are not there.
 #include "attention.h"
 #include "launch.h"
 #include "lds_sync.h"
@@ -50,9 +56,9 @@ constexpr int kRows = kWaves * kWaveRows;
 constexpr int kTile = 64;
 // Division of the work.  A unit's beginning and end cost about three tiles; a share
 // has at least two tiles and that, if a unit has: smaller shares write and join
-// more pieces, larger ones leave CUs idle (14 sequences of 1 to 300 new tokens, 32
-// heads over 8, window 1024: 33.8 us with 5, 38.4 with 6 and 2 extra, 44 with 10 and 2;
-// one of 20 over 1000: 25.5, 22.9, 28.7).  Pieces of a unit are joined one after
+// more pieces, larger ones leave CUs idle.  A trade that no value wins everywhere (kernel
+// trace; 14 sequences of 1 to 300 new tokens, 32 heads over 8, window 1024: 33.8 us with 5,
+// 38.4 with 6 and 2 extra, 44 with 10 and 2; one of 20 over 1000: 25.5, 22.9, 28.7).  Pieces of a unit are joined one after
 // another by the workgroup that finishes last, 64 KB each, so there are few (4
 // sequences of up to 100 over 8000: 63 us with 16, 92 with 32).
 constexpr int kExtra = 3;

@@ -22,11 +22,13 @@
 // left), two products each: the matrix cores idle here, and the result carries
 // one 16-bit rounding instead of two.
 //
-// Measured: 64 sequences of up to 16000 keys, 64 heads over 8, bf16 (767 MB): 155 us, 4.9
-// TB/s; all of 5000 keys 231 us, 5.7 TB/s; traffic as counted is the keys and
-// values once.  One sequence of 1024 keys, 32 heads (17 MB): 14.0 us, of which about 3
-// are the launch, 3 the division of the work, 3 the joining of pieces and the rest
-// the chain of page number, keys, values.
+// Measured, calls back to back: 64 sequences of up to 16000 keys, 64 heads over 8, bf16
+// (767 MB): 155 us, 4.9 TB/s; all of 5000 keys 231 us, 5.7 TB/s; traffic as counted is the
+// keys and values once.  One sequence of 1024 keys, 32 heads (17 MB): 13.9 us, of which
+// about 3 are the launch, 3 the division of the work, 3 the joining of pieces and
+// the rest the chain of page number, keys, values.  Heads of 80 and 96 elements run the
+// form for 128, whose lanes past the head load its first 16 bytes again: 32 sequences of 4000
+// keys, 32 heads over 8 (328 and 393 MB) 84 and 87 us; of 128 elements (525 MB) 103.
 //
 // The next tile's keys are loaded into the registers of this one's as soon as
 // S^T is done, its values as soon as these are in LDS, and the page numbers one
@@ -45,7 +47,7 @@ constexpr int kTile = kWaves * kWaveKeys;
 // Division of the work: a share may be one tile (one sequence of 1024 keys, 32 heads:
 // 14.0 us; two tiles at least: 16.5), and a unit many pieces, which the last of its
 // workgroups reads (one of 60001 keys, 8 heads over one: 43.8 us with 64, 55 with 16,
-// 57 with 256).
+// 57 with 256; single launches, kernel trace).
 constexpr int kExtra = 0;
 constexpr int kLeast = 1;
 constexpr int kPieces = 64;  // whole shares of a split unit (one piece more where it begins inside one)

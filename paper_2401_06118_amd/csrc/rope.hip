@@ -16,12 +16,15 @@
 // whose elements pair with each other (half layout) or within (interleaved), so a
 // pair never crosses lanes, and a lane's 8 cos and sin serve all heads that it
 // runs of its token.  All loads of the heads go out before the first is used.
-// Measured: norms and rotation of 4096 tokens of 64 + 8 heads of 128, bf16 (153 MB):
-// 29.7 us, 5.2 TB/s (a copy of as much: 31); the gradients with norms of 2048 tokens of
-// 32 + 32 heads (102 MB) 23.4 us and 4.9 for the sum over workgroups; two heads' loads at
-// a time there: 25.1.
+// Measured, calls back to back: norms and rotation of 4096 tokens of 64 + 8 heads of 128,
+// bf16 (153 MB): 29.8 us, 5.2 TB/s (a copy of as much: 31); the gradients with norms of 2048
+// tokens of 32 + 32 heads (102 MB) 27.8 us, of which 23.5 are the first kernel's and 4.9 the
+// sum over workgroups (kernel trace; two heads' loads at a time there: 25.1).
 // Any other alignment, head size or rotated part takes the general kernels, one
-// wave a head.
+// wave a head and 2 or 4 bytes a lane, bound by their instructions: 4096 tokens of 32 + 8
+// heads of 96 elements, 24 of them rotated, bf16 (63 MB) 62 us, with norms 73, their gradients
+// 109 (all 96 rotated, by the vectorised kernels: 19, 20 and 31); appended 98 and 111 (22
+// and 27).
 #include "rope.h"
 
 #include <algorithm>
@@ -190,7 +193,7 @@ __device__ __forceinline__ typename Elem<TY>::V load8(const void* base, int64_t 
   return v;
 }
 // STREAM: past the L2s, for outputs that do not fit them (4096 tokens of 72
-// heads of 128 in bf16, with norms: 41 us with plain stores, 32 with these).
+// heads of 128 in bf16, with norms, kernel trace: 41 us with plain stores, 32 with these).
 template <int TY, bool STREAM>
 __device__ __forceinline__ void store8(void* base, int64_t off, const float* y) {
   typedef typename Elem<TY>::V V;
@@ -547,8 +550,8 @@ hipError_t launch_vector(const RopeArgs& a, hipStream_t s) {
   const int groups = 256 / lanes;
   // several heads a group once that still leaves every CU work: the table's row
   // and the position are read once for them.  Two, or four with norms (4096 tokens
-  // of 72 heads of 128, bf16: two 28.4 us without norms and 31.9 with them, four
-  // 29.3 and 30.7; appending 2700 tokens of 32 + 32 + 32 heads 25.6 against 27.7; eight are slower
+  // of 72 heads of 128, bf16, kernel trace: two 28.4 us without norms and 31.9 with them,
+  // four 29.3 and 30.7; appending 2700 tokens of 32 + 32 + 32 heads 25.6 against 27.7; eight are slower
   // everywhere).
   const int64_t one = ((int64_t)a.tokens * all + groups - 1) / groups;
   if (one >= 8 * (int64_t)num_cus()) {
