@@ -649,6 +649,96 @@ typedef struct aqlm_logit_rules {
 int aqlm_process_logits(const void* logits, int64_t logits_stride, void* out, int64_t out_stride, int32_t dtype,
                         int64_t rows, int64_t vocab, const aqlm_logit_rules* rules, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The ends of a model and the norms of its residual stream: the embedding, layer and
+ * RMS norms, a loss against a teacher's largest logits, the draw of a token; and the
+ * gradients.  Rows have strides in elements and contiguous elements; any element's
+ * address will do.  Types: AQLM_F16, AQLM_BF16, AQLM_F32; sums and statistics are held
+ * in 32 bits or more, results are rounded once. */
+
+/* out[t] = scale * table[tokens[t]]; zeros for a token outside the table (padding).
+ * table: [vocab][dim]; out: [count][dim], of its type.  vocab up to 2^30, dim up to 2^24. */
+int aqlm_embed(const void* table, int64_t table_stride, const int32_t* tokens, void* out, int64_t out_stride,
+               int32_t dtype, int64_t count, int64_t vocab, int64_t dim, float scale, void* stream);
+
+/* grad[v] = scale * the sum of dout[t] over the t with tokens[t] = v: the gradient of
+ * aqlm_embed's table, all rows written (zeros where the token does not occur), of dout's
+ * type or fp32.  The places are sorted by token on the device and summed in fp32 in a fixed
+ * order.  workspace: aqlm_embed_backward_workspace_bytes(count, dim, dtype) bytes, 16-byte
+ * aligned, any contents. */
+size_t aqlm_embed_backward_workspace_bytes(int64_t count, int64_t dim, int32_t dtype);
+int aqlm_embed_backward(const void* dout, int64_t dout_stride, const int32_t* tokens, void* grad, int64_t grad_stride,
+                        int32_t dtype, int32_t grad_dtype, int64_t count, int64_t vocab, int64_t dim, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* A norm; weight and bias: [dim] of the activations' type, or NULL. */
+typedef struct aqlm_norm {
+  const void* weight;
+  const void* bias; /* not read by the backward pass */
+  float eps;        /* >= 0 */
+  int32_t rms;      /* RMS norm: the mean is not subtracted */
+} aqlm_norm;
+
+/* h = x + residual, rounded to the type (residual NULL: h = x); out = (h - mean h) /
+ * sqrt(mean (h - mean h)^2 + eps) * weight + bias over each row of dim elements, up to
+ * 16384.  sum (NULL, or where residual is given): gets h.  out and sum may each be x or
+ * residual itself (same address and stride), not one another. */
+int aqlm_layer_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* out,
+                    int64_t out_stride, void* sum, int64_t sum_stride, int32_t dtype, int64_t rows, int64_t dim,
+                    const aqlm_norm* norm, void* stream);
+
+/* Gradients of aqlm_layer_norm: dy is that of out, x what was normalised (h), dsum (or
+ * NULL) that of h from elsewhere, added to dx.  dx: the gradient of h, and so of x and of
+ * residual; it may be dy, x or dsum itself.  dweight, dbias (fp32 [dim], or NULL: left
+ * out) are written, not added to, summed over the rows in a fixed order.  workspace:
+ * aqlm_layer_norm_backward_workspace_bytes(dim) bytes where there is one of them, 16-byte
+ * aligned, any contents. */
+size_t aqlm_layer_norm_backward_workspace_bytes(int64_t dim);
+int aqlm_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* dsum,
+                             int64_t dsum_stride, void* dx, int64_t dx_stride, float* dweight, float* dbias,
+                             int32_t dtype, int64_t rows, int64_t dim, const aqlm_norm* norm, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's largest logits: ids [rows][listed], the tokens, and teacher
+ * (any of the types), their logits; ids outside the vocabulary are no entries, and an id that
+ * is listed several times has the sum of its entries' mass.  With q = softmax(logits /
+ * temperature) and P = the sum of p_k:
+ *   without teacher_lse   p_k = softmax over the row's entries of teacher / temperature,
+ *   with it [rows]        p_k = exp(teacher / temperature - teacher_lse), the rest of the mass
+ *                         p_r = max(0, 1 - P) against q_r, the mass of q outside the entries
+ *                         (p_r = 0 where every token is listed);
+ *   loss[row] = sum_k p_k log(p_k / q_k) + p_r log(p_r / q_r)                     (fp32)
+ *   grad[row] = weights[row] * dloss[row] / dlogits[row]                   (logits' type)
+ * (weights NULL: 1; it carries a loss scale, 1 / tokens, temperature^2).  A row whose weight
+ * is 0 has loss and gradient 0, whatever its logits are; so has a row without entries (with
+ * teacher_lse its whole mass is one outcome).  grad NULL: the loss alone; it may be the logits
+ * (same address and stride).  Limits: 2^22 - 1 rows, vocab 2^19, 2048 listed. */
+int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, const void* teacher,
+                      int64_t teacher_stride, int32_t teacher_dtype, const int32_t* ids, int64_t ids_stride,
+                      const float* teacher_lse, const float* weights, float temperature, float* loss, void* grad,
+                      int64_t grad_stride, int64_t rows, int64_t vocab, int64_t listed, void* stream);
+
+/* How tokens are drawn; [rows] each, NULL: left out. */
+typedef struct aqlm_sampling {
+  const float* temperature; /* NULL: 1; not above 0: the largest logit, of equal ones the first */
+  const int32_t* top_k;     /* not above 0: all */
+  const float* top_p;       /* 1 and above: all; 0 and below: one */
+  const float* min_p;       /* not above 0: all; above 1: as 1 */
+} aqlm_sampling;
+
+/* tokens[row] = a token of logits [rows][vocab] by uniform[row] in [0, 1).  In the order of
+ * falling logits, equal ones by their number, with weights exp((l - max) / temperature): top_k
+ * keeps the first k, top_p of these the ones with less than p of their mass before them,
+ * min_p those with l - max >= temperature * log(min_p), and at least one is kept.  The token is
+ * the first, in the order of numbers, at which the kept mass exceeds uniform times all kept mass.
+ * -inf is a masked token; a row with NaN, or with nothing else than masked tokens, gives -1.
+ * logprob (NULL, or [rows]): the logarithm of the token's share of the kept mass (0 at
+ * temperature 0, NaN with -1).  Weights are computed in 64 bits and rounded to multiples of
+ * 2^-44, sums of them are exact: the same token whatever the batch.  Limits: 2^20 rows,
+ * vocab 2^19. */
+int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_t rows, int64_t vocab,
+                const float* uniform, const aqlm_sampling* rules, int32_t* tokens, float* logprob, void* stream);
+
 /* Static text for a status code (never NULL). */
 const char* aqlm_status_string(int status);
 

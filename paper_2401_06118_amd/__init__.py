@@ -21,7 +21,10 @@ Eq. 2 and Fig. 3).  This package exposes the three operations of the C ABI in
   code from a codebook chunk held on chip;
 - the operators around these products in a block and in a decode step
   (``block.py``): :func:`rotary_table`, :func:`rope`, :func:`rope_backward`,
-  :func:`paged_append`, :func:`paged_attention`, :func:`process_logits`.
+  :func:`paged_append`, :func:`paged_attention`, :func:`process_logits`;
+- the ends of a model and the norms of its residual stream (``ends.py``):
+  :func:`embed`, :func:`embed_backward`, :func:`layer_norm`,
+  :func:`layer_norm_backward`, :func:`distill_loss`, :func:`sample`.
 
 Every computation runs in the hand-written HIP kernels of
 ``libaqlm_mi355x.so``; this module only marshals arguments.
@@ -501,3 +504,5 @@ def gemv_sorted_grouped(problems, *, workspace=None, stream=None):
 
 from .block import (  # noqa: E402,F401  (after the helpers it uses)
     attention_workspace, paged_append, paged_attention, process_logits, rope, rope_backward, rotary_table)
+from .ends import (  # noqa: E402,F401
+    distill_loss, embed, embed_backward, layer_norm, layer_norm_backward, sample)

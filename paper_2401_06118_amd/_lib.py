@@ -78,6 +78,18 @@ class LogitRules(ctypes.Structure):
                 ("history", ctypes.c_int32), ("biases", ctypes.c_int32)]
 
 
+class Norm(ctypes.Structure):
+    """Mirror of ``aqlm_norm`` in include/aqlm.h."""
+    _fields_ = [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("rms", ctypes.c_int32)]
+
+
+class Sampling(ctypes.Structure):
+    """Mirror of ``aqlm_sampling`` in include/aqlm.h."""
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
+
+
 _lock = threading.Lock()
 _lib = None
 
@@ -172,6 +184,24 @@ def load():
         lib.aqlm_paged_attention.restype = ctypes.c_int
         lib.aqlm_process_logits.argtypes = [p, i64, p, i64, i32, i64, i64, ctypes.POINTER(LogitRules), p]
         lib.aqlm_process_logits.restype = ctypes.c_int
+        f32, size = ctypes.c_float, ctypes.c_size_t
+        lib.aqlm_embed.argtypes = [p, i64, p, p, i64, i32, i64, i64, i64, f32, p]
+        lib.aqlm_embed.restype = ctypes.c_int
+        lib.aqlm_embed_backward_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.aqlm_embed_backward_workspace_bytes.restype = size
+        lib.aqlm_embed_backward.argtypes = [p, i64, p, p, i64, i32, i32, i64, i64, i64, f32, p, size, p]
+        lib.aqlm_embed_backward.restype = ctypes.c_int
+        lib.aqlm_layer_norm.argtypes = [p, i64, p, i64, p, i64, p, i64, i32, i64, i64, ctypes.POINTER(Norm), p]
+        lib.aqlm_layer_norm.restype = ctypes.c_int
+        lib.aqlm_layer_norm_backward_workspace_bytes.argtypes = [i64]
+        lib.aqlm_layer_norm_backward_workspace_bytes.restype = size
+        lib.aqlm_layer_norm_backward.argtypes = [p, i64, p, i64, p, i64, p, i64, p, p, i32, i64, i64,
+                                                 ctypes.POINTER(Norm), p, size, p]
+        lib.aqlm_layer_norm_backward.restype = ctypes.c_int
+        lib.aqlm_distill_loss.argtypes = [p, i64, i32, p, i64, i32, p, i64, p, p, f32, p, p, i64, i64, i64, i64, p]
+        lib.aqlm_distill_loss.restype = ctypes.c_int
+        lib.aqlm_sample.argtypes = [p, i64, i32, i64, i64, p, ctypes.POINTER(Sampling), p, p, p]
+        lib.aqlm_sample.restype = ctypes.c_int
         lib.aqlm_status_string.argtypes = [ctypes.c_int]
         lib.aqlm_status_string.restype = ctypes.c_char_p
         _lib = lib

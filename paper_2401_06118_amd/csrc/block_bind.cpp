@@ -1,4 +1,4 @@
-// Python binding of the operators in block.py: shapes, types and strides are read
+// Python binding of the operators in block.py and ends.py: shapes, types and strides are read
 // from the tensors, output tensors are made, and the C ABI (include/aqlm.h) is
 // called.  A decode step makes several such calls per layer, each a few
 // microseconds long on the GPU: marshalled in Python they took 12 to 18 us of
@@ -367,6 +367,195 @@ PyObject* process_logits(PyObject* const* a) {
   return wrap(out);
 }
 
+// ---------------------------------------------------------------------------
+// ends.py
+
+// A call's launches go to the tensors' device, whichever is the current one.
+struct OnDevice {
+  int before = 0;
+  bool changed = false;
+  explicit OnDevice(const at::Tensor& t) {
+    if (hipGetDevice(&before) == hipSuccess && t.get_device() != before)
+      changed = hipSetDevice(t.get_device()) == hipSuccess;
+  }
+  ~OnDevice() {
+    if (changed) (void)hipSetDevice(before);
+  }
+};
+
+// A [rows, n] activation with contiguous rows; `like`: one whose type and device it has;
+// rows, n of -1: any.
+const at::Tensor& rows2(PyObject* o, const char* name, const at::Tensor* like = nullptr, int64_t rows = -1,
+                        int64_t n = -1) {
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda() || t.dim() != 2 || (t.size(1) > 1 && t.size(0) > 0 && t.stride(1) != 1))
+    refuse(std::string(name) + " must be a GPU tensor with two dimensions, its rows contiguous");
+  if ((rows >= 0 && t.size(0) != rows) || (n >= 0 && t.size(1) != n))
+    refuse(std::string(name) + " does not have the shape of the other tensors");
+  if (like && (t.scalar_type() != like->scalar_type() || t.device() != like->device()))
+    refuse(std::string(name) + " must have the type and device of the other tensors");
+  dtype_of(t, name);
+  return t;
+}
+// (the stride of a dimension of one is never used, whatever it says)
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
+
+// A caller's output of a shape and type, checked, or a new one.
+at::Tensor output2(PyObject* out, const char* name, const at::Tensor& like, int64_t rows, int64_t n, at::ScalarType type) {
+  if (!given(out)) return at::empty({rows, n}, like.options().dtype(type));
+  const at::Tensor& o = rows2(out, name, nullptr, rows, n);
+  if (o.scalar_type() != type || o.device() != like.device())
+    refuse(std::string(name) + " must have the type and device of the result");
+  return o;
+}
+
+aqlm_norm norm_of(PyObject* weight, PyObject* bias, double eps, bool rms, const at::Tensor& like) {
+  aqlm_norm n{};
+  if (given(weight)) n.weight = vector(tensor(weight, "weight"), "weight", like, like.size(1), like.scalar_type());
+  if (given(bias)) n.bias = vector(tensor(bias, "bias"), "bias", like, like.size(1), like.scalar_type());
+  n.eps = (float)eps;
+  n.rms = rms;
+  return n;
+}
+
+// table, tokens, scale, out, stream
+PyObject* embed(PyObject* const* a) {
+  const at::Tensor &table = rows2(a[0], "table"), &tokens = tensor(a[1], "tokens");
+  if (tokens.dim() != 1) refuse("tokens must be an int32 tensor [tokens]");
+  const int64_t count = tokens.numel();
+  const void* ids = vector(tokens, "tokens", table, count, at::kInt);
+  const at::Tensor out = output2(a[3], "out", table, count, table.size(1), table.scalar_type());
+  const OnDevice on(table);
+  done(aqlm_embed(table.data_ptr(), row_stride(table), (const int32_t*)ids, out.data_ptr(), row_stride(out),
+                  dtype_of(table, "table"), count, table.size(0), table.size(1), (float)number(a[2]), stream_of(a[4])),
+       "aqlm_embed");
+  written(a[3]);
+  return wrap(out);
+}
+
+// dout, tokens, vocab, scale, fp32, out, stream; the last of the results is the workspace
+PyObject* embed_backward(PyObject* const* a) {
+  const at::Tensor &dout = rows2(a[0], "dout"), &tokens = tensor(a[1], "tokens");
+  const int64_t count = dout.size(0), vocab = integer(a[2]);
+  if (tokens.dim() != 1) refuse("tokens must be an int32 tensor [tokens]");
+  const void* ids = vector(tokens, "tokens", dout, count, at::kInt);
+  if (vocab <= 0) refuse("vocab must be positive");
+  at::ScalarType type = truth(a[4]) ? at::kFloat : dout.scalar_type();
+  if (given(a[5]) && tensor(a[5], "out").scalar_type() == at::kFloat) type = at::kFloat;
+  const size_t bytes = aqlm_embed_backward_workspace_bytes(count, dout.size(1), dtype_of(dout, "dout"));
+  if (bytes == 0) done(AQLM_ERR_SHAPE, "aqlm_embed_backward");
+  const at::Tensor out = output2(a[5], "out", dout, vocab, dout.size(1), type);
+  const at::Tensor ws = at::empty({(int64_t)bytes}, dout.options().dtype(at::kByte));
+  const OnDevice on(dout);
+  done(aqlm_embed_backward(dout.data_ptr(), row_stride(dout), (const int32_t*)ids, out.data_ptr(), row_stride(out),
+                           dtype_of(dout, "dout"), dtype_of(out, "out"), count, vocab, dout.size(1), (float)number(a[3]),
+                           ws.data_ptr(), bytes, stream_of(a[6])),
+       "aqlm_embed_backward");
+  written(a[5]);
+  return Py_BuildValue("NN", wrap(out), wrap(ws));
+}
+
+// x, weight, bias, residual, eps, rms, out, sum_out, stream
+PyObject* layer_norm(PyObject* const* a) {
+  const at::Tensor& x = rows2(a[0], "x");
+  const int64_t rows = x.size(0), dim = x.size(1);
+  const aqlm_norm n = norm_of(a[1], a[2], number(a[4]), truth(a[5]), x);
+  const at::Tensor out = output2(a[6], "out", x, rows, dim, x.scalar_type());
+  const bool both = given(a[3]);
+  if (!both && given(a[7])) refuse("sum_out goes with residual");
+  at::Tensor r, sum;
+  if (both) {
+    r = rows2(a[3], "residual", &x, rows, dim);
+    sum = output2(a[7], "sum_out", x, rows, dim, x.scalar_type());
+  }
+  const OnDevice on(x);
+  done(aqlm_layer_norm(x.data_ptr(), row_stride(x), both ? r.data_ptr() : nullptr, both ? row_stride(r) : 0,
+                       out.data_ptr(), row_stride(out), both ? sum.data_ptr() : nullptr, both ? row_stride(sum) : 0,
+                       dtype_of(x, "x"), rows, dim, &n, stream_of(a[8])),
+       "aqlm_layer_norm");
+  written(a[6]);
+  written(a[7]);
+  return both ? Py_BuildValue("NN", wrap(out), wrap(sum)) : wrap(out);
+}
+
+// dy, x, weight, dsum, eps, rms, bias, out, stream; the last of the results is the workspace
+PyObject* layer_norm_backward(PyObject* const* a) {
+  const at::Tensor& dy = rows2(a[0], "dy");
+  const int64_t rows = dy.size(0), dim = dy.size(1);
+  const at::Tensor& x = rows2(a[1], "x", &dy, rows, dim);
+  const aqlm_norm n = norm_of(a[2], Py_None, number(a[4]), truth(a[5]), dy);
+  at::Tensor dsum, ws, dw, db;
+  if (given(a[3])) dsum = rows2(a[3], "dsum", &dy, rows, dim);
+  const at::Tensor out = output2(a[7], "out", dy, rows, dim, dy.scalar_type());
+  const bool bias = truth(a[6]);
+  size_t bytes = 0;
+  if (n.weight || bias) {
+    bytes = aqlm_layer_norm_backward_workspace_bytes(dim);
+    ws = at::empty({(int64_t)bytes}, dy.options().dtype(at::kByte));
+    if (n.weight) dw = at::empty({dim}, dy.options().dtype(at::kFloat));
+    if (bias) db = at::empty({dim}, dy.options().dtype(at::kFloat));
+  }
+  const OnDevice on(dy);
+  done(aqlm_layer_norm_backward(dy.data_ptr(), row_stride(dy), x.data_ptr(), row_stride(x),
+                                dsum.defined() ? dsum.data_ptr() : nullptr, dsum.defined() ? row_stride(dsum) : 0,
+                                out.data_ptr(), row_stride(out), dw.defined() ? dw.data_ptr<float>() : nullptr,
+                                bias ? db.data_ptr<float>() : nullptr, dtype_of(dy, "dy"), rows, dim, &n,
+                                bytes ? ws.data_ptr() : nullptr, bytes, stream_of(a[8])),
+       "aqlm_layer_norm_backward");
+  written(a[7]);
+  return Py_BuildValue("NNNN", wrap(out), dw.defined() ? wrap(dw) : none(), bias ? wrap(db) : none(),
+                       bytes ? wrap(ws) : none());
+}
+
+// logits, teacher, ids, teacher_lse, weights, temperature, grad, out, stream
+PyObject* distill_loss(PyObject* const* a) {
+  const at::Tensor& x = rows2(a[0], "logits");
+  const int64_t rows = x.size(0), vocab = x.size(1);
+  const at::Tensor &t = rows2(a[1], "teacher_logits", nullptr, rows), &ids = tensor(a[2], "teacher_ids");
+  if (t.device() != x.device()) refuse("teacher_logits must be on the device of logits");
+  const void* pi = table2(ids, "teacher_ids", x, rows, at::kInt);
+  if (ids.size(1) != t.size(1)) refuse("teacher_logits and teacher_ids must have one shape");
+  const void* lse = given(a[3]) ? vector(tensor(a[3], "teacher_lse"), "teacher_lse", x, rows, at::kFloat) : nullptr;
+  const void* w = given(a[4]) ? vector(tensor(a[4], "weights"), "weights", x, rows, at::kFloat) : nullptr;
+  const bool want = truth(a[6]);
+  if (!want && given(a[7])) refuse("out is the gradient's, which is not asked for");
+  at::Tensor grad;
+  if (want) grad = output2(a[7], "out", x, rows, vocab, x.scalar_type());
+  const at::Tensor loss = at::empty({rows}, x.options().dtype(at::kFloat));
+  const OnDevice on(x);
+  done(aqlm_distill_loss(x.data_ptr(), row_stride(x), dtype_of(x, "logits"), t.data_ptr(), row_stride(t),
+                         dtype_of(t, "teacher_logits"), (const int32_t*)pi, row_stride(ids), (const float*)lse,
+                         (const float*)w, (float)number(a[5]), loss.data_ptr<float>(), want ? grad.data_ptr() : nullptr,
+                         want ? row_stride(grad) : 0, rows, vocab, ids.size(1), stream_of(a[8])),
+       "aqlm_distill_loss");
+  written(a[7]);
+  return Py_BuildValue("NN", wrap(loss), want ? wrap(grad) : none());
+}
+
+// logits, uniform, temperature, top_k, top_p, min_p, return_logprob, stream
+PyObject* sample(PyObject* const* a) {
+  const at::Tensor& x = rows2(a[0], "logits");
+  const int64_t rows = x.size(0);
+  const void* u = vector(tensor(a[1], "uniform"), "uniform", x, rows, at::kFloat);
+  auto rule = [&](int i, const char* name, at::ScalarType type) -> const void* {
+    return given(a[i]) ? vector(tensor(a[i], name), name, x, rows, type) : nullptr;
+  };
+  aqlm_sampling r{};
+  r.temperature = (const float*)rule(2, "temperature", at::kFloat);
+  r.top_k = (const int32_t*)rule(3, "top_k", at::kInt);
+  r.top_p = (const float*)rule(4, "top_p", at::kFloat);
+  r.min_p = (const float*)rule(5, "min_p", at::kFloat);
+  const bool want = truth(a[6]);
+  const at::Tensor tokens = at::empty({rows}, x.options().dtype(at::kInt));
+  at::Tensor logprob;
+  if (want) logprob = at::empty({rows}, x.options().dtype(at::kFloat));
+  const OnDevice on(x);
+  done(aqlm_sample(x.data_ptr(), row_stride(x), dtype_of(x, "logits"), rows, x.size(1), (const float*)u, &r,
+                   tokens.data_ptr<int32_t>(), want ? logprob.data_ptr<float>() : nullptr, stream_of(a[7])),
+       "aqlm_sample");
+  return want ? Py_BuildValue("NN", wrap(tokens), wrap(logprob)) : wrap(tokens);
+}
+
 // Whether a stream (its handle) is recording a graph.
 PyObject* capturing(PyObject* const* a) {
   hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
@@ -386,7 +575,9 @@ PyObject* set_check(PyObject* const* a) {
   { #F, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {AQLM_ENTRY(rope, 11),           AQLM_ENTRY(rope_backward, 13),   AQLM_ENTRY(paged_append, 15),
                          AQLM_ENTRY(paged_attention, 14), AQLM_ENTRY(process_logits, 12), AQLM_ENTRY(capturing, 1),
-                         AQLM_ENTRY(set_check, 1),
+                         AQLM_ENTRY(set_check, 1),      AQLM_ENTRY(embed, 5),            AQLM_ENTRY(embed_backward, 7),
+                         AQLM_ENTRY(layer_norm, 9),     AQLM_ENTRY(layer_norm_backward, 9),
+                         AQLM_ENTRY(distill_loss, 9),   AQLM_ENTRY(sample, 8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

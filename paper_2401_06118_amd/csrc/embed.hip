@@ -1,0 +1,292 @@
+// Rows of the embedding table by token, scaled, and the table's gradient.
+//
+//   y[t] = scale E[id_t]                        (ids outside the table: zeros)
+//   dE[v] = scale sum over t with id_t = v of dy[t]
+//
+// Both are bound by memory: the first reads each row that occurs and writes one per token,
+// the second reads a row per token and writes one per token of the vocabulary, zeros for
+// those that do not occur.
+#include "ends.h"
+
+#include "common.h"
+#include "elements.h"
+#include "join.h"
+#include "launch.h"
+
+namespace aqlm {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// A thread: PER pieces of a row, kThreads pieces apart; blocks_per_row workgroups a row.
+template <int TY, int PER, bool NT>
+__global__ void __launch_bounds__(kThreads) k_embed(EmbedArgs a, int blocks_per_row) {
+  typedef typename Elem<TY>::T T;
+  typedef typename Elem<TY>::V V;
+  constexpr int N = kPiece<TY>;
+  for (int64_t b = blockIdx.x; b < a.count * blocks_per_row; b += gridDim.x) {
+    const int64_t t = b / blocks_per_row;
+    const int c0 = ((int)(b - t * blocks_per_row) * PER * kThreads + threadIdx.x) * N;
+    const int id = a.tokens[t];
+    const bool held = (uint32_t)id < (uint32_t)a.vocab;
+    const T* const in = (const T*)a.table + (held ? id : 0) * a.table_row;
+    T* const out = (T*)a.out + t * a.out_row;
+    V v[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int c = c0 + j * kThreads * N;
+      v[j] = held && c < a.dim ? load_piece<TY>(in, c, a.dim) : V(0);
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int c = c0 + j * kThreads * N;
+      if (c >= a.dim) continue;
+      // (a row that is not held is zeros whatever the scale)
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[j][e] = held ? (T)((float)v[j][e] * a.scale) : (T)0.f;
+      store_piece<TY, NT>(out, c, a.dim, v[j]);
+    }
+  }
+}
+
+template <int TY, int PER>
+hipError_t launch_embed_per(const EmbedArgs& a, hipStream_t s) {
+  const int pieces = (a.dim + kPiece<TY> - 1) / kPiece<TY>;
+  const int per_row = (pieces + PER * kThreads - 1) / (PER * kThreads);
+  const int64_t blocks = a.count * per_row;
+  const unsigned grid = (unsigned)(blocks < (1 << 22) ? blocks : (1 << 22));
+  k_embed<TY, PER, false><<<grid, kThreads, 0, s>>>(a, per_row);
+  return hipGetLastError();
+}
+
+template <int TY>
+hipError_t launch_embed_typed(const EmbedArgs& a, hipStream_t s) {
+  return launch_embed_per<TY, 1>(a, s);
+}
+
+// ---------------------------------------------------------------------------
+// Gradient.  One launch sorts the places 0 .. tokens - 1 by token (stable) and writes the
+// zero rows; the next sums each token's rows in the order of its places.
+//
+// Sorting: workgroup b of 2^lg holds the tokens whose low lg bits are b, so that tokens
+// with small numbers, the frequent ones, are spread.  It walks all ids twice: counts (how many
+// belong to earlier workgroups, and for each wave's share of the places how many are
+// each of its own tokens), then writes places.  2^lg x tokens x 4 bytes from the L2s, beside
+// the zero rows' bytes.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr int kSortOwn = 512;  // tokens of a workgroup
+
+template <int TY>
+__global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedGradArgs a, int lg, int64_t counters) {
+  typedef typename Elem<TY>::T T;
+  typedef typename Elem<TY>::V V;
+  constexpr int N = kPiece<TY>;
+  __shared__ int at[kSortWaves][kSortOwn];  // counts, then the next place of a wave's token
+  __shared__ int from[kSortOwn], total[kSortOwn];  // where a token's places begin, how many
+  __shared__ int below[kSortWaves], sums[kSortWaves];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int b = blockIdx.x, own = (a.vocab - b + (1 << lg) - 1) >> lg;  // tokens b, b + 2^lg, ...
+  for (int64_t i = (int64_t)b * kSortThreads + tid; i < counters; i += (int64_t)gridDim.x * kSortThreads) a.counters[i] = 0;
+  for (int i = tid; i < kSortWaves * kSortOwn; i += kSortThreads) (&at[0][0])[i] = 0;
+  __syncthreads();
+  // (shares of whole waves' loads; in 64 bits, as tokens go up to 2^31)
+  const int64_t share = ((int64_t)(a.tokens_count + kSortWaves - 1) / kSortWaves + kWave - 1) / kWave * kWave;
+  const int begin = (int)min((int64_t)a.tokens_count, wave * share);
+  const int end = (int)min((int64_t)a.tokens_count, (wave + 1) * share);
+  // The share's ids, kBatch loads of the wave in flight.
+  constexpr int kBatch = 8;
+  auto walk = [&](auto take) {
+    for (int64_t i0 = begin; i0 < end; i0 += kBatch * kWave) {
+      int id[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int64_t i = i0 + j * kWave + lane;
+        id[j] = i < end ? a.tokens[i] : -1;
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const bool held = (uint32_t)id[j] < (uint32_t)a.vocab;
+        take((int)(i0 + j * kWave + lane), id[j], held, held && (id[j] & ((1 << lg) - 1)) == b);
+      }
+    }
+  };
+  int before = 0;
+  walk([&](int, int id, bool held, bool mine) {
+    before += held && (id & ((1 << lg) - 1)) < b;
+    if (mine) atomicAdd(&at[wave][id >> lg], 1);
+  });
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) before += __shfl_xor(before, s);
+  if (lane == 0) below[wave] = before;
+  __syncthreads();
+  // exclusive sums over the tokens, then over the waves of each
+  int n = 0;
+  if (tid < own) {
+    for (int w = 0; w < kSortWaves; ++w) n += at[w][tid];
+    total[tid] = n;
+  }
+  int incl = n;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) {
+    const int o = __shfl_up(incl, s);
+    if (lane >= s) incl += o;
+  }
+  if (lane == kWave - 1) sums[wave] = incl;
+  __syncthreads();
+  int base = incl - n;
+  for (int w = 0; w < kSortWaves; ++w) base += below[w] + (w < wave ? sums[w] : 0);
+  if (b == (int)gridDim.x - 1 && tid == 0) {
+    int all = 0;
+    for (int w = 0; w < kSortWaves; ++w) all += below[w] + sums[w];
+    *a.held = all;
+  }
+  if (tid < own) {
+    int next = base;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = at[w][tid];
+      at[w][tid] = next;
+      next += c;
+    }
+    from[tid] = base;
+  }
+  __syncthreads();
+  walk([&](int i, int id, bool, bool mine) {
+    for (uint64_t left = __ballot(mine); left != 0;) {
+      const int lead = __builtin_ctzll(left);
+      const int r = __shfl(id, lead) >> lg;
+      const uint64_t same = __ballot(mine && id >> lg == r);
+      const int p = at[wave][r];
+      if (mine && id >> lg == r) {
+        const int place = p + __popcll(same & ((1ull << lane) - 1));
+        a.order[place] = i;
+        a.first[place] = from[r];
+        a.last[place] = from[r] + total[r];
+      }
+      if (lane == lead) at[wave][r] = p + __popcll(same);
+      left &= ~same;
+    }
+  });
+  // rows of tokens that do not occur
+  V zero;
+#pragma unroll
+  for (int e = 0; e < N; ++e) zero[e] = (T)0.f;
+  for (int r = wave; r < own; r += kSortWaves) {
+    if (total[r] != 0) continue;
+    T* const out = (T*)a.out + (((int64_t)r << lg) + b) * a.out_row;
+    for (int c = lane * N; c < a.dim; c += kWave * N) store_piece<TY>(out, c, a.dim, zero);
+  }
+}
+
+// A workgroup: the rows of kEmbedUnit sorted places, in a block of columns (a piece of 16
+// bytes a thread).  Sums of tokens that lie in one unit are written; pieces of those
+// that do not go to memory, and the last workgroup to bring one adds them in the order of
+// the units.
+template <int TY, int OTY>
+__global__ void __launch_bounds__(kThreads) k_embed_sum(EmbedGradArgs a) {
+  typedef typename Elem<TY>::T T;
+  typedef typename Elem<TY>::V V;
+  typedef typename Elem<OTY>::T O;
+  constexpr int N = kPiece<TY>;
+  __shared__ int flag;
+  const int held = *a.held;
+  const int c = (blockIdx.y * kThreads + threadIdx.x) * N;
+  const bool active = c < a.dim;
+  for (int64_t first = (int64_t)blockIdx.x * kEmbedUnit; first < held; first += (int64_t)gridDim.x * kEmbedUnit) {
+    const int p0 = (int)first, unit = p0 / kEmbedUnit, p1 = (int)min(first + kEmbedUnit, (int64_t)held);
+    float sum[N];
+    auto write = [&](int place, const float* s) {
+      if (!active) return;
+      O* const out = (O*)a.out + a.tokens[place] * a.out_row + c;
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (c + e < a.dim) out[e] = (O)(s[e] * a.scale);
+    };
+    auto part = [&](int u, int which) { return a.parts + ((int64_t)u * 2 + which) * a.dim + c; };
+    auto put = [&](int which) {
+      if (!active) return;
+      float* const p = part(unit, which);
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (c + e < a.dim) put_through(p + e, sum[e]);
+    };
+    V v[kEmbedUnit];
+#pragma unroll
+    for (int i = 0; i < kEmbedUnit; ++i) {
+      v[i] = V(0);
+      if (p0 + i < p1 && active) v[i] = load_piece<TY>((const T*)a.dout + a.order[p0 + i] * a.dout_row, c, a.dim);
+    }
+    // what is open at this unit's ends
+    const int head_first = a.first[p0], tail_last = a.last[p1 - 1], tail_first = a.first[p1 - 1];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEmbedUnit; ++i) {
+      if (p0 + i >= p1) break;
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] += (float)v[i][e];
+      const int f = a.first[p0 + i], l = a.last[p0 + i];
+      if (l == p0 + i + 1) {  // the token's last place
+        if (f >= p0) write(a.order[p0 + i], sum);
+        else put(0);
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] = 0.f;
+      }
+    }
+    if (tail_last > p1) put(tail_first < p0 ? 0 : 1);
+    // join: the token that began before this unit, and the one that goes on behind it
+    auto join = [&](int f, int l) {
+      const int u0 = f / kEmbedUnit, u1 = (l - 1) / kEmbedUnit;
+      if (!last_of(a.counters + (int64_t)u0 * gridDim.y + blockIdx.y, u1 - u0 + 1, &flag)) return;
+      if (!active) return;
+      float s[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) s[e] = 0.f;
+      for (int u = u0; u <= u1; ++u) {
+        const float* const p = part(u, u == u0 ? 1 : 0);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (c + e < a.dim) s[e] += get_through(p + e);
+      }
+      write(a.order[f], s);
+    };
+    if (head_first < p0) join(head_first, a.last[p0]);
+    if (tail_last > p1 && tail_first >= p0) join(tail_first, tail_last);
+  }
+}
+
+template <int TY, int OTY>
+hipError_t launch_grad_typed(const EmbedGradArgs& a, hipStream_t s) {
+  int lg = 8;
+  while ((int64_t)kSortOwn << lg < a.vocab) ++lg;
+  const int units = (int)((a.tokens_count + (int64_t)kEmbedUnit - 1) / kEmbedUnit);
+  const int columns = embed_grad_column_blocks(a.dim, TY);
+  k_embed_sort<OTY><<<1u << lg, kSortThreads, 0, s>>>(a, lg, (int64_t)units * columns);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || units == 0) return e;
+  // (a launch has fewer than 2^32 threads)
+  const int grid = min(units, max(1, (1 << 23) / columns));
+  k_embed_sum<TY, OTY><<<dim3((unsigned)grid, (unsigned)columns), kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int embed_grad_column_blocks(int32_t dim, int dtype) {
+  const int columns = kThreads * (dtype == kF32 ? 4 : 8);
+  return (dim + columns - 1) / columns;
+}
+
+hipError_t launch_embed(const EmbedArgs& a, int dtype, hipStream_t s) {
+  if (dtype == kF16) return launch_embed_typed<kF16>(a, s);
+  if (dtype == kBf16) return launch_embed_typed<kBf16>(a, s);
+  return launch_embed_typed<kF32>(a, s);
+}
+
+hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int out_dtype, hipStream_t s) {
+  if (dtype == kF32) return launch_grad_typed<kF32, kF32>(a, s);
+  if (dtype == kF16) return out_dtype == kF16 ? launch_grad_typed<kF16, kF16>(a, s) : launch_grad_typed<kF16, kF32>(a, s);
+  return out_dtype == kBf16 ? launch_grad_typed<kBf16, kBf16>(a, s) : launch_grad_typed<kBf16, kF32>(a, s);
+}
+
+}  // namespace aqlm

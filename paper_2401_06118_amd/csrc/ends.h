@@ -1,0 +1,98 @@
+// The ends of a model and the norms of its residual stream: arguments of the kernels in
+// embed.hip, norm.hip, distill.hip and sample.hip.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace aqlm {
+
+// Row strides in elements.
+struct EmbedArgs {
+  const void* table;
+  void* out;
+  const int32_t* tokens;
+  int64_t table_row, out_row, count;
+  int32_t vocab, dim;
+  float scale;
+};
+
+struct EmbedGradArgs {
+  const void* dout;
+  void* out;
+  const int32_t* tokens;
+  int64_t dout_row, out_row;
+  int32_t tokens_count, vocab, dim;
+  float scale;
+  // workspace
+  uint32_t* counters;  // [units][column blocks]
+  int32_t* held;       // [1] tokens of the vocabulary
+  int32_t* order;      // [tokens] places, those of one token together, ascending
+  int32_t* first;      // [tokens] where the token's places begin in order,
+  int32_t* last;       // [tokens] and end
+  float* parts;        // [units][2][dim]
+};
+
+constexpr int kEmbedUnit = 16;  // places of `order` that a workgroup sums
+int embed_grad_column_blocks(int32_t dim, int dtype);
+
+struct NormArgs {
+  const void *x, *residual, *weight, *bias;
+  void *out, *sum;
+  int64_t x_row, residual_row, out_row, sum_row, rows;
+  int32_t dim;
+  bool rms;
+  float eps;
+};
+
+constexpr int kNormMaxDim = 16384;
+
+struct NormGradArgs {
+  const void *dy, *x, *weight, *dsum;
+  void* out;
+  float *dweight, *dbias;
+  float* parts;  // [slots][dim] for each of dweight and dbias
+  int64_t dy_row, x_row, dsum_row, out_row, rows;
+  int32_t dim;
+  bool rms;
+  float eps;
+};
+
+int norm_grad_slots(int32_t dim);
+
+struct DistillArgs {
+  const void *logits, *teacher;
+  const int32_t* ids;
+  const float *teacher_lse, *weights;
+  float* loss;
+  void* grad;  // or null
+  int64_t logits_row, teacher_row, ids_row, grad_row, rows;
+  int32_t vocab, listed, teacher_dtype;
+  float tau;
+};
+
+constexpr int kDistillMaxListed = 2048;
+constexpr int kDistillMaxVocab = 1 << 19;
+constexpr int64_t kDistillMaxRows = (1 << 22) - 1;  // (a launch has fewer than 2^32 threads)
+
+struct SampleArgs {
+  const void* logits;
+  const float *uniform, *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  int32_t* tokens;
+  float* logprob;  // or null
+  int64_t row;
+  int32_t rows, vocab;
+};
+
+constexpr int kSampleMaxVocab = 1 << 19;
+constexpr int64_t kSampleMaxRows = 1 << 20;
+
+hipError_t launch_embed(const EmbedArgs& a, int dtype, hipStream_t s);
+hipError_t launch_embed_grad(const EmbedGradArgs& a, int dtype, int out_dtype, hipStream_t s);
+hipError_t launch_norm(const NormArgs& a, int dtype, hipStream_t s);
+hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t s);
+hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s);
+hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t s);
+
+}  // namespace aqlm
