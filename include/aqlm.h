@@ -733,11 +733,17 @@ typedef struct aqlm_sampling {
  * the first, in the order of numbers, at which the kept mass exceeds uniform times all kept mass.
  * -inf is a masked token; a row with NaN, or with nothing else than masked tokens, gives -1.
  * logprob (NULL, or [rows]): the logarithm of the token's share of the kept mass (0 at
- * temperature 0, NaN with -1).  Weights are computed in 64 bits and rounded to multiples of
- * 2^-44, sums of them are exact: the same token whatever the batch.  Limits: 2^20 rows,
- * vocab 2^19. */
+ * temperature 0, NaN with -1).  Weights are computed in 64 bits and added as whole multiples of
+ * 2^-44: the same token whatever the batch.
+ *   workspace: aqlm_sample_workspace_bytes() (25 MB), 16-byte aligned, whose first
+ *   AQLM_SAMPLE_COUNTER_BYTES are zero before its first use.  Every launch leaves them zero, so
+ *   one workspace serves any calls on one stream; calls that may overlap need one each.
+ * Limits: 2^20 rows, vocab 2^19. */
+#define AQLM_SAMPLE_COUNTER_BYTES 16384
+size_t aqlm_sample_workspace_bytes(void);
 int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_t rows, int64_t vocab,
-                const float* uniform, const aqlm_sampling* rules, int32_t* tokens, float* logprob, void* stream);
+                const float* uniform, const aqlm_sampling* rules, int32_t* tokens, float* logprob, void* workspace,
+                size_t workspace_bytes, void* stream);
 
 /* Static text for a status code (never NULL). */
 const char* aqlm_status_string(int status);

@@ -83,8 +83,17 @@ struct SampleArgs {
   float* logprob;  // or null
   int64_t row;
   int32_t rows, vocab;
+  // workspace, of kSampleSlices slices
+  uint32_t* counters;  // [rows of a launch]
+  uint64_t* records;   // [slices][2]
+  uint64_t* masses;    // [slices][512]
+  uint32_t* counts;    // [slices][512]
 };
 
+constexpr int kSampleSlice = 8192;  // logits of a workgroup
+constexpr int kSampleSlices = 4096;  // of a launch
+constexpr size_t kSampleCounterBytes = kSampleSlices * 4, kSampleRecordBytes = kSampleSlices * 16,
+                 kSampleMassBytes = kSampleSlices * size_t(512) * 8, kSampleCountBytes = kSampleSlices * size_t(512) * 4;
 constexpr int kSampleMaxVocab = 1 << 19;
 constexpr int64_t kSampleMaxRows = 1 << 20;
 

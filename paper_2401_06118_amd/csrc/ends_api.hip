@@ -13,6 +13,8 @@
 
 namespace {
 
+static_assert(aqlm::kSampleCounterBytes == AQLM_SAMPLE_COUNTER_BYTES, "counters");
+
 constexpr int64_t k2G = int64_t(1) << 31;
 constexpr int64_t kMaxTokens = k2G - 65536;  // (places are held in 32 bits on the device)
 constexpr int64_t kMaxTable = int64_t(1) << 30;
@@ -224,15 +226,21 @@ int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, 
   return status_of(aqlm::launch_distill(a, dtype, (hipStream_t)stream));
 }
 
+size_t aqlm_sample_workspace_bytes(void) {
+  return aqlm::kSampleCounterBytes + aqlm::kSampleRecordBytes + aqlm::kSampleMassBytes + aqlm::kSampleCountBytes;
+}
+
 int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_t rows, int64_t vocab,
-                const float* uniform, const aqlm_sampling* r, int32_t* tokens, float* logprob, void* stream) {
+                const float* uniform, const aqlm_sampling* r, int32_t* tokens, float* logprob, void* workspace,
+                size_t workspace_bytes, void* stream) {
   if (!r) return AQLM_ERR_NULL;
   if (!known_dtype(dtype)) return AQLM_ERR_UNSUPPORTED;
   if (rows < 0 || rows > aqlm::kSampleMaxRows || vocab <= 0 || vocab > aqlm::kSampleMaxVocab || !rows_in(logits_stride))
     return AQLM_ERR_SHAPE;
   if (rows == 0) return AQLM_OK;
-  if (!logits || !uniform || !tokens) return AQLM_ERR_NULL;
-  if (!element_aligned(logits, dtype)) return AQLM_ERR_ALIGN;
+  if (!logits || !uniform || !tokens || !workspace) return AQLM_ERR_NULL;
+  if (!element_aligned(logits, dtype) || !multiple(workspace, 16)) return AQLM_ERR_ALIGN;
+  if (workspace_bytes < aqlm_sample_workspace_bytes()) return AQLM_ERR_WORKSPACE;
   for (const void* p : {(const void*)uniform, (const void*)r->temperature, (const void*)r->top_k, (const void*)r->top_p,
                         (const void*)r->min_p, (const void*)tokens, (const void*)logprob})
     if (!multiple(p, 4)) return AQLM_ERR_ALIGN;
@@ -248,6 +256,12 @@ int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_
   a.row = logits_stride;
   a.rows = (int32_t)rows;
   a.vocab = (int32_t)vocab;
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
+  a.counters = reinterpret_cast<uint32_t*>(ws);
+  a.records = reinterpret_cast<uint64_t*>(ws + aqlm::kSampleCounterBytes);
+  a.masses = reinterpret_cast<uint64_t*>(ws + aqlm::kSampleCounterBytes + aqlm::kSampleRecordBytes);
+  a.counts = reinterpret_cast<uint32_t*>(ws + aqlm::kSampleCounterBytes + aqlm::kSampleRecordBytes +
+                                         aqlm::kSampleMassBytes);
   return status_of(aqlm::launch_sample(a, dtype, (hipStream_t)stream));
 }
 

@@ -107,14 +107,18 @@ def test_distill_loss(lib):
 
 
 def test_sample(lib):
-    def call(z=P, zs=1000, dtype=F16, rows=3, vocab=1000, u=P, r=(None, None, None, None), tokens=P, lp=None):
-        r = None if r is None else ctypes.byref(_lib.Sampling(*r))
-        return lib.aqlm_sample(z, zs, dtype, rows, vocab, u, r, tokens, lp, None)
+    need = lib.aqlm_sample_workspace_bytes()
 
-    refused(call, NULL, z=[None], u=[None], r=[None], tokens=[None])
+    def call(z=P, zs=1000, dtype=F16, rows=3, vocab=1000, u=P, r=(None, None, None, None), tokens=P, lp=None, ws=P,
+             size=need):
+        r = None if r is None else ctypes.byref(_lib.Sampling(*r))
+        return lib.aqlm_sample(z, zs, dtype, rows, vocab, u, r, tokens, lp, ws, size, None)
+
+    refused(call, NULL, z=[None], u=[None], r=[None], tokens=[None], ws=[None])
+    refused(call, WORKSPACE, size=[0, need - 1])
     refused(call, SHAPE, zs=[-1], rows=[-1, (1 << 20) + 1], vocab=[0, -1, (1 << 19) + 1, BIG])
     refused(call, UNSUP, dtype=[3])
-    refused(call, ALIGN, z=[P + 1], u=[P + 2], tokens=[P + 1], lp=[P + 2],
+    refused(call, ALIGN, z=[P + 1], u=[P + 2], tokens=[P + 1], lp=[P + 2], ws=[P + 8],
             r=[(P + 1, None, None, None), (None, P + 1, None, None), (None, None, P + 1, None), (None, None, None, P + 1)])
     assert call(rows=0, z=None) == OK
 
