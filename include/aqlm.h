@@ -735,12 +735,10 @@ typedef struct aqlm_sampling {
  * logprob (NULL, or [rows]): the logarithm of the token's share of the kept mass (0 at
  * temperature 0, NaN with -1).  Weights are computed in 64 bits and added as whole multiples of
  * 2^-44: the same token whatever the batch.
- *   workspace: aqlm_sample_workspace_bytes() (25 MB), 16-byte aligned, whose first
- *   AQLM_SAMPLE_COUNTER_BYTES are zero before its first use.  Every launch leaves them zero, so
- *   one workspace serves any calls on one stream; calls that may overlap need one each.
+ *   workspace: aqlm_sample_workspace_bytes(rows, vocab, rules) bytes, 16-byte aligned, any
+ *   contents (0, and not read, up to a vocab of 8192, or of 32768 with top_k).
  * Limits: 2^20 rows, vocab 2^19. */
-#define AQLM_SAMPLE_COUNTER_BYTES 16384
-size_t aqlm_sample_workspace_bytes(void);
+size_t aqlm_sample_workspace_bytes(int64_t rows, int64_t vocab, const aqlm_sampling* rules);
 int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_t rows, int64_t vocab,
                 const float* uniform, const aqlm_sampling* rules, int32_t* tokens, float* logprob, void* workspace,
                 size_t workspace_bytes, void* stream);

@@ -505,4 +505,4 @@ def gemv_sorted_grouped(problems, *, workspace=None, stream=None):
 from .block import (  # noqa: E402,F401  (after the helpers it uses)
     attention_workspace, paged_append, paged_attention, process_logits, rope, rope_backward, rotary_table)
 from .ends import (  # noqa: E402,F401
-    distill_loss, embed, embed_backward, layer_norm, layer_norm_backward, sample, sample_workspace)
+    distill_loss, embed, embed_backward, layer_norm, layer_norm_backward, sample)

@@ -532,7 +532,7 @@ PyObject* distill_loss(PyObject* const* a) {
   return Py_BuildValue("NN", wrap(loss), want ? wrap(grad) : none());
 }
 
-// logits, uniform, temperature, top_k, top_p, min_p, return_logprob, workspace, stream
+// logits, uniform, temperature, top_k, top_p, min_p, return_logprob, stream; the last of the results is the workspace
 PyObject* sample(PyObject* const* a) {
   const at::Tensor& x = rows2(a[0], "logits");
   const int64_t rows = x.size(0);
@@ -545,19 +545,19 @@ PyObject* sample(PyObject* const* a) {
   r.top_k = (const int32_t*)rule(3, "top_k", at::kInt);
   r.top_p = (const float*)rule(4, "top_p", at::kFloat);
   r.min_p = (const float*)rule(5, "min_p", at::kFloat);
-  const at::Tensor& ws = tensor(a[7], "workspace");
-  if (!ws.is_cuda() || ws.device() != x.device() || !ws.is_contiguous())
-    refuse("workspace must be a contiguous GPU tensor on the device of logits");
   const bool want = truth(a[6]);
   const at::Tensor tokens = at::empty({rows}, x.options().dtype(at::kInt));
   at::Tensor logprob;
   if (want) logprob = at::empty({rows}, x.options().dtype(at::kFloat));
+  const size_t bytes = aqlm_sample_workspace_bytes(rows, x.size(1), &r);
+  at::Tensor ws;
+  if (bytes) ws = at::empty({(int64_t)bytes}, x.options().dtype(at::kByte));
   const OnDevice on(x);
   done(aqlm_sample(x.data_ptr(), row_stride(x), dtype_of(x, "logits"), rows, x.size(1), (const float*)u, &r,
-                   tokens.data_ptr<int32_t>(), want ? logprob.data_ptr<float>() : nullptr, ws.data_ptr(), ws.nbytes(),
-                   stream_of(a[8])),
+                   tokens.data_ptr<int32_t>(), want ? logprob.data_ptr<float>() : nullptr, bytes ? ws.data_ptr() : nullptr,
+                   bytes, stream_of(a[7])),
        "aqlm_sample");
-  return want ? Py_BuildValue("NN", wrap(tokens), wrap(logprob)) : wrap(tokens);
+  return Py_BuildValue("NNN", wrap(tokens), want ? wrap(logprob) : none(), bytes ? wrap(ws) : none());
 }
 
 // Whether a stream (its handle) is recording a graph.
@@ -581,7 +581,7 @@ PyMethodDef methods[] = {AQLM_ENTRY(rope, 11),           AQLM_ENTRY(rope_backwar
                          AQLM_ENTRY(paged_attention, 14), AQLM_ENTRY(process_logits, 12), AQLM_ENTRY(capturing, 1),
                          AQLM_ENTRY(set_check, 1),      AQLM_ENTRY(embed, 5),            AQLM_ENTRY(embed_backward, 7),
                          AQLM_ENTRY(layer_norm, 9),     AQLM_ENTRY(layer_norm_backward, 9),
-                         AQLM_ENTRY(distill_loss, 9),   AQLM_ENTRY(sample, 9),
+                         AQLM_ENTRY(distill_loss, 9),   AQLM_ENTRY(sample, 8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

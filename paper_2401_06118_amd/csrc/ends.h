@@ -83,17 +83,29 @@ struct SampleArgs {
   float* logprob;  // or null
   int64_t row;
   int32_t rows, vocab;
-  // workspace, of kSampleSlices slices
-  uint32_t* counters;  // [rows of a launch]
-  uint64_t* records;   // [slices][2]
-  uint64_t* masses;    // [slices][512]
-  uint32_t* counts;    // [slices][512]
+  // workspace, where a row is cut: [slices of a launch]
+  struct SampleRecord* records;
+  uint64_t* masses;  // [][kSampleBins]
+  uint32_t* counts;  // [][kSampleBins]
+  uint64_t* lists;   // [][kSampleListed]
 };
 
-constexpr int kSampleSlice = 8192;  // logits of a workgroup
-constexpr int kSampleSlices = 4096;  // of a launch
-constexpr size_t kSampleCounterBytes = kSampleSlices * 4, kSampleRecordBytes = kSampleSlices * 16,
-                 kSampleMassBytes = kSampleSlices * size_t(512) * 8, kSampleCountBytes = kSampleSlices * size_t(512) * 4;
+// What a slice of a row holds.
+struct SampleRecord {
+  uint64_t mass;  // relative to its largest weight; where the largest is drawn: its first place
+  float top;      // largest logit, or NaN
+  int32_t cut;    // the list has all tokens of the bins up to this one
+  int32_t listed;
+  int32_t pad;
+};
+
+constexpr int kSampleRow = 32768;    // logits of a row that a workgroup holds at most
+constexpr int kSampleSlice = 8192;   // logits of a slice
+// Whether rows are cut into slices.
+inline bool sample_cut(int64_t vocab, bool top_k) { return vocab > (top_k ? kSampleRow : kSampleSlice); }
+constexpr int kSampleSlices = 4096;  // slices of a launch
+constexpr int kSampleBins = 512, kSampleListed = 512;
+constexpr size_t kSampleSliceBytes = sizeof(SampleRecord) + kSampleBins * 12 + kSampleListed * 8;
 constexpr int kSampleMaxVocab = 1 << 19;
 constexpr int64_t kSampleMaxRows = 1 << 20;
 

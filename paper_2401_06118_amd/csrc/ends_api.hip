@@ -3,6 +3,7 @@
 // any launch; on an error nothing is launched.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -12,8 +13,6 @@
 #include "rope.h"
 
 namespace {
-
-static_assert(aqlm::kSampleCounterBytes == AQLM_SAMPLE_COUNTER_BYTES, "counters");
 
 constexpr int64_t k2G = int64_t(1) << 31;
 constexpr int64_t kMaxTokens = k2G - 65536;  // (places are held in 32 bits on the device)
@@ -46,6 +45,12 @@ EmbedWorkspace embed_workspace(int64_t count, int64_t dim, int32_t dtype) {
   w.parts = w.last + places;
   w.bytes = w.parts + units * 2 * (size_t)dim * 4;
   return w;
+}
+
+// Slices of a launch over rows that are cut.
+int64_t sample_slices(int64_t rows, int64_t vocab) {
+  const int64_t slices = (vocab + aqlm::kSampleSlice - 1) / aqlm::kSampleSlice;
+  return std::min(rows, aqlm::kSampleSlices / slices) * slices;
 }
 
 bool embed_sizes(int64_t count, int64_t vocab, int64_t dim) {
@@ -226,8 +231,10 @@ int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, 
   return status_of(aqlm::launch_distill(a, dtype, (hipStream_t)stream));
 }
 
-size_t aqlm_sample_workspace_bytes(void) {
-  return aqlm::kSampleCounterBytes + aqlm::kSampleRecordBytes + aqlm::kSampleMassBytes + aqlm::kSampleCountBytes;
+size_t aqlm_sample_workspace_bytes(int64_t rows, int64_t vocab, const aqlm_sampling* r) {
+  if (rows <= 0 || vocab <= 0 || vocab > aqlm::kSampleMaxVocab || !r || !aqlm::sample_cut(vocab, r->top_k != nullptr))
+    return 0;
+  return (size_t)sample_slices(rows, vocab) * aqlm::kSampleSliceBytes;
 }
 
 int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_t rows, int64_t vocab,
@@ -238,9 +245,10 @@ int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_
   if (rows < 0 || rows > aqlm::kSampleMaxRows || vocab <= 0 || vocab > aqlm::kSampleMaxVocab || !rows_in(logits_stride))
     return AQLM_ERR_SHAPE;
   if (rows == 0) return AQLM_OK;
-  if (!logits || !uniform || !tokens || !workspace) return AQLM_ERR_NULL;
-  if (!element_aligned(logits, dtype) || !multiple(workspace, 16)) return AQLM_ERR_ALIGN;
-  if (workspace_bytes < aqlm_sample_workspace_bytes()) return AQLM_ERR_WORKSPACE;
+  const size_t need = aqlm_sample_workspace_bytes(rows, vocab, r);
+  if (!logits || !uniform || !tokens || (need > 0 && !workspace)) return AQLM_ERR_NULL;
+  if (!element_aligned(logits, dtype) || (need > 0 && !multiple(workspace, 16))) return AQLM_ERR_ALIGN;
+  if (workspace_bytes < need) return AQLM_ERR_WORKSPACE;
   for (const void* p : {(const void*)uniform, (const void*)r->temperature, (const void*)r->top_k, (const void*)r->top_p,
                         (const void*)r->min_p, (const void*)tokens, (const void*)logprob})
     if (!multiple(p, 4)) return AQLM_ERR_ALIGN;
@@ -256,12 +264,14 @@ int aqlm_sample(const void* logits, int64_t logits_stride, int32_t dtype, int64_
   a.row = logits_stride;
   a.rows = (int32_t)rows;
   a.vocab = (int32_t)vocab;
-  uint8_t* const ws = static_cast<uint8_t*>(workspace);
-  a.counters = reinterpret_cast<uint32_t*>(ws);
-  a.records = reinterpret_cast<uint64_t*>(ws + aqlm::kSampleCounterBytes);
-  a.masses = reinterpret_cast<uint64_t*>(ws + aqlm::kSampleCounterBytes + aqlm::kSampleRecordBytes);
-  a.counts = reinterpret_cast<uint32_t*>(ws + aqlm::kSampleCounterBytes + aqlm::kSampleRecordBytes +
-                                         aqlm::kSampleMassBytes);
+  if (need > 0) {
+    const size_t n = (size_t)sample_slices(rows, vocab);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.records = reinterpret_cast<aqlm::SampleRecord*>(ws);
+    a.masses = reinterpret_cast<uint64_t*>(ws += n * sizeof(aqlm::SampleRecord));
+    a.lists = reinterpret_cast<uint64_t*>(ws += n * aqlm::kSampleBins * 8);
+    a.counts = reinterpret_cast<uint32_t*>(ws + n * aqlm::kSampleListed * 8);
+  }
   return status_of(aqlm::launch_sample(a, dtype, (hipStream_t)stream));
 }
 

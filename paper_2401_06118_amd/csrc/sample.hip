@@ -12,17 +12,19 @@
 // token does not depend on an order of sums, and differs from that of real numbers
 // only where u is within about 2^-40 of a border.
 //
-// A workgroup takes a slice of 8192 logits and holds it in registers: its maximum, and
-// relative to that counts and masses by bins of 1/16 of T (512 of them: what is lower has
-// no mass left).  The last workgroup of a row joins the slices', finds the bin in which the
-// last member lies, collects the tokens down to it from the row (or, if those are more
-// than the list holds, that bin's), sorts them, and draws.  What the list does
-// not hold (thousands of equal logits) is found by eleven bits of logit and number at a time.
+// Counts and masses of the tokens by bins of T / 16 (512 of them: what is lower has no mass
+// left) show in which bin the last member lies.  The tokens down to it (or, if those are more
+// than a list holds, that bin's) are collected and sorted; the kept ones are the first of
+// them.  What the list does not hold either (thousands of equal logits) is found by
+// eleven bits of logit and number at a time (draw_slowly).
+//
+// Rows of up to 32768 logits are a workgroup's each, which holds them in registers.  Longer
+// ones are cut into slices of 8192: one launch makes the slices' maxima, bins (relative to
+// their own maximum) and lists of their first tokens, another joins a row's.
 #include "ends.h"
 
 #include "common.h"
 #include "elements.h"
-#include "join.h"
 #include "launch.h"
 #include "lds_sync.h"
 
@@ -30,15 +32,16 @@ namespace aqlm {
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / kWave;
-constexpr int kBins = 512;    // of a slice, one a thread
-constexpr int kList = 2048;   // tokens that are sorted
-constexpr int kMostK = 1024;  // up to this top-k bins need no masses: the list holds all that count
-constexpr int kDigit = 2048;  // bins of the search by bits
+constexpr int kBins = kSampleBins;
+constexpr int kList = 2048;      // tokens that are sorted
+constexpr int kFew = 256;        // tokens that are compared with one another, without sorting
+constexpr int kMostK = 256;      // up to this top-k bins need no masses: the lists hold all that count
+constexpr int kDigit = 2048;     // bins of the search by bits
 constexpr int kSegments = 2048;  // of a row: 64 pieces of 16 bytes each
-static_assert(kBins == kThreads, "a thread has a bin");
+constexpr int kSliceThreads = 512, kJoinThreads = 512, kRowThreads = 512;
 static_assert(kSampleMaxVocab <= kSegments * kWave * 4, "segments");
 static_assert(kSampleMaxVocab <= kSampleSlice * kWave, "a wave has a row's slices");
+static_assert(kMostK <= kSampleListed, "a slice lists the first k");
 
 // The rules of a row and its largest logit.
 struct Rules {
@@ -77,17 +80,16 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
 }
 __device__ __forceinline__ uint64_t place_of(float l, int i) { return (uint64_t)key_of(l) << 32 | (uint32_t)i; }
 
-__device__ __forceinline__ int bin_of(float l, float c) {
-  return (int)floorf(fminf(fmaxf(l * c, -0x1p30f), 0x1p30f));
-}
+// (The largest of a row is below 2^29 in size, or bins are not used: has_bins.)
+__device__ __forceinline__ int bin_of(float l, float c) { return (int)floorf(fminf(fmaxf(l * c, -0x1p30f), 0x1p30f)); }
+__device__ __forceinline__ int low_bin_of(float l, float c) { return (int)floorf(fmaxf(l * c, -0x1p30f)); }
 
-// 2^44 exp((l - max) / T), rounded.  2^f for |f| <= 1/2 is the exponential series up to the
-// 11th power of f log 2 (the next is below 2^-47).
+// 2^44 exp((l - max) / T), rounded; 0 for masked ones.  2^f for |f| <= 1/2 is the exponential
+// series up to the 11th power of f log 2 (the next is below 2^-47).  Without branches, so
+// that several are computed at a time: one after another is one chain of 64-bit operations.
 __device__ __forceinline__ uint64_t weight_of(const Rules& r, float l) {
-  if (l == r.max_f) return 1ull << 44;  // (infinite ones too)
-  const double y = ((double)l - r.max) * r.inv;
-  if (!(y > -46.0)) return 0;
-  const double n = __builtin_rint(y), f = (y - n) * 0.69314718055994530942;
+  const double d = l == r.max_f ? 0.0 : (double)l - r.max;  // (infinite ones too)
+  const double y = fmax(d * r.inv, -60.0), n = __builtin_rint(y), f = (y - n) * 0.69314718055994530942;
   double e = 1.0 / 39916800.0;
   e = e * f + 1.0 / 3628800.0;
   e = e * f + 1.0 / 362880.0;
@@ -105,40 +107,43 @@ __device__ __forceinline__ uint64_t weight_of(const Rules& r, float l) {
   return __builtin_bit_cast(uint64_t, whole) & 0xFFFFFFFFFFFFFull;
 }
 
-
 // 2^y for y <= 0.
 __device__ __forceinline__ double factor(double y) { return y > -1000.0 ? exp2(y) : 0.0; }
 
-struct Search {
-  uint64_t mass[kDigit];  // of bins; then of segments
-  uint32_t count[kDigit];
-};
-struct Joined {
-  double factor[kWave];  // of a slice's masses
-  uint64_t mass[kWave];  // of a slice
-  int32_t offset[kWave];  // of its bins
-  uint64_t list[kList];
-};
 struct Shared {
   union {
-    Search search;
-    Joined joined;
     struct {
-      uint64_t mass[kBins];
+      uint64_t mass[kDigit];  // of bins; then of segments
+      uint32_t count[kDigit];
+    } search;
+    struct {
+      uint64_t list[kList];
+      uint64_t mass[kBins];  // by bin, the largest logits' first
       uint32_t count[kBins];
-    } slice;
+    };
   };
-  uint64_t wave_mass[kWaves];
-  uint32_t wave_count[kWaves];
-  uint64_t waves[4][kWaves];
+  uint64_t wave_mass[16];
+  uint32_t wave_count[16];
+  uint64_t parts[2 * kWave];
+  uint64_t weight[kFew];
+  uint64_t few[2][kFew / kWave];
+  double factor[kWave];   // of a slice's masses
+  uint64_t slice[kWave];  // kept mass of a slice
   uint64_t found_mass;
-  uint32_t found_count;
-  int32_t found;
-  int32_t flag;
-  float top[kWaves];
+  uint32_t found_count, found_in;
+  int32_t found, listing;
+  float top[16];
 };
 
+__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }  // (NaN stays)
+__device__ __forceinline__ float wave_largest(float v) {
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) v = larger(v, __shfl_xor(v, s));
+  return v;
+}
+
 // Sums of what the threads before this one have, over the workgroup.
+template <int THREADS>
 __device__ __forceinline__ void sums_before(Shared& sh, uint64_t& m, uint32_t& c) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   uint64_t im = m;
@@ -159,11 +164,27 @@ __device__ __forceinline__ void sums_before(Shared& sh, uint64_t& m, uint32_t& c
   lds_barrier();
   m = im - m;
   c = ic - c;
-  for (int w = 0; w < wave; ++w) {
-    m += sh.wave_mass[w];
-    c += sh.wave_count[w];
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave - 1; ++w) {  // (all loads at once)
+    const uint64_t om = sh.wave_mass[w];
+    const uint32_t oc = sh.wave_count[w];
+    m += w < wave ? om : 0;
+    c += w < wave ? oc : 0;
   }
   lds_barrier();
+}
+
+// The sum over the workgroup, in every thread.
+template <int THREADS>
+__device__ __forceinline__ uint64_t sum_all(Shared& sh, uint64_t m) {
+  m = wave_sum64(m);
+  if (threadIdx.x % kWave == 0) sh.wave_mass[threadIdx.x / kWave] = m;
+  lds_barrier();
+  m = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) m += sh.wave_mass[w];
+  lds_barrier();
+  return m;
 }
 
 __device__ __forceinline__ uint64_t wave_before(uint64_t v) {
@@ -190,27 +211,50 @@ __device__ __forceinline__ void finish(const SampleArgs& a, int b, const Rules& 
     a.logprob[b] = (float)((l == r.max_f ? 0.0 : ((double)l - r.max) / r.t) - log((double)total * 0x1p-44));
 }
 
-// Calls f(number, logit) for every token of the row that is not masked.
-template <int TY, typename F>
-__device__ __forceinline__ void each(const void* row, int vocab, F f) {
-  constexpr int N = kPiece<TY>;
-  for (int i = threadIdx.x * N; i < vocab; i += kThreads * N) {
-    const typename Elem<TY>::V v = load_piece<TY>(row, i, vocab);
+// The sum over the threads of the first n, n <= kFew, in every one of the workgroup.  `turn`: which of two places.
+__device__ __forceinline__ uint64_t sum_few(Shared& sh, int turn, uint64_t m, int n) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  if (wave < kFew / kWave) {
+    if (wave * kWave < n) m = wave_sum64(m);
+    if (lane == 0) sh.few[turn][wave] = wave * kWave < n ? m : 0;
+  }
+  lds_barrier();
+  m = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      float l = (float)v[e];
-      asm volatile("" : "+v"(l));  // (one after another: all at once would take too many registers)
-      if (i + e < vocab && l != -INFINITY) f(i + e, l);
+  for (int w = 0; w < kFew / kWave; ++w) m += sh.few[turn][w];
+  return m;
+}
+
+// Calls f(number, logit) for every token of the row that is not masked.
+template <int TY, int THREADS, typename F>
+__device__ __forceinline__ void each(const void* row, int vocab, F f) {
+  constexpr int N = kPiece<TY>, kBatch = 8;  // loads in flight
+  for (int i0 = threadIdx.x * N; i0 < vocab; i0 += kBatch * THREADS * N) {
+    typename Elem<TY>::V v[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i0 + j * THREADS * N;
+      if (i < vocab) v[j] = load_piece<TY>(row, i, vocab);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i0 + j * THREADS * N;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        float l = (float)v[j][e];
+        asm volatile("" : "+v"(l));  // (one after another: all at once would take too many registers)
+        if (i + e < vocab && l != -INFINITY) f(i + e, l);
+      }
     }
   }
 }
 
 // The place of the last of the order's tokens up to `most` of them (by_count) or until they
 // have `mass`; kept_mass: its own and all before it.
-template <int TY>
+template <int TY, int THREADS>
 __device__ __forceinline__ uint64_t last_kept(Shared& sh, const Rules& r, const void* row, int vocab, bool by_count, uint32_t most,
                               double mass, uint64_t& kept_mass) {
-  constexpr int kEach = kDigit / kThreads;
+  constexpr int kEach = kDigit / THREADS;
   const int tid = threadIdx.x;
   uint64_t prefix = 0, above_mass = 0;
   uint32_t above = 0;
@@ -220,13 +264,13 @@ __device__ __forceinline__ uint64_t last_kept(Shared& sh, const Rules& r, const 
     const int shift = d == 0 ? 53 : d == 1 ? 42 : d == 2 ? 32 : d == 3 ? 10 : 0;
     const int top = d == 0 ? 64 : d == 1 ? 53 : d == 2 ? 42 : d == 3 ? 32 : 10;
     const int mask = d < 2 ? 2047 : 1023;
-    for (int i = tid; i < kDigit; i += kThreads) {
+    for (int i = tid; i < kDigit; i += THREADS) {
       sh.search.mass[i] = 0;
       sh.search.count[i] = 0;
     }
     if (tid == 0) sh.found = -1;
     lds_barrier();
-    each<TY>(row, vocab, [&](int i, float l) {
+    each<TY, THREADS>(row, vocab, [&](int i, float l) {
       const uint64_t at = place_of(l, i);
       if (d != 0 && at >> top != prefix >> top) return;
       const int bin = (int)(at >> shift) & mask;
@@ -240,7 +284,7 @@ __device__ __forceinline__ uint64_t last_kept(Shared& sh, const Rules& r, const 
       m += sh.search.mass[kEach * tid + j];
       c += sh.search.count[kEach * tid + j];
     }
-    sums_before(sh, m, c);
+    sums_before<THREADS>(sh, m, c);
     m += above_mass;
     c += above;
     // the last bin with a token before which the limit is not reached
@@ -274,26 +318,22 @@ __device__ __forceinline__ uint64_t last_kept(Shared& sh, const Rules& r, const 
 }
 
 // Everything from the row itself, whatever it holds.
-template <int TY>
+template <int TY, int THREADS>
 __device__ __forceinline__ void draw_slowly(Shared& sh, const SampleArgs& a, int b, const Rules& r) {
-  constexpr int N = kPiece<TY>, kEach = kSegments / kThreads;
+  constexpr int N = kPiece<TY>, kEach = kSegments / THREADS;
   typedef typename Elem<TY>::T T;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const T* const row = (const T*)a.logits + b * a.row;
   uint64_t last = ~0ull, kept = 0;
   lds_barrier();
-  if (r.k > 0) last = last_kept<TY>(sh, r, row, a.vocab, true, (uint32_t)r.k, 0.0, kept);
+  if (r.k > 0) last = last_kept<TY, THREADS>(sh, r, row, a.vocab, true, (uint32_t)r.k, 0.0, kept);
   if (r.top_p) {
     if (last == ~0ull) {
       uint64_t m = 0;
-      each<TY>(row, a.vocab, [&](int, float l) { m += weight_of(r, l); });
-      m = wave_sum64(m);
-      if (lane == 0) sh.wave_mass[wave] = m;
-      lds_barrier();
-      for (int w = 0; w < kWaves; ++w) kept += sh.wave_mass[w];
-      lds_barrier();
+      each<TY, THREADS>(row, a.vocab, [&](int, float l) { m += weight_of(r, l); });
+      kept = sum_all<THREADS>(sh, m);
     }
-    const uint64_t q = last_kept<TY>(sh, r, row, a.vocab, false, 0, fmax(r.p * (double)kept, 1.0), kept);
+    const uint64_t q = last_kept<TY, THREADS>(sh, r, row, a.vocab, false, 0, fmax(r.p * (double)kept, 1.0), kept);
     last = q < last ? q : last;
   }
   auto weight = [&](int i, float l) -> uint64_t {
@@ -302,7 +342,7 @@ __device__ __forceinline__ void draw_slowly(Shared& sh, const SampleArgs& a, int
   };
   // kept mass of each segment of 64 pieces
   const int segments = (a.vocab + kWave * N - 1) / (kWave * N);
-  for (int g = wave; g < segments; g += kWaves) {
+  for (int g = wave; g < segments; g += THREADS / kWave) {
     const int i = (g * kWave + lane) * N;
     uint64_t m = 0;
     if (i < a.vocab) {
@@ -313,14 +353,14 @@ __device__ __forceinline__ void draw_slowly(Shared& sh, const SampleArgs& a, int
     m = wave_sum64(m);
     if (lane == 0) sh.search.mass[g] = m;
   }
-  for (int g = segments + tid; g < kSegments; g += kThreads) sh.search.mass[g] = 0;
+  for (int g = segments + tid; g < kSegments; g += THREADS) sh.search.mass[g] = 0;
   lds_barrier();
   uint64_t m = 0;
   uint32_t none = 0;
   for (int j = 0; j < kEach; ++j) m += sh.search.mass[kEach * tid + j];
   const uint64_t mine = m;
-  sums_before(sh, m, none);
-  if (tid == kThreads - 1) sh.found_mass = m + mine;
+  sums_before<THREADS>(sh, m, none);
+  if (tid == THREADS - 1) sh.found_mass = m + mine;
   lds_barrier();
   const uint64_t total = sh.found_mass, target = target_of(a.uniform[b], total);
   lds_barrier();
@@ -359,419 +399,811 @@ __device__ __forceinline__ void draw_slowly(Shared& sh, const SampleArgs& a, int
   if (found >= 0) finish(a, b, r, found, found_l, total);
 }
 
-// One workgroup a slice; the last of a row goes on with it.
-template <int TY>
-__global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
-  constexpr int N = kPiece<TY>, PER = kSampleSlice / (kThreads * N);
-  typedef typename Elem<TY>::T T;
-  typedef typename Elem<TY>::V V;
-  __shared__ Shared sh;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int b = blockIdx.y, slices = gridDim.x, slice = blockIdx.x;
-  const T* const row = (const T*)a.logits + b * a.row;
-  // (rows of a launch have a workspace each)
-  uint64_t* const records = a.records + (int64_t)b * slices * 2;
-  uint64_t* const masses = a.masses + (int64_t)b * slices * kBins;
-  uint32_t* const counts = a.counts + (int64_t)b * slices * kBins;
-  float x[PER][N];
-  {
-    V v[PER];
+// What is kept of a row: logits above l, and l itself up to number i.
+struct Edge {
+  float l;
+  int i;
+  int bin;
+  float high, upper;  // l c: the upper ends of what the list holds and of its bin
+};
+enum Outcome { kDrawn, kKnown, kUnknown };
+
+// The bins: in whole numbers of l c below the largest's, or (fine) the 512 parts of one of them.
+struct Bins {
+  int top;  // of the largest
+  bool fine;
+  float low;  // fine: the lower end
+  __device__ int at(float f) const { return fine ? kBins - 1 - (int)((f - low) * kBins) : top - (int)floorf(f); }
+  __device__ float lower(int bin) const { return fine ? low + (float)(kBins - 1 - bin) / kBins : (float)(top - bin); }
+  __device__ float upper(int bin) const { return lower(bin) + (fine ? 1.f / kBins : 1.f); }
+  __device__ int last() const { return fine ? kBins - 1 : kBins - 2; }
+};
+
+// The edge's bin by one wave, eight bins a lane, from sh.mass and sh.count, and what lies before them:
+// sh.found, that bin, sh.found_in, what it has, and the sums before it; sh.listing: the list's fill.
+__device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_count, bool whole, double most,
+                                          const Bins& bins, uint64_t mass_before, uint32_t count_before) {
+  constexpr int kEach = kBins / kWave;
+  const int lane = threadIdx.x;
+  uint64_t mass[kEach], m = 0;
+  uint32_t count[kEach], c = 0;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int i = slice * kSampleSlice + (j * kThreads + tid) * N;
-      if (i + N <= a.vocab) v[j] = *(const V*)(row + i);
-      else {
+  for (int j = 0; j < kEach; ++j) {
+    mass[j] = by_count ? 0 : sh.mass[lane * kEach + j];
+    count[j] = sh.count[lane * kEach + j];
+    m += mass[j];
+    c += count[j];
+  }
+  mass_before += wave_before(m);
+  uint32_t incl = c;
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[j][e] = i + e < a.vocab ? row[i + e] : (T)-INFINITY;
+  for (int s = 1; s < kWave; s <<= 1) {
+    const uint32_t o = __shfl_up(incl, s);
+    if (lane >= s) incl += o;
+  }
+  count_before += incl - c;
+  int mine = bins.last();  // at most: the first bin in which a rule's limit lies
+  if (r.min_p && !whole) {
+    // the largest logit in 32 bits that is not above the limit: what lies in higher bins is kept
+    const double least = r.max + r.lim;
+    float f = (float)least;
+    if ((double)f > least) f = logit_of(key_of(f) + 1);
+    f = fminf(fmaxf(f * r.c, bins.lower(bins.last())), bins.upper(0));
+    mine = min(max(bins.at(f), 0), mine);
+  }
+  uint64_t bm = mass_before;
+  uint32_t bc = count_before;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    bool limit = r.k > 0 && bc < (uint32_t)r.k && (uint32_t)r.k <= bc + count[j];
+    if (!by_count) limit |= r.top_p && count[j] != 0 && (double)(bm + mass[j]) >= most;
+    if (limit) mine = min(mine, lane * kEach + j);
+    bm += mass[j];
+    bc += count[j];
+  }
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) mine = min(mine, __shfl_xor(mine, s));
+  if (lane == mine / kEach) {
+    uint32_t in = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (j < mine % kEach) {
+        mass_before += mass[j];
+        count_before += count[j];
+      }
+      if (j == mine % kEach) in = count[j];
+    }
+    sh.found = mine;
+    sh.found_mass = mass_before;
+    sh.found_count = count_before;
+    sh.found_in = in;
+    sh.listing = 0;
+  }
+}
+
+// all: the row's mass.  visit(low, high, edge bin, take) calls take(l, place) for all tokens with
+// low <= l c < high.  kDrawn: the token is written; kKnown: the edge is, and sh.list begins
+// with the sh.found_in tokens beside it that are kept; kUnknown: draw_slowly.
+// by_count: sh.count need not count all, but show a bin down to which there are k.
+template <int THREADS, typename F>
+__device__ __forceinline__ Outcome choose(Shared& sh, const SampleArgs& a, int b, const Rules& r, bool by_count,
+                                          uint64_t all, int top_bin, Edge& edge, F visit) {
+  constexpr int kEach = kList / THREADS;
+  const int tid = threadIdx.x, wave = tid / kWave;
+  const bool whole = r.k > 0 && r.top_p;  // (top-p's limit needs the first k's mass)
+  if (whole && !by_count) return kUnknown;
+  Bins bins{top_bin, false, 0.f};
+  if (wave == 0) find_edge(sh, r, by_count, whole, r.p * (double)all, bins, 0, 0);
+  lds_barrier();
+  edge.bin = sh.found;
+  uint32_t before = sh.found_count;
+  uint64_t before_mass = sh.found_mass;
+  bool listed = by_count || before + sh.found_in <= kList;  // all that can be kept is in the list
+  float low = bins.lower(edge.bin), high = listed ? INFINITY : bins.upper(edge.bin);
+  edge.upper = high;
+  if (!listed && sh.found_in > kList && fabsf(low) < 0x1p14f) {
+    // more than the list holds: parts of the bin
+    lds_barrier();
+    for (int i = tid; i < kBins; i += THREADS) {
+      sh.mass[i] = 0;
+      sh.count[i] = 0;
+    }
+    lds_barrier();
+    bins.fine = true;
+    bins.low = low;
+    visit(low, high, edge.bin, [&](float l, uint64_t) {
+      const int bin = bins.at(l * r.c);
+      atomicAdd(&sh.count[bin], 1u);
+      atomicAdd((unsigned long long*)&sh.mass[bin], (unsigned long long)weight_of(r, l));
+    });
+    lds_barrier();
+    if (wave == 0) find_edge(sh, r, false, false, r.p * (double)all, bins, before_mass, before);
+    lds_barrier();
+    before = sh.found_count;
+    before_mass = sh.found_mass;
+    low = bins.lower(sh.found);
+    high = bins.upper(sh.found);
+  }
+  if (!listed && sh.found_in > kList) return kUnknown;
+  if (listed) {
+    before = 0;
+    before_mass = 0;
+  }
+  visit(low, high, edge.bin, [&](float, uint64_t place) {
+    const int at = atomicAdd(&sh.listing, 1);
+    if (at < kList) sh.list[at] = place;
+  });
+  lds_barrier();
+  const int n = sh.listing;
+  if (n > kList) return kUnknown;  // (by_count only)
+  edge.high = high;
+  auto keeps = [&](uint32_t rank, uint64_t mass_before, float l, double most) {
+    return (r.k == 0 || rank < (uint32_t)r.k) && (!r.top_p || (double)mass_before < most) &&
+           (l == r.max_f || (double)l - r.max >= r.lim);
+  };
+
+  if (listed && n <= kFew) {  // each against all
+    uint64_t place = ~0ull, w = 0;
+    float l = 0.f;
+    if (tid < n) {
+      place = sh.list[tid];
+      l = logit_of((uint32_t)(place >> 32));
+      w = weight_of(r, l);
+      sh.weight[tid] = w;
+    }
+    lds_barrier();
+    uint32_t rank = 0;
+    uint64_t upto = 0;
+    const bool active = wave * kWave < n;
+    if (active) {
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) {
+        const uint64_t o = sh.list[j], ow = sh.weight[j];
+        rank += o < place;
+        upto += o < place ? ow : 0;
       }
     }
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[j][e] = (float)v[j][e];
+    uint64_t limit_mass = all;
+    if (whole) limit_mass = sum_few(sh, 0, active && tid < n && rank < (uint32_t)r.k ? w : 0, n);
+    if (!(tid < n && (rank == 0 || keeps(rank, upto, l, r.p * (double)limit_mass)))) w = 0;
+    const uint64_t total = sum_few(sh, 1, w, n), target = target_of(a.uniform[b], total);
+    if (tid < n) sh.weight[tid] = w;
+    lds_barrier();
+    if (!active) return kDrawn;
+    uint64_t from = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) {
+      const uint32_t o = (uint32_t)sh.list[j];
+      const uint64_t ow = sh.weight[j];
+      from += o < (uint32_t)place ? ow : 0;
+    }
+    if (tid < n && from <= target && target < from + w) finish(a, b, r, (int)(uint32_t)place, l, total);
+    return kDrawn;
   }
-  Rules r = rules_of(a, b);
-  const bool by_count = r.k > 0 && r.k <= kMostK, filtered = r.k > 0 || r.top_p || r.min_p;
-  sh.slice.mass[tid] = 0;
-  sh.slice.count[tid] = 0;
+
+  auto sort = [&](int n) {
+    int size = 2;
+    while (size < n) size <<= 1;
+    for (int i = n + tid; i < size; i += THREADS) sh.list[i] = ~0ull;
+    lds_barrier();
+    for (int k = 2; k <= size; k <<= 1)
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        for (int i = tid; i < size / 2; i += THREADS) {
+          const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+          const uint64_t p = sh.list[lo], q = sh.list[hi];
+          if ((p > q) == ((lo & k) == 0)) {
+            sh.list[lo] = q;
+            sh.list[hi] = p;
+          }
+        }
+        lds_barrier();
+      }
+  };
+  sort(n);
+  // kEach tokens a thread, in order: the kept ones are the first of them
+  uint64_t w[kEach], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = tid * kEach + j;
+    w[j] = i < n ? weight_of(r, logit_of((uint32_t)(sh.list[i] >> 32))) : 0;
+    sum += w[j];
+  }
+  uint64_t upto = sum;
+  uint32_t none = 0;
+  sums_before<THREADS>(sh, upto, none);
+  upto += before_mass;
+  uint64_t limit_mass = all;
+  if (whole) {
+    uint64_t t = upto;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      t += w[j];
+      if (tid * kEach + j == min(r.k, n) - 1) sh.found_mass = t;
+    }
+    lds_barrier();
+    limit_mass = sh.found_mass;
+  }
+  if (tid == 0) sh.found = 0;
+  lds_barrier();
+  const double most = r.p * (double)limit_mass;
+  int kept = 0;
+  uint64_t kept_sum = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = tid * kEach + j;
+    if (i < n) {
+      const bool keep = keeps(before + i, upto, logit_of((uint32_t)(sh.list[i] >> 32)), most);
+      if (keep || before + i == 0) {
+        kept = i + 1;
+        kept_sum += w[j];
+      }
+    }
+    upto += w[j];
+  }
+  if (kept > 0) atomicMax(&sh.found, kept);
+  lds_barrier();
+  kept = sh.found;
+  if (!listed) {
+    if (tid == 0) sh.found_in = (uint32_t)kept;
+    if (kept > 0) {
+      edge.l = logit_of((uint32_t)(sh.list[kept - 1] >> 32));
+      edge.i = (int)(uint32_t)sh.list[kept - 1];
+    } else {  // none of that bin: the least logit above it (l c is within a rounding or two of high)
+      float l = high / r.c;
+      for (int t = 0; t < 4 && !(l * r.c >= high); ++t) l = logit_of(key_of(l) - 1);
+      for (int t = 0; t < 8 && logit_of(key_of(l) + 1) * r.c >= high; ++t) l = logit_of(key_of(l) + 1);
+      edge.l = l;
+      edge.i = INT32_MAX;
+    }
+    return kKnown;
+  }
+  // by number; the token
+  const uint64_t total = sum_all<THREADS>(sh, kept_sum);
+  uint64_t mine[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) mine[j] = sh.list[tid * kEach + j];
+  lds_barrier();
+#pragma unroll
+  for (int j = 0; j < kEach; ++j)
+    if (tid * kEach + j < kept) sh.list[tid * kEach + j] = mine[j] << 32 | mine[j] >> 32;
+  lds_barrier();
+  sort(kept);
+  const uint64_t target = target_of(a.uniform[b], total);
+  uint64_t from = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = tid * kEach + j;
+    w[j] = i < kept ? weight_of(r, logit_of((uint32_t)sh.list[i])) : 0;
+    from += w[j];
+  }
+  sums_before<THREADS>(sh, from, none);
+  int found = -1;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (from <= target && target < from + w[j]) found = tid * kEach + j;
+    from += w[j];
+  }
+  if (found >= 0) {
+    const uint64_t e = sh.list[found];
+    finish(a, b, r, (int)(e >> 32), logit_of((uint32_t)e), total);
+  }
+  return kDrawn;
+}
+
+// The first token at which the kept mass of ROUNDS pieces a thread, numbers from `first` on,
+// exceeds `rest`.  piece(j): a round's.  whole_row: the row's token, rest and total follow from the
+// sum; else total is the row's kept mass.  False if none of them has mass.
+template <int TY, int THREADS, int ROUNDS, typename P>
+__device__ __forceinline__ bool draw(Shared& sh, const SampleArgs& a, int b, const Rules& r, const Edge& edge, int first,
+                                     uint64_t rest, bool whole_row, uint64_t total, P piece) {
+  constexpr int N = kPiece<TY>, kWaves = THREADS / kWave, kParts = ROUNDS * kWaves;
+  typedef typename Elem<TY>::V V;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  // (masked tokens are not above any l)
+  auto keeps = [&](float l, int i) { return l > edge.l || (l == edge.l && i <= edge.i); };
+  auto weights = [&](const V& v, int i, uint64_t* w) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {  // (all at once would take too many registers)
+      float l[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        l[k] = (float)v[e + k];
+        asm volatile("" : "+v"(l[k]));
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t x = weight_of(r, l[k]);
+        w[e + k] = keeps(l[k], i + e + k) ? x : 0;
+      }
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const V v = piece(j);
+    const int i = first + (j * THREADS + tid) * N;
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) any |= keeps((float)v[e], i + e);
+    uint64_t s = 0;
+    if (__ballot(any) != 0) {
+      uint64_t w[N];
+      weights(v, i, w);
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += w[e];
+      s = wave_sum64(s);
+    }
+    if (lane == 0) sh.parts[j * kWaves + wave] = s;
+  }
+  lds_barrier();
+  // the round and wave that it is in: the parts by lanes, two each
+  static_assert(kParts <= 2 * kWave, "parts");
+  const uint64_t p0 = 2 * lane < kParts ? sh.parts[2 * lane] : 0, p1 = 2 * lane + 1 < kParts ? sh.parts[2 * lane + 1] : 0;
+  uint64_t before = wave_before(p0 + p1);
+  const uint64_t sum = __shfl((unsigned long long)(before + p0 + p1), kWave - 1);
+  if (sum == 0) return false;
+  if (whole_row) {
+    total = sum;
+    rest = target_of(a.uniform[b], total);
+  }
+  rest = min(rest, sum - 1);
+  const int at = __builtin_ctzll(__ballot(rest < before + p0 + p1));
+  const bool second = rest >= before + p0;
+  const int g = 2 * at + __shfl((int)second, at);
+  before = __shfl((unsigned long long)(second ? before + p0 : before), at);
+  if (g % kWaves != wave) return true;
+  const int i = first + (g / kWaves * THREADS + tid) * N;
+  const V f = load_piece<TY>((const typename Elem<TY>::T*)a.logits + b * a.row, min(i, a.vocab), a.vocab);
+  uint64_t w[N], own = 0;
+  weights(f, i, w);
+#pragma unroll
+  for (int e = 0; e < N; ++e) own += w[e] = i + e < a.vocab ? w[e] : 0;
+  uint64_t from = before + wave_before(own);
+  int found = -1;
+  float found_l = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if (from <= rest && rest < from + w[e]) {
+      found = i + e;
+      found_l = (float)f[e];
+    }
+    from += w[e];
+  }
+  if (found >= 0) finish(a, b, r, found, found_l, total);
+  return true;
+}
+
+__device__ __forceinline__ void no_token(const SampleArgs& a, int b) {
+  if (threadIdx.x != 0) return;
+  a.tokens[b] = -1;
+  if (a.logprob != nullptr) a.logprob[b] = NAN;
+}
+
+// Pieces of elements [first, ...) of a row, THREADS apart; masked past its end.
+template <int TY, int THREADS, int ROUNDS>
+__device__ __forceinline__ void load_rounds(const void* row, int first, int vocab, typename Elem<TY>::V (&v)[ROUNDS]) {
+  constexpr int N = kPiece<TY>;
+  typedef typename Elem<TY>::T T;
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int i = first + (j * THREADS + threadIdx.x) * N;
+    if (i + N <= vocab) {
+      v[j] = *(const typename Elem<TY>::V*)((const T*)row + i);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[j][e] = i + e < vocab ? ((const T*)row)[i + e] : (T)-INFINITY;
+    }
+  }
+}
+
+// The largest of what the workgroup holds; NaN if one is.  mine: the thread's.
+template <int TY, int THREADS, int ROUNDS>
+__device__ __forceinline__ float largest(Shared& sh, const typename Elem<TY>::V (&v)[ROUNDS], float& mine) {
   float top = -INFINITY;
   bool bad = false;
 #pragma unroll
-  for (int j = 0; j < PER; ++j)
+  for (int j = 0; j < ROUNDS; ++j)
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      top = fmaxf(top, x[j][e]);
-      bad |= x[j][e] != x[j][e];
+    for (int e = 0; e < kPiece<TY>; ++e) {
+      const float l = (float)v[j][e];
+      top = fmaxf(top, l);
+      bad |= l != l;
     }
-  top = bad ? NAN : top;
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) {
-    const float o = __shfl_xor(top, s);
-    top = o > top || o != o ? o : top;  // (NaN stays)
-  }
-  if (lane == 0) sh.top[wave] = top;
-  if (tid == 0) sh.found = INT32_MAX;
+  mine = top;
+  top = wave_largest(bad ? NAN : top);
+  if (threadIdx.x % kWave == 0) sh.top[threadIdx.x / kWave] = top;
   lds_barrier();
-  for (int w = 0; w < kWaves; ++w) {
-    const float o = sh.top[w];
-    top = o > top || o != o ? o : top;
-  }
-  uint64_t total = 0;  // greedy rows: the first of the largest
-  if (top > -INFINITY) {
-    if (r.greedy) {
-      int first = INT32_MAX;
 #pragma unroll
-      for (int j = PER - 1; j >= 0; --j)
+  for (int w = 0; w < THREADS / kWave; ++w) top = larger(top, sh.top[w]);
+  return top;
+}
+
+// The number of the first element that is `top`; sh.found is INT32_MAX before, and a barrier lies between.
+template <int TY, int THREADS, int ROUNDS>
+__device__ __forceinline__ int first_of(Shared& sh, const typename Elem<TY>::V (&v)[ROUNDS], int first, float top) {
+  constexpr int N = kPiece<TY>;
+  int at = INT32_MAX;
 #pragma unroll
-        for (int e = N - 1; e >= 0; --e)
-          if (x[j][e] == top) first = slice * kSampleSlice + (j * kThreads + tid) * N + e;
-      if (first != INT32_MAX) atomicMin(&sh.found, first);
-      lds_barrier();
-      total = (uint64_t)(uint32_t)sh.found;
-    } else {
-      r.max_f = top;
-      r.max = (double)top;
-      const int upper = bin_of(top, r.c);
+  for (int j = ROUNDS - 1; j >= 0; --j)
 #pragma unroll
-      for (int j = 0; j < PER; ++j)
+    for (int e = N - 1; e >= 0; --e)
+      if ((float)v[j][e] == top) at = first + (j * THREADS + threadIdx.x) * N + e;
+  if (at != INT32_MAX) atomicMin(&sh.found, at);
+  lds_barrier();
+  return sh.found;
+}
+
+// Bins and mass (of the thread) of what the workgroup holds, relative to its largest (r).
+// slot(bin): where a bin is kept.
+template <int TY, int ROUNDS, typename S>
+__device__ __forceinline__ uint64_t count_bins(Shared& sh, const Rules& r, typename Elem<TY>::V (&v)[ROUNDS], bool filtered,
+                                               bool by_count, S slot) {
+  constexpr int G = 4;  // weights at a time (all at once would take too many registers)
+  const int upper = bin_of(r.max_f, r.c);
+  uint64_t total = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          float l = x[j][e];
-          asm volatile("" : "+v"(l));  // (one after another: all at once would take too many registers)
-          const int bin = filtered ? upper - bin_of(l, r.c) : 0;
-          if (l == -INFINITY || bin >= kBins - 1) continue;
-          if (filtered) atomicAdd(&sh.slice.count[bin], 1u);
-          if (!by_count) {
-            const uint64_t w = weight_of(r, l);
-            total += w;
-            if (filtered) atomicAdd((unsigned long long*)&sh.slice.mass[bin], (unsigned long long)w);
-          }
-        }
-      total = wave_sum64(total);
-      if (lane == 0) sh.wave_mass[wave] = total;
-      lds_barrier();
-      total = 0;
-      for (int w = 0; w < kWaves; ++w) total += sh.wave_mass[w];
+  for (int j = 0; j < ROUNDS; ++j)
+#pragma unroll
+    for (int e0 = 0; e0 < kPiece<TY>; e0 += G) {
+      float l[G];
+      uint64_t w[G];
+#pragma unroll
+      for (int e = 0; e < G; ++e) {
+        l[e] = (float)v[j][e0 + e];
+        asm volatile("" : "+v"(l[e]));
+      }
+      if (!by_count) {
+#pragma unroll
+        for (int e = 0; e < G; ++e) total += w[e] = weight_of(r, l[e]);
+      }
       if (filtered) {
-        put_through(counts + slice * kBins + tid, sh.slice.count[tid]);
-        if (!by_count) put_through(masses + slice * kBins + tid, sh.slice.mass[tid]);
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+          const int bin = upper - low_bin_of(l[e], r.c);  // (masked ones: far below)
+          if (bin >= kBins - 1) continue;
+          atomicAdd(&sh.count[slot(bin)], 1u);
+          if (!by_count) atomicAdd((unsigned long long*)&sh.mass[slot(bin)], (unsigned long long)w[e]);
+        }
       }
     }
+  return total;
+}
+
+__device__ __forceinline__ bool by_counts(const Rules& r) { return r.k > 0 && r.k <= kMostK; }
+__device__ __forceinline__ bool is_filtered(const Rules& r) { return r.k > 0 || r.top_p || r.min_p; }
+// Bins are exact whole numbers of 32 bits only for logits that are not huge next to T.
+__device__ __forceinline__ bool has_bins(const Rules& r) { return fabsf(r.max_f * r.c) < 0x1p29f; }
+
+// A row that a workgroup holds, ROUNDS pieces a thread.
+template <int TY, int ROUNDS>
+__global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
+  constexpr int N = kPiece<TY>, THREADS = kRowThreads;
+  typedef typename Elem<TY>::T T;
+  typedef typename Elem<TY>::V V;
+  __shared__ Shared sh;
+  constexpr int kHits = ROUNDS > 8 ? 128 : 256;  // threads whose tokens are dealt out, at most
+  __shared__ V dealt[ROUNDS > 1 ? kHits : 1][ROUNDS];
+  __shared__ int whose[kHits], hits;
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const void* const row = (const T*)a.logits + b * a.row;
+  V v[ROUNDS];
+  load_rounds<TY, THREADS, ROUNDS>(row, 0, a.vocab, v);
+  Rules r = rules_of(a, b);
+  for (int i = tid; i < kBins; i += THREADS) {
+    sh.mass[i] = 0;
+    sh.count[i] = 0;
   }
   if (tid == 0) {
-    put_through(records + slice * 2, (uint64_t)__builtin_bit_cast(uint32_t, top));
-    put_through(records + slice * 2 + 1, total);
+    sh.found = INT32_MAX;
+    hits = 0;
   }
-  if (!last_of(a.counters + b, (uint32_t)slices, &sh.flag)) return;
-
-  // The row: a lane has a slice.
-  uint64_t rec_mass = 0;
-  float rec_top = -INFINITY;
-  if (lane < slices) {
-    rec_top = __builtin_bit_cast(float, (uint32_t)get_through(records + lane * 2));
-    rec_mass = get_through(records + lane * 2 + 1);
-  }
-  top = rec_top;
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) {
-    const float o = __shfl_xor(top, s);
-    top = o > top || o != o ? o : top;
-  }
-  if (!(top > -INFINITY)) {  // NaN, or nothing that could be drawn
-    if (tid == 0) {
-      a.tokens[b] = -1;
-      if (a.logprob != nullptr) a.logprob[b] = NAN;
-    }
-    return;
-  }
+  float mine;
+  r.max_f = largest<TY, THREADS, ROUNDS>(sh, v, mine);
+  if (!(r.max_f > -INFINITY)) return no_token(a, b);
   if (r.greedy) {
-    const uint64_t which = __ballot(rec_top == top);
-    if (tid == __builtin_ctzll(which)) {
-      a.tokens[b] = (int32_t)rec_mass;
+    const int first = first_of<TY, THREADS, ROUNDS>(sh, v, 0, r.max_f);
+    if (tid == 0) {
+      a.tokens[b] = first;
       if (a.logprob != nullptr) a.logprob[b] = 0.f;
     }
     return;
   }
-  r.max_f = top;
-  r.max = (double)top;
-  const float top_c = top * r.c;
-  bool slowly = filtered && !(fabsf(top_c) < 0x1p29f);
-  // slices' masses in multiples of 2^-44 of the row's largest weight
-  const int top_bin = bin_of(top, r.c);
-  const bool some = rec_top > -INFINITY;
-  const double by = some ? rec_top == top ? 1.0 : factor(((double)rec_top - r.max) * r.inv) : 0.0;
-  const int offset = some ? min(top_bin - bin_of(rec_top, r.c), kBins) : kBins;
-  uint64_t mass = (uint64_t)((double)rec_mass * by + 0.5);
-  const uint64_t all = wave_sum64(mass);
-  const float u = a.uniform[b];
-  // kept: bins above the edge, and in it up to the last one
-  float edge_low = -INFINITY, edge_high = -INFINITY;
-  uint64_t last = 0;
-  do {
-    if (!filtered || slowly) break;
-    if (wave == 0) {
-      sh.joined.factor[lane] = by;
-      sh.joined.offset[lane] = offset;
-    }
-    lds_barrier();
-    // the row's bins, a thread each; the lowest one has what has no mass
-    double bin_mass = 0.0;
-    uint32_t bin_count = 0;
-    for (int s = 0; s < slices; ++s) {
-      const int from = tid - sh.joined.offset[s];
-      if (from < 0 || tid >= kBins - 1) continue;
-      bin_count += get_through(counts + s * kBins + from);
-      if (!by_count) bin_mass += (double)get_through(masses + s * kBins + from) * sh.joined.factor[s];
-    }
-    const uint64_t own = (uint64_t)(bin_mass + 0.5);
-    uint64_t m = own;
-    uint32_t c = bin_count;
-    sums_before(sh, m, c);
-    // the bin of the last kept one: the first of those in which a rule's limit lies
-    if (tid == 0) sh.found = kBins - 2;
-    lds_barrier();
-    const bool whole = r.k > 0 && r.top_p;  // (top-p's limit needs the first k's mass)
-    slowly = whole && !by_count;
-    if (slowly) break;
-    bool limit = r.k > 0 && c < (uint32_t)r.k && (uint32_t)r.k <= c + bin_count;
-    if (!by_count) limit |= r.top_p && bin_count != 0 && (double)(m + own) >= r.p * (double)all;
-    if (limit) atomicMin(&sh.found, tid);
-    if (r.min_p && !whole && tid == 0) {
-      // the largest logit in 32 bits that is not above the limit: what lies in higher bins is kept
-      const double least = r.max + r.lim;
-      float f = (float)least;
-      if ((double)f > least) f = key_of(f) == ~0u ? f : logit_of(key_of(f) + 1);
-      atomicMin(&sh.found, max(0, min(top_bin - bin_of(f, r.c), kBins - 2)));
-    }
-    lds_barrier();
-    const int edge = sh.found;
-    lds_barrier();
-    if (tid == edge) {
-      sh.found_mass = m;
-      sh.found_count = c;
-      sh.flag = (int)bin_count;
-    }
-    if (tid == 0) sh.found = 0;
-    lds_barrier();
-    uint32_t before = sh.found_count;
-    uint64_t before_mass = sh.found_mass;
-    const uint32_t in_edge = (uint32_t)sh.flag;
-    const bool listed = before + in_edge <= kList;  // all that can be kept is in the list
-    slowly = !listed && (by_count || in_edge > kList);
-    if (slowly) break;
-    if (listed) {
-      before = 0;
-      before_mass = 0;
-    }
-    // collect
-    const float low = (float)(top_bin - edge), high = listed ? INFINITY : low + 1.f;
-    each<TY>(row, a.vocab, [&](int i, float l) {
-      const float f = l * r.c;
-      if (f >= low && f < high) {
-        const int at = atomicAdd(&sh.found, 1);
-        if (at < kList) sh.joined.list[at] = place_of(l, i);
+  r.max = (double)r.max_f;
+  Edge edge{-INFINITY, -1, 0, 0.f, 0.f};
+  if (is_filtered(r)) {
+    Outcome o = kUnknown;
+    if (has_bins(r)) {
+      const bool by_count = by_counts(r);
+      const int top_bin = bin_of(r.max_f, r.c);
+      uint64_t all = 0;
+      if (by_count) {
+        // the threads' largest alone: where k of them lie, at least k tokens do
+        const int bin = top_bin - low_bin_of(mine, r.c);
+        if (bin < kBins - 1) atomicAdd(&sh.count[bin], 1u);
+        lds_barrier();
+      } else {
+        all = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, true, false, [](int bin) { return bin; }));
       }
-    });
-    lds_barrier();
-    const int n = min(sh.found, kList);
-    auto sort = [&](int n) {
-      int size = 2;
-      while (size < n) size <<= 1;
-      for (int i = n + tid; i < size; i += kThreads) sh.joined.list[i] = ~0ull;
-      lds_barrier();
-      for (int k = 2; k <= size; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-          for (int i = tid; i < size / 2; i += kThreads) {
-            const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-            const uint64_t p = sh.joined.list[lo], q = sh.joined.list[hi];
-            if ((p > q) == ((lo & k) == 0)) {
-              sh.joined.list[lo] = q;
-              sh.joined.list[hi] = p;
-            }
+      o = choose<THREADS>(sh, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, auto take) {
+        if (ROUNDS > 1 && by_count) {
+          // few threads hold any: theirs are dealt to all
+          const bool hit = mine * r.c >= low;
+          const int at = hit ? atomicAdd(&hits, 1) : kHits;
+          if (at < kHits) {
+            whose[at] = tid;
+#pragma unroll
+            for (int j = 0; j < ROUNDS; ++j) dealt[at][j] = v[j];
           }
           lds_barrier();
+          const int n = hits;
+          if (n <= kHits) {
+            for (int i = tid; i < n * ROUNDS * N; i += THREADS) {
+              const int w = i / (ROUNDS * N), j = i / N % ROUNDS, e = i % N;
+              const float l = (float)((const T*)&dealt[w][j])[e];
+              if (l * r.c >= low) take(l, place_of(l, (j * THREADS + whose[w]) * N + e));
+            }
+            return;
+          }
         }
-    };
-    sort(n);
-    // four tokens a thread, in order: the kept ones are the first of them
-    constexpr int kEach = kList / kThreads;
-    uint64_t w[kEach], sum = 0;
-    for (int j = 0; j < kEach; ++j) {
-      const int i = tid * kEach + j;
-      w[j] = i < n ? weight_of(r, logit_of((uint32_t)(sh.joined.list[i] >> 32))) : 0;
-      sum += w[j];
-    }
-    uint64_t upto = sum;
-    uint32_t none = 0;
-    sums_before(sh, upto, none);
-    upto += before_mass;
-    uint64_t limit_mass = all;
-    if (whole) {
-      uint64_t t = upto;
-      for (int j = 0; j < kEach; ++j) {
-        t += w[j];
-        if (tid * kEach + j == min(r.k, n) - 1) sh.found_mass = t;
-      }
-      lds_barrier();
-      limit_mass = sh.found_mass;
-    }
-    if (tid == 0) sh.found = 0;
-    lds_barrier();
-    const double most = r.p * (double)limit_mass;
-    int kept = 0;
-    uint64_t kept_sum = 0;
-    for (int j = 0; j < kEach; ++j) {
-      const int i = tid * kEach + j;
-      if (i < n) {
-        const float l = logit_of((uint32_t)(sh.joined.list[i] >> 32));
-        const bool keep = (r.k == 0 || before + i < (uint32_t)r.k) && (!r.top_p || (double)upto < most) &&
-                          (l == top || (double)l - r.max >= r.lim);
-        if (keep || before + i == 0) {
-          kept = i + 1;
-          kept_sum += w[j];
+#pragma unroll
+        for (int j = 0; j < ROUNDS; ++j) {
+          asm volatile("" : "+v"(v[j]));
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            float l = (float)v[j][e];
+            asm volatile("" : "+v"(l));
+            const float f = l * r.c;
+            if (f >= low && f < high) take(l, place_of(l, (j * THREADS + tid) * N + e));
+          }
         }
-      }
-      upto += w[j];
+      });
     }
-    if (kept > 0) atomicMax(&sh.found, kept);
-    lds_barrier();
-    kept = sh.found;
-    if (listed) {
-      // by number; the token
-      kept_sum = wave_sum64(kept_sum);
-      if (lane == 0) sh.wave_mass[wave] = kept_sum;
-      uint64_t mine[kEach];
-      for (int j = 0; j < kEach; ++j) mine[j] = sh.joined.list[tid * kEach + j];
-      lds_barrier();
-      uint64_t sum_all = 0;
-      for (int v = 0; v < kWaves; ++v) sum_all += sh.wave_mass[v];
-      for (int j = 0; j < kEach; ++j)
-        if (tid * kEach + j < kept) sh.joined.list[tid * kEach + j] = mine[j] << 32 | mine[j] >> 32;
-      lds_barrier();
-      sort(kept);
-      const uint64_t target = target_of(u, sum_all);
-      uint64_t m2 = 0;
-      for (int j = 0; j < kEach; ++j) {
-        const int i = tid * kEach + j;
-        w[j] = i < kept ? weight_of(r, logit_of((uint32_t)sh.joined.list[i])) : 0;
-        m2 += w[j];
-      }
-      sums_before(sh, m2, none);
-      int found = -1;
-      for (int j = 0; j < kEach; ++j) {
-        if (m2 <= target && target < m2 + w[j]) found = tid * kEach + j;
-        m2 += w[j];
-      }
-      if (found >= 0) {
-        const uint64_t e = sh.joined.list[found];
-        finish(a, b, r, (int)(e >> 32), logit_of((uint32_t)e), sum_all);
-      }
-      return;
-    }
-    // kept mass of the slices: their bins above the edge, and what the list keeps
-    last = kept > 0 ? sh.joined.list[kept - 1] : 0;
-    edge_low = low;
-    edge_high = high;
-    if (tid < kWave) sh.joined.mass[tid] = 0;
-    lds_barrier();
-    for (int s = wave; s < slices; s += kWaves) {
-      uint64_t v = 0;
-      for (int i = lane; i < edge - sh.joined.offset[s]; i += kWave) v += get_through(masses + s * kBins + i);
-      v = wave_sum64(v);
-      if (lane == 0) sh.joined.mass[s] = (uint64_t)((double)v * sh.joined.factor[s] + 0.5);
-    }
-    lds_barrier();
-    for (int j = 0; j < kEach; ++j) {
-      const int i = tid * kEach + j;
-      if (i < kept)
-        atomicAdd((unsigned long long*)&sh.joined.mass[(uint32_t)sh.joined.list[i] / kSampleSlice],
-                  (unsigned long long)w[j]);
-    }
-    lds_barrier();
-    mass = sh.joined.mass[lane];
-  } while (false);
-  if (slowly) return draw_slowly<TY>(sh, a, b, r);
+    if (o == kDrawn) return;
+    if (o == kUnknown) return draw_slowly<TY, THREADS>(sh, a, b, r);
+  }
+  draw<TY, THREADS, ROUNDS>(sh, a, b, r, edge, 0, 0, true, 0, [&](int j) {
+    asm volatile("" : "+v"(v[j]));  // (otherwise the elements converted above are kept, which spills)
+    return v[j];
+  });
+}
 
-  // The slice, then the token in it.
-  const uint64_t mass_before = wave_before(mass), mass_all = wave_sum64(mass), target = target_of(u, mass_all);
-  const uint64_t which = __ballot(mass_before <= target && target < mass_before + mass);
-  int at = __builtin_ctzll(which);
-  uint64_t rest = target - __shfl((unsigned long long)mass_before, at);
-  auto weight = [&](int i, float l) -> uint64_t {
-    const float f = l * r.c;
-    return i < a.vocab && l != -INFINITY && (!filtered || f >= edge_high || (f >= edge_low && place_of(l, i) <= last))
-               ? weight_of(r, l) : 0;
-  };
+// A slice of a longer row.
+template <int TY>
+__global__ void __launch_bounds__(kSliceThreads) k_sample_slices(SampleArgs a) {
+  constexpr int N = kPiece<TY>, THREADS = kSliceThreads, ROUNDS = kSampleSlice / (THREADS * N);
+  typedef typename Elem<TY>::V V;
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, b = blockIdx.y, slice = blockIdx.x;
+  const int64_t at = (int64_t)b * gridDim.x + slice;
+  const void* const row = (const typename Elem<TY>::T*)a.logits + b * a.row;
+  V v[ROUNDS];
+  load_rounds<TY, THREADS, ROUNDS>(row, slice * kSampleSlice, a.vocab, v);
+  Rules r = rules_of(a, b);
+  const bool by_count = by_counts(r), filtered = is_filtered(r);
+  sh.mass[tid] = 0;
+  sh.count[tid] = 0;
+  if (tid == 0) sh.found = INT32_MAX;
+  float mine;
+  r.max_f = largest<TY, THREADS, ROUNDS>(sh, v, mine);
+  SampleRecord rec{};
+  rec.top = r.max_f;
+  rec.cut = -1;
+  if (r.max_f > -INFINITY) {
+    if (r.greedy) {
+      rec.mass = (uint64_t)first_of<TY, THREADS, ROUNDS>(sh, v, slice * kSampleSlice, r.max_f);
+    } else {
+      r.max = (double)r.max_f;
+      const int upper = bin_of(r.max_f, r.c);
+      // (a bin's place does not depend on the slice's maximum, so that those of a row lie beside one another)
+      auto slot = [&](int bin) { return (upper - bin) & (kBins - 1); };
+      if (by_count) {
+        // the threads' largest alone: where k of them lie, at least k tokens do
+        const int bin = upper - low_bin_of(mine, r.c);
+        if (bin < kBins - 1) atomicAdd(&sh.count[slot(bin)], 1u);
+        lds_barrier();
+      } else {
+        rec.mass = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, filtered, false, slot));
+      }
+      if (filtered) {
+        if (!by_count) {
+          a.counts[at * kBins + tid] = sh.count[tid];
+          a.masses[at * kBins + tid] = sh.mass[tid];
+        }
+        // the first tokens: down to the bin with the k-th, or to the last one up to which a list holds all
+        uint64_t none = 0;
+        const uint32_t own = sh.count[slot(tid)];
+        uint32_t c = own;
+        sums_before<THREADS>(sh, none, c);
+        if (tid == 0) {
+          sh.found = by_count ? kBins - 1 : 0;
+          sh.listing = 0;
+        }
+        lds_barrier();
+        if (by_count && c < (uint32_t)r.k && (uint32_t)r.k <= c + own) sh.found = tid + 1;
+        if (!by_count && tid < kBins - 1 && c + own <= kSampleListed) atomicMax(&sh.found, tid + 1);
+        lds_barrier();
+        rec.cut = sh.found - 1;
+        const float low = (float)(upper - rec.cut);
+#pragma unroll
+        for (int j = 0; j < ROUNDS; ++j)
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float l = (float)v[j][e];
+            if (l * r.c >= low) {
+              const int to = atomicAdd(&sh.listing, 1);
+              if (to < kSampleListed)
+                a.lists[at * kSampleListed + to] = place_of(l, slice * kSampleSlice + (j * THREADS + tid) * N + e);
+            }
+          }
+        lds_barrier();
+        rec.listed = sh.listing;
+        if (rec.listed > kSampleListed) {  // (by_count only)
+          rec.cut = -1;
+          rec.listed = 0;
+        }
+      }
+    }
+  }
+  if (tid == 0) a.records[at] = rec;
+}
+
+// A row from its slices.
+template <int TY>
+__global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int slices) {
+  constexpr int N = kPiece<TY>, THREADS = kJoinThreads, ROUNDS = kSampleSlice / (THREADS * N);
+  typedef typename Elem<TY>::V V;
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, b = blockIdx.x;
+  const int64_t at = (int64_t)b * slices;
+  const void* const row = (const typename Elem<TY>::T*)a.logits + b * a.row;
+  Rules r = rules_of(a, b);
+  SampleRecord rec{};
+  rec.top = -INFINITY;
+  if (lane < slices) rec = a.records[at + lane];
+  r.max_f = wave_largest(rec.top);
+  if (!(r.max_f > -INFINITY)) return no_token(a, b);
+  if (r.greedy) {
+    if (tid == __builtin_ctzll(__ballot(rec.top == r.max_f))) {
+      a.tokens[b] = (int32_t)rec.mass;
+      if (a.logprob != nullptr) a.logprob[b] = 0.f;
+    }
+    return;
+  }
+  r.max = (double)r.max_f;
+  const bool by_count = by_counts(r), filtered = is_filtered(r);
+  // slices' masses in multiples of 2^-44 of the row's largest weight
+  const bool some = rec.top > -INFINITY;
+  const double by = !some ? 0.0 : rec.top == r.max_f ? 1.0 : factor(((double)rec.top - r.max) * r.inv);
+  uint64_t mass = (uint64_t)((double)rec.mass * by + 0.5);
+  Edge edge{-INFINITY, -1, 0, 0.f, 0.f};
+  if (filtered) {
+    Outcome o = kUnknown;
+    const int top_bin = bin_of(r.max_f, r.c), lower = some ? top_bin - bin_of(rec.top, r.c) : 2 * kBins;
+    if (has_bins(r)) {
+      const uint64_t all = wave_sum64(mass);
+      // Calls f(place) for all that the slices' lists hold.
+      auto lists = [&](auto f) {
+        for (int s = wave; s < slices; s += THREADS / kWave) {
+          const int n = __builtin_amdgcn_readlane(rec.listed, s);
+          const uint64_t* const list = a.lists + (at + s) * kSampleListed;
+          uint64_t e[kSampleListed / kWave];
+#pragma unroll
+          for (int j = 0; j < kSampleListed / kWave; ++j)
+            if (j * kWave < n) e[j] = list[min(j * kWave + lane, n - 1)];
+#pragma unroll
+          for (int j = 0; j < kSampleListed / kWave; ++j)
+            if (j * kWave + lane < n) f(e[j]);
+        }
+      };
+      if (by_count) {
+        sh.count[tid] = 0;
+        lds_barrier();
+        lists([&](uint64_t place) {
+          const int bin = top_bin - low_bin_of(logit_of((uint32_t)(place >> 32)), r.c);
+          if (bin < kBins - 1) atomicAdd(&sh.count[bin], 1u);
+        });
+      } else {
+        // the row's bins, a thread each; the lowest one has what has no mass
+        const int bin = (top_bin - tid) & (kBins - 1);
+        double m = 0.0;
+        uint32_t c = 0;
+        constexpr int kBatch = 16;
+        for (int s0 = 0; s0 < slices; s0 += kBatch) {
+          uint64_t masses[kBatch];
+          uint32_t counts[kBatch];
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            const int64_t i = (at + min(s0 + j, slices - 1)) * kBins + tid;
+            counts[j] = a.counts[i];
+            masses[j] = a.masses[i];
+          }
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            const int s = min(s0 + j, kWave - 1);
+            // (a slice's place holds another bin where the row's is above its maximum)
+            const bool has = s0 + j < slices && bin >= __builtin_amdgcn_readlane(lower, s) && bin < kBins - 1;
+            const double f = __shfl(by, s);  // (by all lanes)
+            c += has ? counts[j] : 0;
+            m += has ? (double)masses[j] * f : 0.0;
+          }
+        }
+        sh.mass[bin] = (uint64_t)(m + 0.5);
+        sh.count[bin] = c;
+      }
+      lds_barrier();
+      // (of counted rows every slice lists the first k, or it does not count here)
+      if (!by_count || __ballot(some && rec.cut < 0) == 0)
+        o = choose<THREADS>(sh, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int edge_bin, auto take) {
+          if (by_count || __ballot(some && edge_bin - lower > rec.cut) == 0)
+            lists([&](uint64_t place) {
+              const float l = logit_of((uint32_t)(place >> 32)), f = l * r.c;
+              if (f >= low && f < high) take(l, place);
+            });
+          else
+            each<TY, THREADS>(row, a.vocab, [&](int i, float l) {
+              const float f = l * r.c;
+              if (f >= low && f < high) take(l, place_of(l, i));
+            });
+        });
+    }
+    if (o == kDrawn) return;
+    if (o == kUnknown) return draw_slowly<TY, THREADS>(sh, a, b, r);
+    // kept mass of the slices: their bins above the edge, and what the list keeps
+    if (wave == 0) sh.factor[lane] = by;
+    lds_barrier();
+    for (int s = wave; s < slices; s += THREADS / kWave) {
+      uint64_t m = 0;
+      const int from = __builtin_amdgcn_readlane(lower, s);
+      for (int i = lane; i < edge.bin - from; i += kWave)
+        m += a.masses[(at + s) * kBins + ((top_bin - from - i) & (kBins - 1))];
+      m = wave_sum64(m);
+      if (lane == 0) sh.slice[s] = (uint64_t)((double)m * sh.factor[s] + 0.5);
+    }
+    lds_barrier();
+    if (edge.high < edge.upper)  // of its bin, what lies above the list
+      each<TY, THREADS>(row, a.vocab, [&](int i, float l) {
+        const float f = l * r.c;
+        if (f >= edge.high && f < edge.upper)
+          atomicAdd((unsigned long long*)&sh.slice[i / kSampleSlice], (unsigned long long)weight_of(r, l));
+      });
+    for (int i = tid; i < (int)sh.found_in; i += THREADS)
+      atomicAdd((unsigned long long*)&sh.slice[(uint32_t)sh.list[i] / kSampleSlice],
+                (unsigned long long)weight_of(r, logit_of((uint32_t)(sh.list[i] >> 32))));
+    lds_barrier();
+    mass = lane < slices ? sh.slice[lane] : 0;
+  }
+  // the slice, then the token in it
+  const uint64_t before = wave_before(mass), total = wave_sum64(mass), target = target_of(a.uniform[b], total);
+  int s = __builtin_ctzll(__ballot(before <= target && target < before + mass));
+  uint64_t rest = target - __shfl((unsigned long long)before, s);
 #pragma unroll 1
   for (int turn = 0; turn < 2; ++turn) {
-    const int i0 = at * kSampleSlice + tid * N;
-    V v[PER];
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (i0 + j * kThreads * N < a.vocab) v[j] = load_piece<TY>(row, i0 + j * kThreads * N, a.vocab);
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      uint64_t s = 0;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        float l = (float)v[j][e];
-        asm volatile("" : "+v"(l), "+v"(s));
-        s += weight(i0 + j * kThreads * N + e, l);
-      }
-      s = wave_sum64(s);
-      if (lane == 0) sh.waves[j][wave] = s;
-    }
+    V v[ROUNDS];
+    load_rounds<TY, THREADS, ROUNDS>(row, s * kSampleSlice, a.vocab, v);
+    if (draw<TY, THREADS, ROUNDS>(sh, a, b, r, edge, s * kSampleSlice, rest, false, total, [&](int j) { return v[j]; })) return;
+    // (the slice's mass is less than the multiples show: the largest one's has some)
+    s = __builtin_ctzll(__ballot(rec.top == r.max_f));
+    rest = 0;
     lds_barrier();
-    uint64_t sum = 0;
-#pragma unroll 1
-    for (int g = 0; g < PER * kWaves; ++g) sum += sh.waves[g / kWaves][g % kWaves];
-    if (sum == 0) {  // (its mass is less than the multiples show: the largest one's slice has some)
-      at = __builtin_ctzll(__ballot(rec_top == top));
-      rest = 0;
-      lds_barrier();
-      continue;
-    }
-    rest = min(rest, sum - 1);
-    // the round and wave that it is in
-    uint64_t before = 0;
-    int g = 0;
-#pragma unroll 1
-    for (; g < PER * kWaves - 1; ++g) {
-      const uint64_t m = sh.waves[g / kWaves][g % kWaves];
-      if (rest < before + m) break;
-      before += m;
-    }
-    if (g % kWaves != wave) return;
-    const int i = i0 + g / kWaves * kThreads * N;
-    const V f = load_piece<TY>(row, min(i, a.vocab), a.vocab);
-    uint64_t w[N], own = 0;
-#pragma unroll
-    for (int e = 0; e < N; ++e) own += w[e] = weight(i + e, (float)f[e]);
-    uint64_t from = before + wave_before(own);
-    int found = -1;
-    float found_l = 0.f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      if (from <= rest && rest < from + w[e]) {
-        found = i + e;
-        found_l = (float)f[e];
-      }
-      from += w[e];
-    }
-    if (found >= 0) finish(a, b, r, found, found_l, mass_all);
-    return;
   }
 }
 
 template <int TY>
 hipError_t launch_typed(SampleArgs a, hipStream_t s) {
+  constexpr int kRound = kRowThreads * kPiece<TY>;
+  if (!sample_cut(a.vocab, a.top_k != nullptr)) {
+    if (a.vocab <= kRound) k_sample_row<TY, 1><<<(unsigned)a.rows, kRowThreads, 0, s>>>(a);
+    else if (a.vocab <= kSampleSlice) k_sample_row<TY, kSampleSlice / kRound><<<(unsigned)a.rows, kRowThreads, 0, s>>>(a);
+    else k_sample_row<TY, kSampleRow / kRound><<<(unsigned)a.rows, kRowThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
   const int slices = (a.vocab + kSampleSlice - 1) / kSampleSlice, most = kSampleSlices / slices;
-  const int64_t size = dtype_bytes(TY);
   for (int rows = a.rows; rows > 0; rows -= most) {
-    k_sample<TY><<<dim3((unsigned)slices, (unsigned)(rows < most ? rows : most)), kThreads, 0, s>>>(a);
+    const unsigned n = (unsigned)(rows < most ? rows : most);
+    k_sample_slices<TY><<<dim3((unsigned)slices, n), kSliceThreads, 0, s>>>(a);
+    k_sample_join<TY><<<n, kJoinThreads, 0, s>>>(a, slices);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    a.logits = (const uint8_t*)a.logits + most * a.row * size;
+    a.logits = (const uint8_t*)a.logits + most * a.row * dtype_bytes(TY);
     a.uniform += most;
     a.tokens += most;
     if (a.logprob != nullptr) a.logprob += most;

@@ -20,11 +20,9 @@ place, so autograd refuses to use what it saved of them.
 """
 from __future__ import annotations
 
-import threading
-
 import torch
 
-from . import _lib, _stream_handle, block
+from . import _stream_handle, block
 from .block import _binding, _made
 
 
@@ -104,47 +102,8 @@ def distill_loss(logits, teacher_logits, teacher_ids, *, teacher_lse=None, tempe
     return r
 
 
-_SAMPLE_COUNTER_BYTES = 16384  # AQLM_SAMPLE_COUNTER_BYTES
-
-
-def sample_workspace(device="cuda") -> torch.Tensor:
-    """A workspace for :func:`sample`, ready for use (25 MB).  One serves any calls on one
-    stream, one after another."""
-    ws = torch.empty((int(_lib.load().aqlm_sample_workspace_bytes()),), dtype=torch.uint8, device=device)
-    ws[:_SAMPLE_COUNTER_BYTES].zero_()
-    return ws
-
-
-# Workspaces of calls that bring none, one per device and stream, kept for good (as
-# paged_attention's are).
-_workspaces = {}
-_workspaces_lock = threading.Lock()
-
-
-def _workspace(device, stream, handle):
-    if (block._ext or _binding()).capturing(handle):
-        # a graph's launches may run beside this stream's later ones: it gets its own
-        return _workspace_on(stream, device)
-    key = (device, handle)
-    ws = _workspaces.get(key)
-    if ws is None:
-        with _workspaces_lock:  # (of threads that come together, one makes it)
-            ws = _workspaces.get(key)
-            if ws is None:
-                ws = _workspaces[key] = _workspace_on(stream, device)
-    return ws
-
-
-def _workspace_on(stream, device):
-    """Made and zeroed on the stream that launches: in its order, its graph and its memory."""
-    if stream is None:
-        return sample_workspace(device)
-    with torch.cuda.stream(stream):
-        return sample_workspace(device)
-
-
 def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None, return_logprob: bool = False,
-           workspace=None, stream=None):
+           stream=None):
     """A token of each row of ``logits`` [rows, vocab] by the numbers ``uniform`` (fp32
     [rows], in [0, 1)): int32 [rows].  Each rule is a tensor [rows] or None: ``temperature``
     fp32 (1; 0: the largest logit), ``top_k`` int32 (0: all), ``top_p`` fp32 (1: all),
@@ -152,15 +111,9 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
     numbers.  The token is the first one, by number, at which the kept mass exceeds uniform
     times all of it.  -inf masks a token; a row with NaN or with nothing but masked
     tokens gives -1.  With ``return_logprob`` also the logarithm of the token's share of
-    the kept mass (fp32 [rows]).  ``workspace``: as :func:`sample_workspace` makes it;
-    without one, one per stream is kept for good."""
-    handle = _handle(logits, stream)
-    if workspace is None:
-        if not logits.is_cuda:
-            raise ValueError("logits must be a GPU tensor with two dimensions, its rows contiguous")
-        workspace = _workspace(logits.device, stream, handle)
-    r = (block._ext or _binding()).sample(logits, uniform, temperature, top_k, top_p, min_p, return_logprob, workspace,
-                                          handle)
+    the kept mass (fp32 [rows])."""
+    r = (block._ext or _binding()).sample(logits, uniform, temperature, top_k, top_p, min_p, return_logprob,
+                                          _handle(logits, stream))
     if stream is not None:
-        _made(stream, *(r if return_logprob else (r,)))
-    return r
+        _made(stream, *r)
+    return r[:2] if return_logprob else r[0]

@@ -107,9 +107,15 @@ def test_distill_loss(lib):
 
 
 def test_sample(lib):
-    need = lib.aqlm_sample_workspace_bytes()
+    def room(rows, vocab, *r):
+        return lib.aqlm_sample_workspace_bytes(rows, vocab, ctypes.byref(_lib.Sampling(*r)))
 
-    def call(z=P, zs=1000, dtype=F16, rows=3, vocab=1000, u=P, r=(None, None, None, None), tokens=P, lp=None, ws=P,
+    need = room(3, 40000)
+    assert need > 0 and room(6, 40000) == 2 * need and room(3, 40000, None, P) == need
+    assert [room(*v) for v in ((3, 8192), (3, 32768, None, P), (0, 40000), (-1, 40000), (3, (1 << 19) + 1))] == [0] * 5
+    assert room(1 << 20, 40000) < 1 << 26 and lib.aqlm_sample_workspace_bytes(3, 40000, None) == 0  # (rows in turn)
+
+    def call(z=P, zs=40000, dtype=F16, rows=3, vocab=40000, u=P, r=(None, None, None, None), tokens=P, lp=None, ws=P,
              size=need):
         r = None if r is None else ctypes.byref(_lib.Sampling(*r))
         return lib.aqlm_sample(z, zs, dtype, rows, vocab, u, r, tokens, lp, ws, size, None)
