@@ -38,7 +38,8 @@ constexpr int kFew = 256;        // tokens that are compared with one another, w
 constexpr int kMostK = 256;      // up to this top-k bins need no masses: the lists hold all that count
 constexpr int kDigit = 2048;     // bins of the search by bits
 constexpr int kSegments = 2048;  // of a row: 64 pieces of 16 bytes each
-constexpr int kSliceThreads = 512, kJoinThreads = 512, kRowThreads = 512;
+constexpr int kSliceThreads = 512, kJoinThreads = 1024, kRowThreads = 512;
+constexpr int kPool = 8192;  // tokens of a bin, of which the list gets a part
 static_assert(kSampleMaxVocab <= kSegments * kWave * 4, "segments");
 static_assert(kSampleMaxVocab <= kSampleSlice * kWave, "a wave has a row's slices");
 static_assert(kMostK <= kSampleListed, "a slice lists the first k");
@@ -404,7 +405,8 @@ struct Edge {
   float l;
   int i;
   int bin;
-  float high, upper;  // l c: the upper ends of what the list holds and of its bin
+  float high;  // the upper end of l c in the list
+  int pooled;
 };
 enum Outcome { kDrawn, kKnown, kUnknown };
 
@@ -456,7 +458,7 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     bool limit = r.k > 0 && bc < (uint32_t)r.k && (uint32_t)r.k <= bc + count[j];
-    if (!by_count) limit |= r.top_p && count[j] != 0 && (double)(bm + mass[j]) >= most;
+    if (!by_count && !whole) limit |= r.top_p && count[j] != 0 && (double)(bm + mass[j]) >= most;
     if (limit) mine = min(mine, lane * kEach + j);
     bm += mass[j];
     bc += count[j];
@@ -485,24 +487,36 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
 // low <= l c < high.  kDrawn: the token is written; kKnown: the edge is, and sh.list begins
 // with the sh.found_in tokens beside it that are kept; kUnknown: draw_slowly.
 // by_count: sh.count need not count all, but show a bin down to which there are k.
+// pool [kPool]: place for tokens, or null; edge.pooled: how many of the edge's bin it has.
 template <int THREADS, typename F>
-__device__ __forceinline__ Outcome choose(Shared& sh, const SampleArgs& a, int b, const Rules& r, bool by_count,
-                                          uint64_t all, int top_bin, Edge& edge, F visit) {
+__device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const SampleArgs& a, int b, const Rules& r,
+                                          bool by_count, uint64_t all, int top_bin, Edge& edge, F visit) {
   constexpr int kEach = kList / THREADS;
   const int tid = threadIdx.x, wave = tid / kWave;
   const bool whole = r.k > 0 && r.top_p;  // (top-p's limit needs the first k's mass)
-  if (whole && !by_count) return kUnknown;
   Bins bins{top_bin, false, 0.f};
   if (wave == 0) find_edge(sh, r, by_count, whole, r.p * (double)all, bins, 0, 0);
   lds_barrier();
   edge.bin = sh.found;
   uint32_t before = sh.found_count;
   uint64_t before_mass = sh.found_mass;
-  bool listed = by_count || before + sh.found_in <= kList;  // all that can be kept is in the list
+  uint32_t in_edge = sh.found_in;
+  bool listed = by_count || before + in_edge <= kList;  // all that can be kept is in the list
   float low = bins.lower(edge.bin), high = listed ? INFINITY : bins.upper(edge.bin);
-  edge.upper = high;
-  if (!listed && sh.found_in > kList && fabsf(low) < 0x1p14f) {
-    // more than the list holds: parts of the bin
+  if (whole && !listed) return kUnknown;
+  auto list = [&](float, uint64_t place) {
+    const int at = atomicAdd(&sh.listing, 1);
+    if (at < kList) sh.list[at] = place;
+  };
+  if (listed || in_edge <= kList) {
+    visit(low, high, edge.bin, list);
+  } else {
+    // more than the list holds: by the 512 parts of the bin
+    if (pool == nullptr || in_edge > kPool || !(fabsf(low) < 0x1p14f)) return kUnknown;
+    visit(low, high, edge.bin, [&](float, uint64_t place) {
+      const int at = atomicAdd(&sh.listing, 1);
+      if (at < kPool) pool[at] = place;
+    });
     lds_barrier();
     for (int i = tid; i < kBins; i += THREADS) {
       sh.mass[i] = 0;
@@ -511,11 +525,13 @@ __device__ __forceinline__ Outcome choose(Shared& sh, const SampleArgs& a, int b
     lds_barrier();
     bins.fine = true;
     bins.low = low;
-    visit(low, high, edge.bin, [&](float l, uint64_t) {
+    edge.pooled = min(sh.listing, kPool);
+    for (int i = tid; i < edge.pooled; i += THREADS) {
+      const float l = logit_of((uint32_t)(pool[i] >> 32));
       const int bin = bins.at(l * r.c);
       atomicAdd(&sh.count[bin], 1u);
       atomicAdd((unsigned long long*)&sh.mass[bin], (unsigned long long)weight_of(r, l));
-    });
+    }
     lds_barrier();
     if (wave == 0) find_edge(sh, r, false, false, r.p * (double)all, bins, before_mass, before);
     lds_barrier();
@@ -523,16 +539,16 @@ __device__ __forceinline__ Outcome choose(Shared& sh, const SampleArgs& a, int b
     before_mass = sh.found_mass;
     low = bins.lower(sh.found);
     high = bins.upper(sh.found);
+    if (sh.found_in > kList) return kUnknown;
+    for (int i = tid; i < edge.pooled; i += THREADS) {
+      const float f = logit_of((uint32_t)(pool[i] >> 32)) * r.c;
+      if (f >= low && f < high) list(f, pool[i]);
+    }
   }
-  if (!listed && sh.found_in > kList) return kUnknown;
   if (listed) {
     before = 0;
     before_mass = 0;
   }
-  visit(low, high, edge.bin, [&](float, uint64_t place) {
-    const int at = atomicAdd(&sh.listing, 1);
-    if (at < kList) sh.list[at] = place;
-  });
   lds_barrier();
   const int n = sh.listing;
   if (n > kList) return kUnknown;  // (by_count only)
@@ -908,7 +924,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
     return;
   }
   r.max = (double)r.max_f;
-  Edge edge{-INFINITY, -1, 0, 0.f, 0.f};
+  Edge edge{-INFINITY, -1, 0, 0.f, 0};
   if (is_filtered(r)) {
     Outcome o = kUnknown;
     if (has_bins(r)) {
@@ -923,7 +939,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
       } else {
         all = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, true, false, [](int bin) { return bin; }));
       }
-      o = choose<THREADS>(sh, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, auto take) {
+      o = choose<THREADS>(sh, nullptr, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, auto take) {
         if (ROUNDS > 1 && by_count) {
           // few threads hold any: theirs are dealt to all
           const bool hit = mine * r.c >= low;
@@ -1052,6 +1068,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
   constexpr int N = kPiece<TY>, THREADS = kJoinThreads, ROUNDS = kSampleSlice / (THREADS * N);
   typedef typename Elem<TY>::V V;
   __shared__ Shared sh;
+  extern __shared__ __align__(16) uint64_t pool[];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, b = blockIdx.x;
   const int64_t at = (int64_t)b * slices;
   const void* const row = (const typename Elem<TY>::T*)a.logits + b * a.row;
@@ -1074,7 +1091,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
   const bool some = rec.top > -INFINITY;
   const double by = !some ? 0.0 : rec.top == r.max_f ? 1.0 : factor(((double)rec.top - r.max) * r.inv);
   uint64_t mass = (uint64_t)((double)rec.mass * by + 0.5);
-  Edge edge{-INFINITY, -1, 0, 0.f, 0.f};
+  Edge edge{-INFINITY, -1, 0, 0.f, 0};
   if (filtered) {
     Outcome o = kUnknown;
     const int top_bin = bin_of(r.max_f, r.c), lower = some ? top_bin - bin_of(rec.top, r.c) : 2 * kBins;
@@ -1095,13 +1112,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
         }
       };
       if (by_count) {
-        sh.count[tid] = 0;
+        if (tid < kBins) sh.count[tid] = 0;
         lds_barrier();
         lists([&](uint64_t place) {
           const int bin = top_bin - low_bin_of(logit_of((uint32_t)(place >> 32)), r.c);
           if (bin < kBins - 1) atomicAdd(&sh.count[bin], 1u);
         });
-      } else {
+      } else if (tid < kBins) {
         // the row's bins, a thread each; the lowest one has what has no mass
         const int bin = (top_bin - tid) & (kBins - 1);
         double m = 0.0;
@@ -1132,7 +1149,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
       lds_barrier();
       // (of counted rows every slice lists the first k, or it does not count here)
       if (!by_count || __ballot(some && rec.cut < 0) == 0)
-        o = choose<THREADS>(sh, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int edge_bin, auto take) {
+        o = choose<THREADS>(sh, pool, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int edge_bin, auto take) {
           if (by_count || __ballot(some && edge_bin - lower > rec.cut) == 0)
             lists([&](uint64_t place) {
               const float l = logit_of((uint32_t)(place >> 32)), f = l * r.c;
@@ -1159,12 +1176,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
       if (lane == 0) sh.slice[s] = (uint64_t)((double)m * sh.factor[s] + 0.5);
     }
     lds_barrier();
-    if (edge.high < edge.upper)  // of its bin, what lies above the list
-      each<TY, THREADS>(row, a.vocab, [&](int i, float l) {
-        const float f = l * r.c;
-        if (f >= edge.high && f < edge.upper)
-          atomicAdd((unsigned long long*)&sh.slice[i / kSampleSlice], (unsigned long long)weight_of(r, l));
-      });
+    for (int i = tid; i < edge.pooled; i += THREADS) {  // of its bin, what lies above the list
+      const float l = logit_of((uint32_t)(pool[i] >> 32));
+      if (l * r.c >= edge.high)
+        atomicAdd((unsigned long long*)&sh.slice[(uint32_t)pool[i] / kSampleSlice], (unsigned long long)weight_of(r, l));
+    }
     for (int i = tid; i < (int)sh.found_in; i += THREADS)
       atomicAdd((unsigned long long*)&sh.slice[(uint32_t)sh.list[i] / kSampleSlice],
                 (unsigned long long)weight_of(r, logit_of((uint32_t)(sh.list[i] >> 32))));
@@ -1197,11 +1213,13 @@ hipError_t launch_typed(SampleArgs a, hipStream_t s) {
     return hipGetLastError();
   }
   const int slices = (a.vocab + kSampleSlice - 1) / kSampleSlice, most = kSampleSlices / slices;
+  hipError_t e = allow_dynamic_lds((const void*)k_sample_join<TY>, kPool * 8);
+  if (e != hipSuccess) return e;
   for (int rows = a.rows; rows > 0; rows -= most) {
     const unsigned n = (unsigned)(rows < most ? rows : most);
     k_sample_slices<TY><<<dim3((unsigned)slices, n), kSliceThreads, 0, s>>>(a);
-    k_sample_join<TY><<<n, kJoinThreads, 0, s>>>(a, slices);
-    const hipError_t e = hipGetLastError();
+    k_sample_join<TY><<<n, kJoinThreads, kPool * 8, s>>>(a, slices);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.logits = (const uint8_t*)a.logits + most * a.row * dtype_bytes(TY);
     a.uniform += most;
