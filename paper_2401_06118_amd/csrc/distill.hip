@@ -23,7 +23,6 @@ namespace aqlm {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ double teacher_at(const DistillArgs& a, int64_t row, int k) {
@@ -36,8 +35,9 @@ __device__ __forceinline__ double teacher_at(const DistillArgs& a, int64_t row, 
 // NV: pieces of the row that a thread keeps in registers (0: the row is read twice).  A
 // row's last piece ends at its end and may begin inside the one before: what both hold
 // counts for the first and is written alike by both.
-template <int TY, int NV>
-__global__ void __launch_bounds__(kThreads) k_distill(DistillArgs a) {
+template <int TY, int kThreads, int NV>
+__global__ void __launch_bounds__(kThreads, 4) k_distill(DistillArgs a) {
+  constexpr int kWaves = kThreads / kWave;
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
   constexpr int N = kPiece<TY>, kAll = (1 << N) - 1;
@@ -116,7 +116,10 @@ __global__ void __launch_bounds__(kThreads) k_distill(DistillArgs a) {
   };
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) add(x[j], tid + j * kThreads);
+    for (int j = 0; j < NV; ++j) {
+      if (NV > 4) asm volatile("" : "+v"(x[j]), "+v"(s), "+v"(m));  // (all at once would take too many registers)
+      add(x[j], tid + j * kThreads);
+    }
   } else {
     for (int i = tid; i < pieces; i += kThreads) add(load_piece<TY>(in, i * N, a.vocab), i);
   }
@@ -217,25 +220,25 @@ __global__ void __launch_bounds__(kThreads) k_distill(DistillArgs a) {
   }
 }
 
-template <int TY, int NV>
+template <int TY, int kThreads, int NV>
 hipError_t launch(const DistillArgs& a, hipStream_t s) {
   const int lds = a.listed * 16 + (a.vocab + 31) / 32 * 4;
-  const hipError_t e = allow_dynamic_lds((const void*)k_distill<TY, NV>, lds);
+  const hipError_t e = allow_dynamic_lds((const void*)k_distill<TY, kThreads, NV>, lds);
   if (e != hipSuccess) return e;
-  k_distill<TY, NV><<<(unsigned)a.rows, kThreads, lds, s>>>(a);
+  k_distill<TY, kThreads, NV><<<(unsigned)a.rows, kThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 
 template <int TY>
 hipError_t launch_typed(const DistillArgs& a, hipStream_t s) {
-  if (a.vocab < kPiece<TY>) return launch<TY, 0>(a, s);
-  const int n = ((a.vocab + kPiece<TY> - 1) / kPiece<TY> + kThreads - 1) / kThreads;
-  if (n <= 1) return launch<TY, 1>(a, s);
-  if (n <= 2) return launch<TY, 2>(a, s);
-  if (n <= 4) return launch<TY, 4>(a, s);
-  if (n <= 8) return launch<TY, 8>(a, s);
-  if (n <= 16) return launch<TY, 16>(a, s);
-  return launch<TY, 0>(a, s);
+  if (a.vocab < kPiece<TY>) return launch<TY, 256, 0>(a, s);
+  const int pieces = (a.vocab + kPiece<TY> - 1) / kPiece<TY>;
+  if (pieces <= 256) return launch<TY, 256, 1>(a, s);
+  if (pieces <= 4 * 256) return launch<TY, 256, 4>(a, s);
+  if (pieces <= 16 * 256) return launch<TY, 256, 16>(a, s);
+  if (pieces <= 16 * 512) return launch<TY, 512, 16>(a, s);
+  if (pieces <= 16 * 1024) return launch<TY, 1024, 16>(a, s);
+  return launch<TY, 1024, 0>(a, s);
 }
 
 }  // namespace
