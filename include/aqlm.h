@@ -712,11 +712,15 @@ int aqlm_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
  * (weights NULL: 1; it carries a loss scale, 1 / tokens, temperature^2).  A row whose weight
  * is 0 has loss and gradient 0, whatever its logits are; so has a row without entries (with
  * teacher_lse its whole mass is one outcome).  grad NULL: the loss alone; it may be the logits
- * (same address and stride).  Limits: 2^22 - 1 rows, vocab 2^19, 2048 listed. */
+ * (same address and stride).  workspace: aqlm_distill_loss_workspace_bytes(rows, vocab, listed,
+ * dtype) bytes (0 for many rows that are not too long), 16-byte aligned, any contents.
+ * Deterministic.  Limits: 2^22 - 1 rows, vocab 2^19, 2048 listed. */
+size_t aqlm_distill_loss_workspace_bytes(int64_t rows, int64_t vocab, int64_t listed, int32_t dtype);
 int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, const void* teacher,
                       int64_t teacher_stride, int32_t teacher_dtype, const int32_t* ids, int64_t ids_stride,
                       const float* teacher_lse, const float* weights, float temperature, float* loss, void* grad,
-                      int64_t grad_stride, int64_t rows, int64_t vocab, int64_t listed, void* stream);
+                      int64_t grad_stride, int64_t rows, int64_t vocab, int64_t listed, void* workspace,
+                      size_t workspace_bytes, void* stream);
 
 /* How tokens are drawn; [rows] each, NULL: left out. */
 typedef struct aqlm_sampling {

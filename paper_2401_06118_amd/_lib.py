@@ -198,7 +198,10 @@ def load():
         lib.aqlm_layer_norm_backward.argtypes = [p, i64, p, i64, p, i64, p, i64, p, p, i32, i64, i64,
                                                  ctypes.POINTER(Norm), p, size, p]
         lib.aqlm_layer_norm_backward.restype = ctypes.c_int
-        lib.aqlm_distill_loss.argtypes = [p, i64, i32, p, i64, i32, p, i64, p, p, f32, p, p, i64, i64, i64, i64, p]
+        lib.aqlm_distill_loss_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        lib.aqlm_distill_loss_workspace_bytes.restype = size
+        lib.aqlm_distill_loss.argtypes = [p, i64, i32, p, i64, i32, p, i64, p, p, f32, p, p, i64, i64, i64, i64, p, size,
+                                          p]
         lib.aqlm_distill_loss.restype = ctypes.c_int
         lib.aqlm_sample_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(Sampling)]
         lib.aqlm_sample_workspace_bytes.restype = size

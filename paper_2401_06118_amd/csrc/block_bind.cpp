@@ -507,7 +507,7 @@ PyObject* layer_norm_backward(PyObject* const* a) {
                        bytes ? wrap(ws) : none());
 }
 
-// logits, teacher, ids, teacher_lse, weights, temperature, grad, out, stream
+// logits, teacher, ids, teacher_lse, weights, temperature, grad, out, stream; the last of the results is the workspace
 PyObject* distill_loss(PyObject* const* a) {
   const at::Tensor& x = rows2(a[0], "logits");
   const int64_t rows = x.size(0), vocab = x.size(1);
@@ -523,13 +523,17 @@ PyObject* distill_loss(PyObject* const* a) {
   if (want) grad = output2(a[7], "out", x, rows, vocab, x.scalar_type());
   const at::Tensor loss = at::empty({rows}, x.options().dtype(at::kFloat));
   const OnDevice on(x);
+  const size_t bytes = aqlm_distill_loss_workspace_bytes(rows, vocab, ids.size(1), dtype_of(x, "logits"));
+  at::Tensor ws;
+  if (bytes) ws = at::empty({(int64_t)bytes}, x.options().dtype(at::kByte));
   done(aqlm_distill_loss(x.data_ptr(), row_stride(x), dtype_of(x, "logits"), t.data_ptr(), row_stride(t),
                          dtype_of(t, "teacher_logits"), (const int32_t*)pi, row_stride(ids), (const float*)lse,
                          (const float*)w, (float)number(a[5]), loss.data_ptr<float>(), want ? grad.data_ptr() : nullptr,
-                         want ? row_stride(grad) : 0, rows, vocab, ids.size(1), stream_of(a[8])),
+                         want ? row_stride(grad) : 0, rows, vocab, ids.size(1), bytes ? ws.data_ptr() : nullptr, bytes,
+                         stream_of(a[8])),
        "aqlm_distill_loss");
   written(a[7]);
-  return Py_BuildValue("NN", wrap(loss), want ? wrap(grad) : none());
+  return Py_BuildValue("NNN", wrap(loss), want ? wrap(grad) : none(), bytes ? wrap(ws) : none());
 }
 
 // logits, uniform, temperature, top_k, top_p, min_p, return_logprob, stream; the last of the results is the workspace

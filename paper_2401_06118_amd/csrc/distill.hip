@@ -23,225 +23,451 @@ namespace aqlm {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLog2e = 1.44269504088896341f, kLowest = -3.402823466e38f;
 
-__device__ __forceinline__ double teacher_at(const DistillArgs& a, int64_t row, int k) {
+__device__ __forceinline__ float teacher_at(const DistillArgs& a, int64_t row, int k) {
   const int64_t i = row * a.teacher_row + k;
-  if (a.teacher_dtype == kF16) return (double)(float)((const _Float16*)a.teacher)[i];
-  if (a.teacher_dtype == kBf16) return (double)(float)((const __bf16*)a.teacher)[i];
-  return (double)((const float*)a.teacher)[i];
+  if (a.teacher_dtype == kF16) return (float)((const _Float16*)a.teacher)[i];
+  if (a.teacher_dtype == kBf16) return (float)((const __bf16*)a.teacher)[i];
+  return ((const float*)a.teacher)[i];
 }
 
-// NV: pieces of the row that a thread keeps in registers (0: the row is read twice).  A
-// row's last piece ends at its end and may begin inside the one before: what both hold
-// counts for the first and is written alike by both.
-template <int TY, int kThreads, int NV>
-__global__ void __launch_bounds__(kThreads, 4) k_distill(DistillArgs a) {
-  constexpr int kWaves = kThreads / kWave;
+// The listed ids of a row, in LDS; an entry belongs to the thread of its number.
+struct List {
+  double* p;     // teacher's mass
+  int32_t* id;   // -1: no entry
+  float* z;      // student's logit
+  float* t;      // teacher's
+};
+// What a workgroup's waves bring together.
+template <int WAVES>
+struct Parts {
+  float top[WAVES][2];   // largest teacher's and student's logit of the list
+  double list[WAVES][4];  // teacher's mass, sum of p (log p' - z / tau), student's mass, how many ids differ
+  float rest[WAVES][2];   // outside the list: maximum and sum relative to it
+  int twice;              // an id is listed several times
+};
+// Of a row: student's log-sum-exp is log_all + m_all / tau.
+struct Sums {
+  double m_all, s_all, p_scale, mass, c_rest, loss;
+  float m_rest;
+};
+
+// Outside the list: maximum and sum relative to it of one piece more, without the elements of `skip`.
+template <int N, typename V>
+__device__ __forceinline__ void add_piece(const V& v, int skip, float c, float& m, float& s) {
+  float f[N], m1 = m;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    f[e] = skip >> e & 1 ? -INFINITY : (float)v[e];
+    m1 = fmaxf(m1, f[e]);
+  }
+  s *= __builtin_amdgcn_exp2f((m - m1) * c);
+  m = m1;
+#pragma unroll
+  for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((f[e] - m) * c);
+}
+
+// The entries into LDS, the waves' maxima into parts.  logit(k, id): the student's; mark(id).
+template <int THREADS, typename L, typename M>
+__device__ __forceinline__ void read_list(const DistillArgs& a, int64_t row, const List& list,
+                                          Parts<THREADS / kWave>& parts, L logit, M mark) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  float top = -INFINITY, zmax = -INFINITY;
+  for (int k = tid; k < a.listed; k += THREADS) {
+    const int id = a.ids[row * a.ids_row + k];
+    const float t = teacher_at(a, row, k);
+    const bool held = (uint32_t)id < (uint32_t)a.vocab;
+    list.id[k] = held ? id : -1;
+    if (!held) continue;
+    const float z = logit(k, id);
+    list.z[k] = z;
+    list.t[k] = t;
+    top = fmaxf(top, t);
+    zmax = fmaxf(zmax, z);
+    mark(id);
+  }
+  if (wave * kWave < a.listed) {
+    top = wave_max(top);
+    zmax = wave_max(zmax);
+    if (lane == 0) {
+      parts.top[wave][0] = top;
+      parts.top[wave][1] = zmax;
+    }
+  }
+}
+
+// The list's sums, in 64 bits.  With teacher_lse log p' is log p, without it p and log p' are
+// relative to the largest.
+template <int THREADS>
+__device__ __forceinline__ void sum_list(const DistillArgs& a, int64_t row, const List& list,
+                                         Parts<THREADS / kWave>& parts, bool dup, double& zmax) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const double inv = 1.0 / (double)a.tau;
+  float top = -INFINITY, z0 = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) {
+    if (w * kWave >= a.listed) break;
+    top = fmaxf(top, parts.top[w][0]);
+    z0 = fmaxf(z0, parts.top[w][1]);
+  }
+  zmax = (double)fmaxf(z0, kLowest);  // (masked ones: -inf relative to it)
+  if (wave * kWave >= a.listed) return;
+  const double shift = a.teacher_lse != nullptr ? (double)a.teacher_lse[row] : top == -INFINITY ? 0.0 : (double)top * inv;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int k = tid; k < a.listed; k += THREADS) {
+    const int id = list.id[k];
+    if (id < 0) continue;
+    const double lp = (double)list.t[k] * inv - shift, p = exp(lp), z = ((double)list.z[k] - zmax) * inv;
+    list.p[k] = p;
+    sum[0] += p;
+    if (p != 0.0) sum[1] += p * (lp - z);
+    bool firstly = true;
+    if (dup)
+      for (int i = 0; i < k; ++i) firstly = firstly && list.id[i] != id;
+    if (firstly) {
+      sum[2] += exp(z);
+      sum[3] += 1.0;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    sum[k] = wave_sum64(sum[k]);
+    if (lane == 0) parts.list[wave][k] = sum[k];
+  }
+}
+
+// Loss and the gradient's factors from the list's sums and the rest's (m, s).
+template <int WAVES>
+__device__ __forceinline__ Sums join(const DistillArgs& a, const Parts<WAVES>& parts, double zmax, float m, double s) {
+  const double inv = 1.0 / (double)a.tau;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    if (w * kWave >= a.listed) break;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] += parts.list[w][k];
+  }
+  Sums r;
+  r.m_rest = m;
+  // relative to the larger of the two maxima
+  const double by = exp(-fabs((double)m - zmax) * inv), listed = zmax >= (double)m ? sum[2] : sum[2] != 0.0 ? sum[2] * by : 0.0;
+  const double rest = zmax >= (double)m ? (s != 0.0 ? s * by : 0.0) : s;
+  r.m_all = fmax((double)m, zmax);
+  r.s_all = listed + rest;
+  // (the list's logits are relative to zmax in the sum of p (log p - z / tau))
+  const double log_all = log(r.s_all) + (r.m_all - zmax) * inv;
+  r.p_scale = 1.0;
+  r.mass = sum[0];
+  if (a.teacher_lse != nullptr) {
+    const double p_rest = sum[3] == (double)a.vocab ? 0.0 : sum[0] == sum[0] ? fmax(1.0 - sum[0], 0.0) : sum[0];
+    const double q_rest = rest / r.s_all;
+    r.mass = sum[0] + p_rest;
+    r.loss = sum[0] != 0.0 ? sum[1] + sum[0] * log_all : 0.0;
+    if (p_rest != 0.0) r.loss += p_rest * log(p_rest / q_rest);
+    r.c_rest = q_rest * r.mass - p_rest;
+  } else if (sum[0] != 0.0) {
+    r.p_scale = 1.0 / sum[0];
+    r.mass = 1.0;
+    r.loss = sum[1] * r.p_scale - log(sum[0]) + log_all;
+    r.c_rest = rest / r.s_all;
+  } else {  // nothing is listed
+    r.loss = r.c_rest = 0.0;
+  }
+  r.c_rest = s != 0.0 ? r.c_rest / s : 0.0;
+  return r;
+}
+
+// Gradients of the listed ids of [from, from + count), over what was written there.
+template <typename T, int THREADS>
+__device__ __forceinline__ void write_list(const DistillArgs& a, T* out, const List& list, const Sums& r, bool dup,
+                                           double scale, int from, int count) {
+  const double inv = 1.0 / (double)a.tau;
+  for (int k = threadIdx.x; k < a.listed; k += THREADS) {
+    const int id = list.id[k];
+    if (id < 0 || (uint32_t)(id - from) >= (uint32_t)count) continue;
+    double p = list.p[k];
+    if (dup) {  // one that is listed several times: their sum
+      p = 0.0;
+      for (int i = 0; i < a.listed; ++i) p += list.id[i] == id ? list.p[i] : 0.0;
+    }
+    out[id] = (T)(float)((exp(((double)list.z[k] - r.m_all) * inv) / r.s_all * r.mass - p * r.p_scale) * scale);
+  }
+}
+
+template <int TY>
+__device__ __forceinline__ typename Elem<TY>::V gradient(const typename Elem<TY>::V& v, float m, float c, float by) {
+  typename Elem<TY>::V g;
+#pragma unroll
+  for (int e = 0; e < kPiece<TY>; ++e)
+    g[e] = (typename Elem<TY>::T)(__builtin_amdgcn_exp2f(((float)v[e] - m) * c) * by);
+  return g;
+}
+
+// Zero loss and gradient of a token that does not count, pieces [i0, i1) of the row.
+template <int TY, int THREADS>
+__device__ __forceinline__ void write_zeros(void* out, int i0, int i1, int vocab) {
+  typename Elem<TY>::V zero;
+#pragma unroll
+  for (int e = 0; e < kPiece<TY>; ++e) zero[e] = (typename Elem<TY>::T)0.f;
+  if (out != nullptr)
+    for (int i = i0 + threadIdx.x; i < i1; i += THREADS) store_piece<TY>(out, i * kPiece<TY>, vocab, zero);
+}
+
+__device__ __forceinline__ List list_at(const DistillArgs& a, uint8_t* lds) {
+  List list;
+  list.p = (double*)lds;
+  list.id = (int32_t*)(list.p + a.listed);
+  list.z = (float*)(list.id + a.listed);
+  list.t = list.z + a.listed;
+  return list;
+}
+constexpr int kListBytes = 20;  // of LDS an entry
+
+// One workgroup a row, NV pieces of 16 bytes a thread in registers.  A row's last piece ends at
+// its end and may begin inside the one before: what both hold counts for the first and is written
+// alike by both.
+template <int TY, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS, 4) k_distill(DistillArgs a) {
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
-  constexpr int N = kPiece<TY>, kAll = (1 << N) - 1;
-  constexpr float kLowest = -3.402823466e38f;
+  constexpr int N = kPiece<TY>, kAll = (1 << N) - 1, kWaves = THREADS / kWave;
   extern __shared__ __align__(16) uint8_t lds[];
-  double* const p_of = (double*)lds;                   // [listed]
-  int32_t* const id_of = (int32_t*)(p_of + a.listed);  // [listed], -1: no entry
-  float* const z_of = (float*)(id_of + a.listed);      // [listed]
-  uint32_t* const bits = (uint32_t*)(z_of + a.listed);  // a bit per id: listed, or past the vocabulary
-  __shared__ double red[2][kWaves][5];
-  __shared__ int twice;
+  __shared__ Parts<kWaves> parts;
+  const List list = list_at(a, lds);
+  uint32_t* const bits = (uint32_t*)(list.t + a.listed);  // a bit per id: listed, or past the vocabulary
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int64_t row = blockIdx.x;
   const T* const in = (const T*)a.logits + row * a.logits_row;
   T* const out = a.grad != nullptr ? (T*)a.grad + row * a.grad_row : nullptr;
   const int pieces = (a.vocab + N - 1) / N;
-  auto place = [&](int i) { return NV > 0 ? min(i * N, a.vocab - N) : i * N; };
   const float weight = a.weights != nullptr ? a.weights[row] : 1.f;
-  if (weight == 0.f) {  // a token that does not count: its logits are not looked at
+  if (weight == 0.f) {  // its logits are not looked at
     if (tid == 0) a.loss[row] = 0.f;
-    V zero;
-#pragma unroll
-    for (int e = 0; e < N; ++e) zero[e] = (T)0.f;
-    if (out != nullptr)
-      for (int i = tid; i < pieces; i += kThreads) store_piece<TY>(out, place(i), a.vocab, zero);
-    return;
+    return write_zeros<TY, THREADS>(out, 0, pieces, a.vocab);
   }
-  V x[NV > 0 ? NV : 1];
-  if constexpr (NV > 0) {
+  auto place = [&](int i) { return min(i * N, a.vocab - N); };
+  V x[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) x[j] = *(const V*)(in + place(tid + j * kThreads));
-  }
+  for (int j = 0; j < NV; ++j) x[j] = *(const V*)(in + place(tid + j * THREADS));
   const int words = (a.vocab + 31) / 32;
-  for (int i = tid; i < words; i += kThreads) bits[i] = i == words - 1 && (a.vocab & 31) != 0 ? ~0u << (a.vocab & 31) : 0u;
-  if (tid == 0) twice = 0;
+  for (int i = tid; i < words; i += THREADS) bits[i] = i == words - 1 && (a.vocab & 31) != 0 ? ~0u << (a.vocab & 31) : 0u;
+  if (tid == 0) parts.twice = 0;
   lds_barrier();
-  const float c = kLog2e / a.tau;
-  const double inv = 1.0 / (double)a.tau;
-  double top = -INFINITY, zmax = -INFINITY;
-  for (int k = tid; k < a.listed; k += kThreads) {
-    const int id = a.ids[row * a.ids_row + k];
-    const bool held = (uint32_t)id < (uint32_t)a.vocab;
-    id_of[k] = held ? id : -1;
-    if (!held) continue;
-    const float z = (float)in[id];
-    const double t = teacher_at(a, row, k) * inv;
-    z_of[k] = z;
-    p_of[k] = t;
-    top = fmax(top, t);
-    zmax = fmax(zmax, (double)z);
-    if (atomicOr(&bits[id / 32], 1u << (id % 32)) >> (id % 32) & 1) twice = 1;
-  }
+  read_list<THREADS>(a, row, list, parts, [&](int, int id) { return (float)in[id]; }, [&](int id) {
+    if (atomicOr(&bits[id / 32], 1u << (id % 32)) >> (id % 32) & 1) parts.twice = 1;
+  });
   lds_barrier();
+  const bool dup = parts.twice != 0;
+  double zmax;
+  sum_list<THREADS>(a, row, list, parts, dup, zmax);
 
-  // Outside the list: this thread's maximum and the sum relative to it.
   int skip_last = 0;  // elements of the last piece that do not count
   {
     const int at = place(pieces - 1);
+#pragma unroll
     for (int e = 0; e < N; ++e)
-      skip_last |= (int)(at + e < (pieces - 1) * N || at + e >= a.vocab || (bits[(at + e) / 32] >> ((at + e) % 32) & 1)) << e;
+      skip_last |= (int)(at + e < (pieces - 1) * N || (bits[(at + e) / 32] >> ((at + e) % 32) & 1)) << e;
   }
+  const float c = kLog2e / a.tau;
   float m = kLowest, s = 0.f;
-  auto add = [&](const V& v, int i) {
-    int b = (int)(((const uint8_t*)bits)[min(i, pieces - 1) * N / 8] >> (i * N % 8)) & kAll;
-    b = i < pieces - 1 ? b : i == pieces - 1 ? skip_last : kAll;
-    float f[N], m1 = m;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      f[e] = b >> e & 1 ? -INFINITY : (float)v[e];
-      m1 = fmaxf(m1, f[e]);
-    }
-    s *= __builtin_amdgcn_exp2f((m - m1) * c);
-    m = m1;
-#pragma unroll
-    for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((f[e] - m) * c);
-  };
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (NV > 4) asm volatile("" : "+v"(x[j]), "+v"(s), "+v"(m));  // (all at once would take too many registers)
-      add(x[j], tid + j * kThreads);
-    }
-  } else {
-    for (int i = tid; i < pieces; i += kThreads) add(load_piece<TY>(in, i * N, a.vocab), i);
+  for (int j = 0; j < NV; ++j) {
+    if (NV > 4) asm volatile("" : "+v"(x[j]), "+v"(s), "+v"(m));  // (all at once would take too many registers)
+    const int i = tid + j * THREADS;
+    int skip = (int)(((const uint8_t*)bits)[min(i, pieces - 1) * N / 8] >> (i * N % 8)) & kAll;
+    skip = i < pieces - 1 ? skip : i == pieces - 1 ? skip_last : kAll;
+    add_piece<N>(x[j], skip, c, m, s);
   }
-  // The row's maxima: outside the list, in it, of the teacher.
-  double most[3] = {(double)m, zmax, top};
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) most[k] = fmax(most[k], __shfl_xor(most[k], o));
-    if (lane == 0) red[0][wave][k] = most[k];
+  const float m_wave = wave_max(m);
+  s = wave_sum(s * __builtin_amdgcn_exp2f((m - m_wave) * c));
+  if (lane == 0) {
+    parts.rest[wave][0] = m_wave;
+    parts.rest[wave][1] = s;
   }
   lds_barrier();
-#pragma unroll 1
+  m = kLowest;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, parts.rest[w][0]);
+  double s_rest = 0.0;
+#pragma unroll
   for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-    for (int k = 0; k < 3; ++k) most[k] = fmax(most[k], red[0][w][k]);
-  const double m_rest = most[0], m_all = fmax(most[0], most[1]);
-  // The list: teacher's mass, sum of p (log p' - z / tau), student's mass; the rest's sum; how
-  // many ids are listed.
-  // With lse log p' is log p, without it p and log p' are relative to the largest.
-  const double lse = a.teacher_lse != nullptr ? (double)a.teacher_lse[row] : most[2] == -INFINITY ? 0.0 : most[2];
-  const bool dup = twice != 0;
-  double sum[5] = {0.0, 0.0, 0.0, (double)s * exp(((double)m - m_rest) * inv), 0.0};
-  for (int k = tid; k < a.listed; k += kThreads) {
-    const int id = id_of[k];
-    if (id < 0) continue;
-    const double lp = p_of[k] - lse, p = exp(lp), z = ((double)z_of[k] - m_all) * inv;
-    p_of[k] = p;
-    sum[0] += p;
-    if (p != 0.0) sum[1] += p * (lp - z);
-    bool firstly = true;
-    if (dup)
-      for (int i = 0; i < k; ++i) firstly = firstly && id_of[i] != id;
-    if (firstly) {
-      sum[2] += exp(z);
-      sum[4] += 1.0;
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 5; ++k) {
-    sum[k] = wave_sum64(sum[k]);
-    if (lane == 0) red[1][wave][k] = sum[k];
-    sum[k] = 0.0;
-  }
-  lds_barrier();  // (p_of too)
-#pragma unroll 1
-  for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-    for (int k = 0; k < 5; ++k) sum[k] += red[1][w][k];
-  const double s_rest = sum[3], shift = exp((m_rest - m_all) * inv);
-  const double s_all = sum[2] + (s_rest != 0.0 ? s_rest * shift : 0.0), log_all = log(s_all);
-  double p_scale = 1.0, mass = sum[0], c_rest = 1.0, loss;
-  if (a.teacher_lse != nullptr) {
-    const double p_rest = sum[4] == (double)a.vocab ? 0.0 : sum[0] == sum[0] ? fmax(1.0 - sum[0], 0.0) : sum[0];
-    const double q_rest = s_rest != 0.0 ? s_rest * shift / s_all : 0.0;
-    mass = sum[0] + p_rest;
-    loss = sum[1] + sum[0] * log_all;
-    if (p_rest != 0.0) loss += p_rest * log(p_rest / q_rest);
-    c_rest = q_rest * mass - p_rest;
-  } else if (sum[0] != 0.0) {
-    p_scale = 1.0 / sum[0];
-    mass = 1.0;
-    loss = sum[1] * p_scale - log(sum[0]) + log_all;
-    c_rest = s_rest * shift / s_all;
-  } else {  // nothing is listed
-    loss = c_rest = 0.0;
-  }
-  if (tid == 0) a.loss[row] = (float)loss;
+    s_rest += (double)(parts.rest[w][1] * __builtin_amdgcn_exp2f((parts.rest[w][0] - m) * c));
+  const Sums r = join<kWaves>(a, parts, zmax, m, s_rest);
+  if (tid == 0) a.loss[row] = (float)r.loss;
   if (out == nullptr) return;
-  const double scale = (double)weight * inv;
-  const float by = s_rest != 0.0 ? (float)(c_rest / s_rest * scale) : 0.f, m0 = (float)m_rest;
-  auto write = [&](const V& v, int i) {
-    V g;
+  const double scale = (double)weight / (double)a.tau;
+  const float by = (float)(r.c_rest * scale);
 #pragma unroll
-    for (int e = 0; e < N; ++e) g[e] = (T)(__builtin_amdgcn_exp2f(((float)v[e] - m0) * c) * by);
-    if constexpr (NV > 0) *(V*)(out + place(i)) = g;
-    else store_piece<TY>(out, i * N, a.vocab, g);
-  };
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      asm volatile("" : "+v"(x[j]));  // (otherwise the converted elements are kept, which spills)
-      if (tid + j * kThreads < pieces) write(x[j], tid + j * kThreads);
-    }
-  } else {
-    for (int i = tid; i < pieces; i += kThreads) write(load_piece<TY>(in, i * N, a.vocab), i);
+  for (int j = 0; j < NV; ++j) {
+    asm volatile("" : "+v"(x[j]));  // (otherwise the converted elements are kept, which spills)
+    const int i = tid + j * THREADS;
+    if (i < pieces) *(V*)(out + place(i)) = gradient<TY>(x[j], m, c, by);
   }
   __syncthreads();  // the listed ids' gradients go over what was written there
-  for (int k = tid; k < a.listed; k += kThreads) {
-    const int id = id_of[k];
-    if (id < 0) continue;
-    double p = p_of[k];
-    if (dup) {  // one that is listed several times: their sum
-      p = 0.0;
-      for (int i = 0; i < a.listed; ++i) p += id_of[i] == id ? p_of[i] : 0.0;
-    }
-    out[id] = (T)(float)((exp(((double)z_of[k] - m_all) * inv) / s_all * mass - p * p_scale) * scale);
-  }
+  write_list<T, THREADS>(a, out, list, r, dup, scale, 0, a.vocab);
 }
 
-template <int TY, int kThreads, int NV>
-hipError_t launch(const DistillArgs& a, hipStream_t s) {
-  const int lds = a.listed * 16 + (a.vocab + 31) / 32 * 4;
-  const hipError_t e = allow_dynamic_lds((const void*)k_distill<TY, kThreads, NV>, lds);
+// Rows that are cut: NV pieces a thread of a slice.  First the slices' maxima and sums outside the
+// list, and the logits of the listed ids (which the gradient may overwrite) ...
+constexpr int kSliceThreads = 256;
+
+template <int TY, int NV>
+__global__ void __launch_bounds__(kSliceThreads) k_distill_slices(DistillArgs a) {
+  typedef typename Elem<TY>::T T;
+  typedef typename Elem<TY>::V V;
+  constexpr int N = kPiece<TY>, kAll = (1 << N) - 1, THREADS = kSliceThreads, kWaves = THREADS / kWave;
+  constexpr int kCount = NV * THREADS * N, kWords = kCount / 32;
+  __shared__ uint32_t bits[kWords];
+  __shared__ float rest[kWaves][2];
+  __shared__ int twice;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int64_t row = a.row0 + blockIdx.y;
+  const T* const in = (const T*)a.logits + row * a.logits_row;
+  const int from = blockIdx.x * kCount;
+  if (a.weights != nullptr && a.weights[row] == 0.f) return;
+  V x[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = from + (tid + j * THREADS) * N;
+    x[j] = load_piece<TY>(in, min(at, a.vocab), a.vocab);
+  }
+  // (elements past the end count as listed)
+  for (int i = tid; i < kWords; i += THREADS) {
+    const int left = a.vocab - from - i * 32;
+    bits[i] = left >= 32 ? 0u : left <= 0 ? ~0u : ~0u << left;
+  }
+  if (tid == 0) twice = 0;
+  lds_barrier();
+  for (int k = tid; k < a.listed; k += THREADS) {
+    const int id = a.ids[row * a.ids_row + k];
+    const uint32_t at = (uint32_t)(id - from);
+    if ((uint32_t)id < (uint32_t)a.vocab && at < (uint32_t)kCount) {
+      if (atomicOr(&bits[at / 32], 1u << (at % 32)) >> (at % 32) & 1) twice = 1;
+      a.listed_logits[row * a.listed + k] = (float)in[id];
+    }
+  }
+  lds_barrier();
+  const float c = kLog2e / a.tau;
+  float m = kLowest, s = 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (NV > 4) asm volatile("" : "+v"(x[j]), "+v"(s), "+v"(m));  // (all at once would take too many registers)
+    const int i = tid + j * THREADS;
+    add_piece<N>(x[j], (int)(((const uint8_t*)bits)[i * N / 8] >> (i * N % 8)) & kAll, c, m, s);
+  }
+  const float m_wave = wave_max(m);
+  s = wave_sum(s * __builtin_amdgcn_exp2f((m - m_wave) * c));
+  if (lane == 0) {
+    rest[wave][0] = m_wave;
+    rest[wave][1] = s;
+  }
+  lds_barrier();
+  if (tid != 0) return;
+  m = kLowest;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, rest[w][0]);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) s += rest[w][1] * __builtin_amdgcn_exp2f((rest[w][0] - m) * c);
+  a.slices[row * gridDim.x + blockIdx.x] = DistillSlice{m, s, twice};
+}
+
+// ... then a slice's gradient, from all slices' sums and the list, which every slice computes for itself.
+template <int TY, int NV>
+__global__ void __launch_bounds__(kSliceThreads) k_distill_grad(DistillArgs a) {
+  typedef typename Elem<TY>::T T;
+  typedef typename Elem<TY>::V V;
+  constexpr int N = kPiece<TY>, THREADS = kSliceThreads, kWaves = THREADS / kWave;
+  extern __shared__ __align__(16) uint8_t lds[];
+  __shared__ Parts<kWaves> parts;
+  const List list = list_at(a, lds);
+  const int tid = threadIdx.x, lane = tid % kWave, slices = gridDim.x;
+  const int64_t row = a.row0 + blockIdx.y;
+  const T* const in = (const T*)a.logits + row * a.logits_row;
+  T* const out = a.grad != nullptr ? (T*)a.grad + row * a.grad_row : nullptr;
+  const int first = blockIdx.x * NV * THREADS, from = first * N;
+  const float weight = a.weights != nullptr ? a.weights[row] : 1.f;
+  if (weight == 0.f) {
+    if (tid == 0 && blockIdx.x == 0) a.loss[row] = 0.f;
+    return write_zeros<TY, THREADS>(out, first, min((a.vocab + N - 1) / N, first + NV * THREADS), a.vocab);
+  }
+  V x[NV];
+  if (out != nullptr) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = from + (tid + j * THREADS) * N;
+      x[j] = load_piece<TY>(in, min(at, a.vocab), a.vocab);
+    }
+  }
+  DistillSlice own{kLowest, 0.f, 0};  // (a lane has a slice)
+  if (lane < slices) own = a.slices[row * slices + lane];
+  read_list<THREADS>(a, row, list, parts, [&](int k, int) { return a.listed_logits[row * a.listed + k]; }, [](int) {});
+  lds_barrier();
+  const bool dup = __ballot(own.twice) != 0;
+  double zmax;
+  sum_list<THREADS>(a, row, list, parts, dup, zmax);
+  const float c = kLog2e / a.tau, m = wave_max(own.m);
+  const double s_rest = wave_sum64((double)(own.s * __builtin_amdgcn_exp2f((own.m - m) * c)));
+  lds_barrier();
+  const Sums r = join<kWaves>(a, parts, zmax, m, s_rest);
+  if (tid == 0 && blockIdx.x == 0) a.loss[row] = (float)r.loss;
+  if (out == nullptr) return;
+  const double scale = (double)weight / (double)a.tau;
+  const float by = (float)(r.c_rest * scale);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = from + (tid + j * THREADS) * N;
+    if (at < a.vocab) store_piece<TY>(out, at, a.vocab, gradient<TY>(x[j], m, c, by));
+  }
+  __syncthreads();  // the listed ids' gradients go over what was written there
+  write_list<T, THREADS>(a, out, list, r, dup, scale, from, NV * THREADS * N);
+}
+
+template <int TY, int THREADS, int NV>
+hipError_t launch_rows(const DistillArgs& a, hipStream_t s) {
+  const int lds = a.listed * kListBytes + (a.vocab + 31) / 32 * 4;
+  const hipError_t e = allow_dynamic_lds((const void*)k_distill<TY, THREADS, NV>, lds);
   if (e != hipSuccess) return e;
-  k_distill<TY, kThreads, NV><<<(unsigned)a.rows, kThreads, lds, s>>>(a);
+  k_distill<TY, THREADS, NV><<<(unsigned)a.rows, THREADS, lds, s>>>(a);
   return hipGetLastError();
+}
+
+template <int TY, int NV>
+hipError_t launch_slices(DistillArgs a, int slices, hipStream_t s) {
+  const int lds = a.listed * kListBytes;
+  hipError_t e = allow_dynamic_lds((const void*)k_distill_grad<TY, NV>, lds);
+  for (a.row0 = 0; a.row0 < a.rows && e == hipSuccess; a.row0 += 65535) {
+    const dim3 grid((unsigned)slices, (unsigned)(a.rows - a.row0 < 65535 ? a.rows - a.row0 : 65535));
+    k_distill_slices<TY, NV><<<grid, kSliceThreads, 0, s>>>(a);
+    k_distill_grad<TY, NV><<<grid, kSliceThreads, lds, s>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 template <int TY>
 hipError_t launch_typed(const DistillArgs& a, hipStream_t s) {
-  if (a.vocab < kPiece<TY>) return launch<TY, 256, 0>(a, s);
+  const DistillCut cut = distill_cut(a.rows, a.vocab, TY);
+  if (cut.slices > 0) return cut.pieces == 8 ? launch_slices<TY, 8>(a, cut.slices, s) : launch_slices<TY, 2>(a, cut.slices, s);
   const int pieces = (a.vocab + kPiece<TY> - 1) / kPiece<TY>;
-  if (pieces <= 256) return launch<TY, 256, 1>(a, s);
-  if (pieces <= 4 * 256) return launch<TY, 256, 4>(a, s);
-  if (pieces <= 16 * 256) return launch<TY, 256, 16>(a, s);
-  if (pieces <= 16 * 512) return launch<TY, 512, 16>(a, s);
-  if (pieces <= 16 * 1024) return launch<TY, 1024, 16>(a, s);
-  return launch<TY, 1024, 0>(a, s);
+  if (pieces <= 256) return launch_rows<TY, 256, 1>(a, s);
+  if (pieces <= 4 * 256) return launch_rows<TY, 256, 4>(a, s);
+  if (pieces <= 16 * 256) return launch_rows<TY, 256, 16>(a, s);
+  return launch_rows<TY, 512, 16>(a, s);
 }
 
 }  // namespace
+
+DistillCut distill_cut(int64_t rows, int64_t vocab, int dtype) {
+  const int n = dtype == kF32 ? 4 : 8;
+  const int64_t pieces = (vocab + n - 1) / n;
+  if (vocab >= n && pieces <= 16 * 512 && rows >= 2 * num_cus()) return {0, 0};
+  const int64_t wide = (pieces + 8 * kSliceThreads - 1) / (8 * kSliceThreads);
+  const int64_t narrow = (pieces + 2 * kSliceThreads - 1) / (2 * kSliceThreads);
+  if (narrow <= kWave && rows * wide < 4 * num_cus()) return {(int)narrow, 2};
+  return {(int)wide, 8};
+}
 
 hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s) {
   if (dtype == kF16) return launch_typed<kF16>(a, s);

@@ -69,10 +69,17 @@ __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
   for (int s = 1; s < kWave; s <<= 1) v += __shfl_xor((unsigned long long)v, s);
   return v;
 }
+// The largest over the lanes, in every lane (rows of 16 by DPP, as wave_sum).
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) v = fmaxf(v, __shfl_xor(v, s));
-  return v;
+  auto move = [&](auto c) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(c)::value, 0xF, 0xF, true));
+  };
+  v = fmaxf(v, move(IntC<0xB1>()));
+  v = fmaxf(v, move(IntC<0x4E>()));
+  v = fmaxf(v, move(IntC<0x141>()));
+  v = fmaxf(v, move(IntC<0x140>()));
+  auto lane = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
+  return fmaxf(fmaxf(lane(0), lane(16)), fmaxf(lane(32), lane(48)));
 }
 
 }  // namespace aqlm

@@ -69,7 +69,23 @@ struct DistillArgs {
   int64_t logits_row, teacher_row, ids_row, grad_row, rows;
   int32_t vocab, listed, teacher_dtype;
   float tau;
+  // workspace, where rows are cut
+  struct DistillSlice* slices;  // [rows][slices]
+  float* listed_logits;         // [rows][listed]
+  int64_t row0;                 // a launch's first
 };
+
+// What a slice of a row has outside the list: largest logit, sum relative to it; and whether an
+// id of it is listed twice.
+struct DistillSlice {
+  float m, s;
+  int32_t twice;
+};
+// Slices of a row (0: rows are not cut), pieces of 16 bytes a thread of a slice has.
+struct DistillCut {
+  int slices, pieces;
+};
+DistillCut distill_cut(int64_t rows, int64_t vocab, int dtype);
 
 constexpr int kDistillMaxListed = 2048;
 constexpr int kDistillMaxVocab = 1 << 19;

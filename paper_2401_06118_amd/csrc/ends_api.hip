@@ -195,10 +195,19 @@ int aqlm_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
   return status_of(aqlm::launch_norm_grad(a, dtype, (hipStream_t)stream));
 }
 
+size_t aqlm_distill_loss_workspace_bytes(int64_t rows, int64_t vocab, int64_t listed, int32_t dtype) {
+  if (rows <= 0 || rows > aqlm::kDistillMaxRows || vocab <= 0 || vocab > aqlm::kDistillMaxVocab || listed <= 0 ||
+      listed > aqlm::kDistillMaxListed || !known_dtype(dtype))
+    return 0;
+  const aqlm::DistillCut cut = aqlm::distill_cut(rows, vocab, dtype);
+  return cut.slices == 0 ? 0 : (size_t)rows * ((size_t)cut.slices * sizeof(aqlm::DistillSlice) + (size_t)listed * 4);
+}
+
 int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, const void* teacher,
                       int64_t teacher_stride, int32_t teacher_dtype, const int32_t* ids, int64_t ids_stride,
                       const float* teacher_lse, const float* weights, float temperature, float* loss, void* grad,
-                      int64_t grad_stride, int64_t rows, int64_t vocab, int64_t listed, void* stream) {
+                      int64_t grad_stride, int64_t rows, int64_t vocab, int64_t listed, void* workspace,
+                      size_t workspace_bytes, void* stream) {
   if (!known_dtype(dtype) || !known_dtype(teacher_dtype)) return AQLM_ERR_UNSUPPORTED;
   if (rows < 0 || rows > aqlm::kDistillMaxRows || vocab <= 0 || vocab > aqlm::kDistillMaxVocab || listed <= 0 ||
       listed > aqlm::kDistillMaxListed || !rows_in(logits_stride) || !rows_in(teacher_stride) || !rows_in(ids_stride) ||
@@ -211,6 +220,10 @@ int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, 
     return AQLM_ERR_ALIGN;
   for (const void* p : {(const void*)ids, (const void*)teacher_lse, (const void*)weights, (const void*)loss})
     if (!multiple(p, 4)) return AQLM_ERR_ALIGN;
+  const size_t need = aqlm_distill_loss_workspace_bytes(rows, vocab, listed, dtype);
+  if (need > 0 && !workspace) return AQLM_ERR_NULL;
+  if (need > 0 && !multiple(workspace, 16)) return AQLM_ERR_ALIGN;
+  if (workspace_bytes < need) return AQLM_ERR_WORKSPACE;
   aqlm::DistillArgs a{};
   a.logits = logits;
   a.teacher = teacher;
@@ -228,6 +241,10 @@ int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, 
   a.listed = (int32_t)listed;
   a.teacher_dtype = teacher_dtype;
   a.tau = temperature;
+  if (need > 0) {
+    a.slices = static_cast<aqlm::DistillSlice*>(workspace);
+    a.listed_logits = reinterpret_cast<float*>(a.slices + rows * aqlm::distill_cut(rows, vocab, dtype).slices);
+  }
   return status_of(aqlm::launch_distill(a, dtype, (hipStream_t)stream));
 }
 

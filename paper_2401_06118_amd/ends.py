@@ -98,8 +98,8 @@ def distill_loss(logits, teacher_logits, teacher_ids, *, teacher_lse=None, tempe
     r = (block._ext or _binding()).distill_loss(logits, teacher_logits, teacher_ids, teacher_lse, weights, temperature,
                                                 grad, out, _handle(logits, stream))
     if stream is not None:
-        _made(stream, *(r if out is None else r[:1]))
-    return r
+        _made(stream, *(r if out is None else r[::2]))
+    return r[:2]
 
 
 def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None, return_logprob: bool = False,

@@ -94,9 +94,16 @@ def test_layer_norm_backward(lib):
 
 def test_distill_loss(lib):
     def call(z=P, zs=1000, dtype=F16, t=P, tstride=8, tt=F32, ids=P, ids_s=8, lse=None, w=None, tau=1.0, loss=P, grad=Q,
-             gs=1000, rows=3, vocab=1000, listed=8):
+             gs=1000, rows=3, vocab=1000, listed=8, ws=P, size=1 << 20):
         return lib.aqlm_distill_loss(z, zs, dtype, t, tstride, tt, ids, ids_s, lse, w, tau, loss, grad, gs, rows, vocab,
-                                     listed, None)
+                                     listed, ws, size, None)
+
+    room = lib.aqlm_distill_loss_workspace_bytes
+    assert 0 < room(3, 1000, 8, F16) < room(3, 1000, 9, F16) and room(1 << 20, 1000, 8, F16) == 0
+    assert [room(*v) for v in ((0, 1000, 8, F16), (3, 0, 8, F16), (3, 1000, 0, F16), (3, 1000, 8, 5))] == [0] * 4
+    refused(call, NULL, ws=[None])
+    refused(call, WORKSPACE, size=[0, room(3, 1000, 8, F16) - 1])
+    refused(call, ALIGN, ws=[P + 8])
 
     refused(call, NULL, z=[None], t=[None], ids=[None], loss=[None])
     refused(call, SHAPE, zs=[-1], tstride=[-1], ids_s=[-1], gs=[-1, 999], rows=[-1, 1 << 22], vocab=[0, (1 << 19) + 1],
