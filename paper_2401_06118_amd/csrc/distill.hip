@@ -99,9 +99,10 @@ __device__ __forceinline__ void read_list(const DistillArgs& a, int64_t row, con
 
 // The list's sums, in 64 bits.  With teacher_lse log p' is log p, without it p and log p' are
 // relative to the largest.
-template <int THREADS>
+// firstly(k, id): whether entry k is the first of its id.
+template <int THREADS, typename F>
 __device__ __forceinline__ void sum_list(const DistillArgs& a, int64_t row, const List& list,
-                                         Parts<THREADS / kWave>& parts, bool dup, double& zmax) {
+                                         Parts<THREADS / kWave>& parts, double& zmax, F firstly) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const double inv = 1.0 / (double)a.tau;
   float top = -INFINITY, z0 = -INFINITY;
@@ -122,10 +123,7 @@ __device__ __forceinline__ void sum_list(const DistillArgs& a, int64_t row, cons
     list.p[k] = p;
     sum[0] += p;
     if (p != 0.0) sum[1] += p * (lp - z);
-    bool firstly = true;
-    if (dup)
-      for (int i = 0; i < k; ++i) firstly = firstly && list.id[i] != id;
-    if (firstly) {
+    if (firstly(k, id)) {
       sum[2] += exp(z);
       sum[3] += 1.0;
     }
@@ -137,17 +135,21 @@ __device__ __forceinline__ void sum_list(const DistillArgs& a, int64_t row, cons
   }
 }
 
-// Loss and the gradient's factors from the list's sums and the rest's (m, s).
 template <int WAVES>
-__device__ __forceinline__ Sums join(const DistillArgs& a, const Parts<WAVES>& parts, double zmax, float m, double s) {
-  const double inv = 1.0 / (double)a.tau;
-  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+__device__ __forceinline__ void add_waves(const DistillArgs& a, const Parts<WAVES>& parts, double (&sum)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = 0.0;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) {
     if (w * kWave >= a.listed) break;
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum[k] += parts.list[w][k];
   }
+}
+
+// Loss and the gradient's factors from the list's sums and the rest's (m, s).
+__device__ __forceinline__ Sums join(const DistillArgs& a, const double (&sum)[4], double zmax, float m, double s) {
+  const double inv = 1.0 / (double)a.tau;
   Sums r;
   r.m_rest = m;
   // relative to the larger of the two maxima
@@ -178,21 +180,10 @@ __device__ __forceinline__ Sums join(const DistillArgs& a, const Parts<WAVES>& p
   return r;
 }
 
-// Gradients of the listed ids of [from, from + count), over what was written there.
-template <typename T, int THREADS>
-__device__ __forceinline__ void write_list(const DistillArgs& a, T* out, const List& list, const Sums& r, bool dup,
-                                           double scale, int from, int count) {
-  const double inv = 1.0 / (double)a.tau;
-  for (int k = threadIdx.x; k < a.listed; k += THREADS) {
-    const int id = list.id[k];
-    if (id < 0 || (uint32_t)(id - from) >= (uint32_t)count) continue;
-    double p = list.p[k];
-    if (dup) {  // one that is listed several times: their sum
-      p = 0.0;
-      for (int i = 0; i < a.listed; ++i) p += list.id[i] == id ? list.p[i] : 0.0;
-    }
-    out[id] = (T)(float)((exp(((double)list.z[k] - r.m_all) * inv) / r.s_all * r.mass - p * r.p_scale) * scale);
-  }
+// A listed id's gradient.
+template <typename T>
+__device__ __forceinline__ T listed_gradient(const Sums& r, float z, double p, double inv, double scale) {
+  return (T)(float)((exp(((double)z - r.m_all) * inv) / r.s_all * r.mass - p * r.p_scale) * scale);
 }
 
 template <int TY>
@@ -260,7 +251,12 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(DistillArgs a) {
   lds_barrier();
   const bool dup = parts.twice != 0;
   double zmax;
-  sum_list<THREADS>(a, row, list, parts, dup, zmax);
+  sum_list<THREADS>(a, row, list, parts, zmax, [&](int k, int id) {
+    bool first = true;
+    if (dup)
+      for (int i = 0; i < k; ++i) first = first && list.id[i] != id;
+    return first;
+  });
 
   int skip_last = 0;  // elements of the last piece that do not count
   {
@@ -293,7 +289,9 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(DistillArgs a) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w)
     s_rest += (double)(parts.rest[w][1] * __builtin_amdgcn_exp2f((parts.rest[w][0] - m) * c));
-  const Sums r = join<kWaves>(a, parts, zmax, m, s_rest);
+  double sum[4];
+  add_waves<kWaves>(a, parts, sum);
+  const Sums r = join(a, sum, zmax, m, s_rest);
   if (tid == 0) a.loss[row] = (float)r.loss;
   if (out == nullptr) return;
   const double scale = (double)weight / (double)a.tau;
@@ -305,12 +303,75 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(DistillArgs a) {
     if (i < pieces) *(V*)(out + place(i)) = gradient<TY>(x[j], m, c, by);
   }
   __syncthreads();  // the listed ids' gradients go over what was written there
-  write_list<T, THREADS>(a, out, list, r, dup, scale, 0, a.vocab);
+  const double inv = 1.0 / (double)a.tau;
+  for (int k = tid; k < a.listed; k += THREADS) {
+    const int id = list.id[k];
+    if (id < 0) continue;
+    double p = list.p[k];
+    if (dup) {  // one that is listed several times: their sum
+      p = 0.0;
+      for (int i = 0; i < a.listed; ++i) p += list.id[i] == id ? list.p[i] : 0.0;
+    }
+    out[id] = listed_gradient<T>(r, list.z[k], p, inv, scale);
+  }
 }
 
-// Rows that are cut: NV pieces a thread of a slice.  First the slices' maxima and sums outside the
-// list, and the logits of the listed ids (which the gradient may overwrite) ...
+// Rows that are cut: NV pieces a thread of a slice.  One launch makes the slices' maxima and sums
+// outside the list and, by a workgroup of its own, the list's; another writes the gradient.
 constexpr int kSliceThreads = 256;
+
+// Slots of a table of the listed ids.
+inline __host__ __device__ int table_slots(int listed) {
+  int n = 64;
+  while (n < 2 * listed) n <<= 1;
+  return n;
+}
+
+template <int TY>
+__device__ __forceinline__ void sum_row_list(const DistillArgs& a, int64_t row, uint8_t* lds) {
+  typedef typename Elem<TY>::T T;
+  constexpr int THREADS = kSliceThreads;
+  __shared__ Parts<THREADS / kWave> parts;
+  const List list = list_at(a, lds);
+  // the first entry of an id: by a table of ids, linear probing
+  const int slots = table_slots(a.listed), tid = threadIdx.x;
+  int32_t* const key = (int32_t*)(list.t + a.listed);  // [slots]: id, -1 free
+  int32_t* const first = key + slots;                  // [slots]: its first entry
+  const T* const in = (const T*)a.logits + row * a.logits_row;
+  for (int i = tid; i < slots; i += THREADS) {
+    key[i] = -1;
+    first[i] = INT32_MAX;
+  }
+  if (tid == 0) parts.twice = 0;
+  lds_barrier();
+  auto slot_of = [&](int id) {  // (at most half of the slots are taken)
+    int at = (int)((uint32_t)id * 2654435761u) & (slots - 1);
+    for (;;) {
+      const int was = atomicCAS(&key[at], -1, id);
+      if (was == -1 || was == id) return at;
+      at = (at + 1) & (slots - 1);
+    }
+  };
+  read_list<THREADS>(a, row, list, parts, [&](int, int id) { return (float)in[id]; }, [&](int) {});
+  lds_barrier();
+  for (int k = tid; k < a.listed; k += THREADS)
+    if (list.id[k] >= 0 && atomicMin(&first[slot_of(list.id[k])], k) != INT32_MAX) parts.twice = 1;
+  lds_barrier();
+  double zmax;
+  sum_list<THREADS>(a, row, list, parts, zmax, [&](int k, int id) { return first[slot_of(id)] == k; });
+  for (int k = tid; k < a.listed; k += THREADS) {
+    if (list.id[k] < 0) continue;
+    a.listed_mass[row * a.listed + k] = list.p[k];
+    a.listed_logits[row * a.listed + k] = list.z[k];
+  }
+  lds_barrier();
+  if (tid != 0) return;
+  DistillRow r;
+  add_waves<THREADS / kWave>(a, parts, r.sum);
+  r.zmax = zmax;
+  r.twice = parts.twice;
+  a.row_lists[row] = r;
+}
 
 template <int TY, int NV>
 __global__ void __launch_bounds__(kSliceThreads) k_distill_slices(DistillArgs a) {
@@ -318,14 +379,15 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_slices(DistillArgs a)
   typedef typename Elem<TY>::V V;
   constexpr int N = kPiece<TY>, kAll = (1 << N) - 1, THREADS = kSliceThreads, kWaves = THREADS / kWave;
   constexpr int kCount = NV * THREADS * N, kWords = kCount / 32;
+  extern __shared__ __align__(16) uint8_t lds[];
   __shared__ uint32_t bits[kWords];
   __shared__ float rest[kWaves][2];
-  __shared__ int twice;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, slices = gridDim.x - 1;
   const int64_t row = a.row0 + blockIdx.y;
-  const T* const in = (const T*)a.logits + row * a.logits_row;
-  const int from = blockIdx.x * kCount;
   if (a.weights != nullptr && a.weights[row] == 0.f) return;
+  if (blockIdx.x == 0) return sum_row_list<TY>(a, row, lds);  // (the longest: first)
+  const int slice = blockIdx.x - 1, from = slice * kCount;
+  const T* const in = (const T*)a.logits + row * a.logits_row;
   V x[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -337,15 +399,11 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_slices(DistillArgs a)
     const int left = a.vocab - from - i * 32;
     bits[i] = left >= 32 ? 0u : left <= 0 ? ~0u : ~0u << left;
   }
-  if (tid == 0) twice = 0;
   lds_barrier();
   for (int k = tid; k < a.listed; k += THREADS) {
     const int id = a.ids[row * a.ids_row + k];
     const uint32_t at = (uint32_t)(id - from);
-    if ((uint32_t)id < (uint32_t)a.vocab && at < (uint32_t)kCount) {
-      if (atomicOr(&bits[at / 32], 1u << (at % 32)) >> (at % 32) & 1) twice = 1;
-      a.listed_logits[row * a.listed + k] = (float)in[id];
-    }
+    if ((uint32_t)id < (uint32_t)a.vocab && at < (uint32_t)kCount) atomicOr(&bits[at / 32], 1u << (at % 32));
   }
   lds_barrier();
   const float c = kLog2e / a.tau;
@@ -370,18 +428,14 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_slices(DistillArgs a)
   for (int w = 0; w < kWaves; ++w) m = fmaxf(m, rest[w][0]);
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) s += rest[w][1] * __builtin_amdgcn_exp2f((rest[w][0] - m) * c);
-  a.slices[row * gridDim.x + blockIdx.x] = DistillSlice{m, s, twice};
+  a.slices[row * slices + slice] = DistillSlice{m, s};
 }
 
-// ... then a slice's gradient, from all slices' sums and the list, which every slice computes for itself.
 template <int TY, int NV>
 __global__ void __launch_bounds__(kSliceThreads) k_distill_grad(DistillArgs a) {
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
-  constexpr int N = kPiece<TY>, THREADS = kSliceThreads, kWaves = THREADS / kWave;
-  extern __shared__ __align__(16) uint8_t lds[];
-  __shared__ Parts<kWaves> parts;
-  const List list = list_at(a, lds);
+  constexpr int N = kPiece<TY>, THREADS = kSliceThreads;
   const int tid = threadIdx.x, lane = tid % kWave, slices = gridDim.x;
   const int64_t row = a.row0 + blockIdx.y;
   const T* const in = (const T*)a.logits + row * a.logits_row;
@@ -400,20 +454,15 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_grad(DistillArgs a) {
       x[j] = load_piece<TY>(in, min(at, a.vocab), a.vocab);
     }
   }
-  DistillSlice own{kLowest, 0.f, 0};  // (a lane has a slice)
+  DistillSlice own{kLowest, 0.f};  // (a lane has a slice)
   if (lane < slices) own = a.slices[row * slices + lane];
-  read_list<THREADS>(a, row, list, parts, [&](int k, int) { return a.listed_logits[row * a.listed + k]; }, [](int) {});
-  lds_barrier();
-  const bool dup = __ballot(own.twice) != 0;
-  double zmax;
-  sum_list<THREADS>(a, row, list, parts, dup, zmax);
+  const DistillRow l = a.row_lists[row];
   const float c = kLog2e / a.tau, m = wave_max(own.m);
   const double s_rest = wave_sum64((double)(own.s * __builtin_amdgcn_exp2f((own.m - m) * c)));
-  lds_barrier();
-  const Sums r = join<kWaves>(a, parts, zmax, m, s_rest);
+  const Sums r = join(a, l.sum, l.zmax, m, s_rest);
   if (tid == 0 && blockIdx.x == 0) a.loss[row] = (float)r.loss;
   if (out == nullptr) return;
-  const double scale = (double)weight / (double)a.tau;
+  const double scale = (double)weight / (double)a.tau, inv = 1.0 / (double)a.tau;
   const float by = (float)(r.c_rest * scale);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -421,7 +470,18 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_grad(DistillArgs a) {
     if (at < a.vocab) store_piece<TY>(out, at, a.vocab, gradient<TY>(x[j], m, c, by));
   }
   __syncthreads();  // the listed ids' gradients go over what was written there
-  write_list<T, THREADS>(a, out, list, r, dup, scale, from, NV * THREADS * N);
+  const int32_t* const ids = a.ids + row * a.ids_row;
+  const double* const mass = a.listed_mass + row * a.listed;
+  for (int k = tid; k < a.listed; k += THREADS) {
+    const int id = ids[k];
+    if ((uint32_t)id >= (uint32_t)a.vocab || (uint32_t)(id - from) >= (uint32_t)(NV * THREADS * N)) continue;
+    double p = mass[k];
+    if (l.twice) {  // one that is listed several times: their sum
+      p = 0.0;
+      for (int i = 0; i < a.listed; ++i) p += ids[i] == id ? mass[i] : 0.0;
+    }
+    out[id] = listed_gradient<T>(r, a.listed_logits[row * a.listed + k], p, inv, scale);
+  }
 }
 
 template <int TY, int THREADS, int NV>
@@ -435,12 +495,12 @@ hipError_t launch_rows(const DistillArgs& a, hipStream_t s) {
 
 template <int TY, int NV>
 hipError_t launch_slices(DistillArgs a, int slices, hipStream_t s) {
-  const int lds = a.listed * kListBytes;
-  hipError_t e = allow_dynamic_lds((const void*)k_distill_grad<TY, NV>, lds);
+  const int lds = a.listed * kListBytes + table_slots(a.listed) * 8;
+  hipError_t e = allow_dynamic_lds((const void*)k_distill_slices<TY, NV>, lds);
   for (a.row0 = 0; a.row0 < a.rows && e == hipSuccess; a.row0 += 65535) {
-    const dim3 grid((unsigned)slices, (unsigned)(a.rows - a.row0 < 65535 ? a.rows - a.row0 : 65535));
-    k_distill_slices<TY, NV><<<grid, kSliceThreads, 0, s>>>(a);
-    k_distill_grad<TY, NV><<<grid, kSliceThreads, lds, s>>>(a);
+    const unsigned n = (unsigned)(a.rows - a.row0 < 65535 ? a.rows - a.row0 : 65535);
+    k_distill_slices<TY, NV><<<dim3((unsigned)slices + 1, n), kSliceThreads, lds, s>>>(a);
+    k_distill_grad<TY, NV><<<dim3((unsigned)slices, n), kSliceThreads, 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;
@@ -451,8 +511,9 @@ hipError_t launch_typed(const DistillArgs& a, hipStream_t s) {
   const DistillCut cut = distill_cut(a.rows, a.vocab, TY);
   if (cut.slices > 0) return cut.pieces == 8 ? launch_slices<TY, 8>(a, cut.slices, s) : launch_slices<TY, 2>(a, cut.slices, s);
   const int pieces = (a.vocab + kPiece<TY> - 1) / kPiece<TY>;
-  if (pieces <= 256) return launch_rows<TY, 256, 1>(a, s);
-  if (pieces <= 4 * 256) return launch_rows<TY, 256, 4>(a, s);
+  if (pieces <= 2 * 64) return launch_rows<TY, 64, 2>(a, s);
+  if (pieces <= 8 * 64) return launch_rows<TY, 64, 8>(a, s);
+  if (pieces <= 8 * 256) return launch_rows<TY, 256, 8>(a, s);
   if (pieces <= 16 * 256) return launch_rows<TY, 256, 16>(a, s);
   return launch_rows<TY, 512, 16>(a, s);
 }

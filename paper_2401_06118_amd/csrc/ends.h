@@ -70,16 +70,21 @@ struct DistillArgs {
   int32_t vocab, listed, teacher_dtype;
   float tau;
   // workspace, where rows are cut
-  struct DistillSlice* slices;  // [rows][slices]
-  float* listed_logits;         // [rows][listed]
-  int64_t row0;                 // a launch's first
+  struct DistillRow* row_lists;  // [rows]
+  double* listed_mass;           // [rows][listed]
+  float* listed_logits;          // [rows][listed]
+  struct DistillSlice* slices;   // [rows][slices]
+  int64_t row0;                  // a launch's first
 };
 
-// What a slice of a row has outside the list: largest logit, sum relative to it; and whether an
-// id of it is listed twice.
+// What a slice of a row has outside the list: largest logit, sum relative to it.
 struct DistillSlice {
   float m, s;
-  int32_t twice;
+};
+// What a row's list adds up to; whether an id is listed several times.
+struct DistillRow {
+  double sum[4], zmax;
+  int64_t twice;
 };
 // Slices of a row (0: rows are not cut), pieces of 16 bytes a thread of a slice has.
 struct DistillCut {

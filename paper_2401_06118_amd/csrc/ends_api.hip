@@ -200,7 +200,7 @@ size_t aqlm_distill_loss_workspace_bytes(int64_t rows, int64_t vocab, int64_t li
       listed > aqlm::kDistillMaxListed || !known_dtype(dtype))
     return 0;
   const aqlm::DistillCut cut = aqlm::distill_cut(rows, vocab, dtype);
-  return cut.slices == 0 ? 0 : (size_t)rows * ((size_t)cut.slices * sizeof(aqlm::DistillSlice) + (size_t)listed * 4);
+  return cut.slices == 0 ? 0 : (size_t)rows * (sizeof(aqlm::DistillRow) + (size_t)cut.slices * sizeof(aqlm::DistillSlice) + (size_t)listed * 12);
 }
 
 int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, const void* teacher,
@@ -242,7 +242,9 @@ int aqlm_distill_loss(const void* logits, int64_t logits_stride, int32_t dtype, 
   a.teacher_dtype = teacher_dtype;
   a.tau = temperature;
   if (need > 0) {
-    a.slices = static_cast<aqlm::DistillSlice*>(workspace);
+    a.row_lists = static_cast<aqlm::DistillRow*>(workspace);
+    a.listed_mass = reinterpret_cast<double*>(a.row_lists + rows);
+    a.slices = reinterpret_cast<aqlm::DistillSlice*>(a.listed_mass + rows * listed);
     a.listed_logits = reinterpret_cast<float*>(a.slices + rows * aqlm::distill_cut(rows, vocab, dtype).slices);
   }
   return status_of(aqlm::launch_distill(a, dtype, (hipStream_t)stream));
