@@ -664,9 +664,9 @@ int aqlm_embed(const void* table, int64_t table_stride, const int32_t* tokens, v
 /* grad[v] = scale * the sum of dout[t] over the t with tokens[t] = v: the gradient of
  * aqlm_embed's table, all rows written (zeros where the token does not occur), of dout's
  * type or fp32.  The places are sorted by token on the device and summed in fp32 in a fixed
- * order.  workspace: aqlm_embed_backward_workspace_bytes(count, dim, dtype) bytes, 16-byte
+ * order.  workspace: aqlm_embed_backward_workspace_bytes(count, vocab, dim, dtype) bytes, 16-byte
  * aligned, any contents. */
-size_t aqlm_embed_backward_workspace_bytes(int64_t count, int64_t dim, int32_t dtype);
+size_t aqlm_embed_backward_workspace_bytes(int64_t count, int64_t vocab, int64_t dim, int32_t dtype);
 int aqlm_embed_backward(const void* dout, int64_t dout_stride, const int32_t* tokens, void* grad, int64_t grad_stride,
                         int32_t dtype, int32_t grad_dtype, int64_t count, int64_t vocab, int64_t dim, float scale,
                         void* workspace, size_t workspace_bytes, void* stream);

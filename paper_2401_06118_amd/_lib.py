@@ -187,7 +187,7 @@ def load():
         f32, size = ctypes.c_float, ctypes.c_size_t
         lib.aqlm_embed.argtypes = [p, i64, p, p, i64, i32, i64, i64, i64, f32, p]
         lib.aqlm_embed.restype = ctypes.c_int
-        lib.aqlm_embed_backward_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.aqlm_embed_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
         lib.aqlm_embed_backward_workspace_bytes.restype = size
         lib.aqlm_embed_backward.argtypes = [p, i64, p, p, i64, i32, i32, i64, i64, i64, f32, p, size, p]
         lib.aqlm_embed_backward.restype = ctypes.c_int

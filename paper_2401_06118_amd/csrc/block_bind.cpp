@@ -442,7 +442,7 @@ PyObject* embed_backward(PyObject* const* a) {
   if (vocab <= 0) refuse("vocab must be positive");
   at::ScalarType type = truth(a[4]) ? at::kFloat : dout.scalar_type();
   if (given(a[5]) && tensor(a[5], "out").scalar_type() == at::kFloat) type = at::kFloat;
-  const size_t bytes = aqlm_embed_backward_workspace_bytes(count, dout.size(1), dtype_of(dout, "dout"));
+  const size_t bytes = aqlm_embed_backward_workspace_bytes(count, vocab, dout.size(1), dtype_of(dout, "dout"));
   if (bytes == 0) done(AQLM_ERR_SHAPE, "aqlm_embed_backward");
   const at::Tensor out = output2(a[5], "out", dout, vocab, dout.size(1), type);
   const at::Tensor ws = at::empty({(int64_t)bytes}, dout.options().dtype(at::kByte));

@@ -66,22 +66,18 @@ hipError_t launch_embed_typed(const EmbedArgs& a, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// Gradient.  One launch sorts the places 0 .. tokens - 1 by token (stable) and writes the
-// zero rows; the next sums each token's rows in the order of its places.
+// Gradient.  One launch sorts the places 0 .. tokens - 1 by token (stable); the next sums each
+// token's rows in the order of its places and, by other workgroups, writes the zero rows: those
+// are most of the bytes, and hide the sums' latency.
 //
 // Sorting: workgroup b of 2^lg holds the tokens whose low lg bits are b, so that tokens
 // with small numbers, the frequent ones, are spread.  It walks all ids twice: counts (how many
 // belong to earlier workgroups, and for each wave's share of the places how many are
-// each of its own tokens), then writes places.  2^lg x tokens x 4 bytes from the L2s, beside
-// the zero rows' bytes.
+// each of its own tokens), then writes places.  2^lg x tokens x 4 bytes from the L2s.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortOwn = 512;  // tokens of a workgroup
 
-template <int TY>
 __global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedGradArgs a, int lg, int64_t counters) {
-  typedef typename Elem<TY>::T T;
-  typedef typename Elem<TY>::V V;
-  constexpr int N = kPiece<TY>;
   __shared__ int at[kSortWaves][kSortOwn];  // counts, then the next place of a wave's token
   __shared__ int from[kSortOwn], total[kSortOwn];  // where a token's places begin, how many
   __shared__ int below[kSortWaves], sums[kSortWaves];
@@ -121,10 +117,11 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedGradArgs a, in
   if (lane == 0) below[wave] = before;
   __syncthreads();
   // exclusive sums over the tokens, then over the waves of each
-  int n = 0;
-  if (tid < own) {
-    for (int w = 0; w < kSortWaves; ++w) n += at[w][tid];
-    total[tid] = n;
+  int n = 0, count[kSortWaves];
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    count[w] = tid < own ? at[w][tid] : 0;
+    n += count[w];
   }
   int incl = n;
 #pragma unroll
@@ -134,21 +131,24 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedGradArgs a, in
   }
   if (lane == kWave - 1) sums[wave] = incl;
   __syncthreads();
-  int base = incl - n;
-  for (int w = 0; w < kSortWaves; ++w) base += below[w] + (w < wave ? sums[w] : 0);
-  if (b == (int)gridDim.x - 1 && tid == 0) {
-    int all = 0;
-    for (int w = 0; w < kSortWaves; ++w) all += below[w] + sums[w];
-    *a.held = all;
+  int base = incl - n, all = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    const int o = sums[w];
+    base += below[w] + (w < wave ? o : 0);
+    all += below[w] + o;
   }
+  if (b == (int)gridDim.x - 1 && tid == 0) *a.held = all;
   if (tid < own) {
     int next = base;
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int c = at[w][tid];
       at[w][tid] = next;
-      next += c;
+      next += count[w];
     }
     from[tid] = base;
+    total[tid] = n;
+    a.occurs[(int64_t)b * kSortOwn + tid] = n != 0;
   }
   __syncthreads();
   walk([&](int i, int id, bool, bool mine) {
@@ -167,57 +167,92 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedGradArgs a, in
       left &= ~same;
     }
   });
-  // rows of tokens that do not occur
-  V zero;
+}
+
+// Rows of tokens that do not occur: a wave a row.
+template <int OTY>
+__device__ __forceinline__ void write_zero_rows(const EmbedGradArgs& a, int lg, int64_t wave, int64_t waves) {
+  constexpr int N = kPiece<OTY>;
+  typename Elem<OTY>::V zero;
 #pragma unroll
-  for (int e = 0; e < N; ++e) zero[e] = (T)0.f;
-  for (int r = wave; r < own; r += kSortWaves) {
-    if (total[r] != 0) continue;
-    T* const out = (T*)a.out + (((int64_t)r << lg) + b) * a.out_row;
-    for (int c = lane * N; c < a.dim; c += kWave * N) store_piece<TY>(out, c, a.dim, zero);
+  for (int e = 0; e < N; ++e) zero[e] = (typename Elem<OTY>::T)0.f;
+  constexpr int kBatch = 8;  // rows whose marks are loaded at once
+  for (int64_t v0 = wave; v0 < a.vocab; v0 += kBatch * waves) {
+    bool occurs[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int64_t v = min(v0 + j * waves, (int64_t)a.vocab - 1);
+      occurs[j] = a.occurs[(v & ((1 << lg) - 1)) * kSortOwn + (v >> lg)] != 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int64_t v = v0 + j * waves;
+      if (v >= a.vocab || occurs[j]) continue;
+      typename Elem<OTY>::T* const out = (typename Elem<OTY>::T*)a.out + v * a.out_row;
+      for (int c = threadIdx.x % kWave * N; c < a.dim; c += kWave * N) store_piece<OTY>(out, c, a.dim, zero);
+    }
   }
 }
 
-// A workgroup: the rows of kEmbedUnit sorted places, in a block of columns (a piece of 16
-// bytes a thread).  Sums of tokens that lie in one unit are written; pieces of those
+// The first units x columns workgroups: the rows of kEmbedUnit sorted places, in a block of columns (a
+// piece of 16 bytes a thread).  Sums of tokens that lie in one unit are written; pieces of those
 // that do not go to memory, and the last workgroup to bring one adds them in the order of
-// the units.
+// the units.  The others write zeros.
 template <int TY, int OTY>
-__global__ void __launch_bounds__(kThreads) k_embed_sum(EmbedGradArgs a) {
+__global__ void __launch_bounds__(kThreads) k_embed_sum(EmbedGradArgs a, int lg, int units, int columns) {
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
   typedef typename Elem<OTY>::T O;
   constexpr int N = kPiece<TY>;
   __shared__ int flag;
-  const int held = *a.held;
-  const int c = (blockIdx.y * kThreads + threadIdx.x) * N;
+  const int summing = units * columns;
+  if ((int)blockIdx.x >= summing)
+    return write_zero_rows<OTY>(a, lg, (int64_t)(blockIdx.x - summing) * (kThreads / kWave) + threadIdx.x / kWave,
+                                (int64_t)(gridDim.x - summing) * (kThreads / kWave));
+  const int held = *a.held, column = blockIdx.x % columns;
+  const int c = (column * kThreads + threadIdx.x) * N;
   const bool active = c < a.dim;
-  for (int64_t first = (int64_t)blockIdx.x * kEmbedUnit; first < held; first += (int64_t)gridDim.x * kEmbedUnit) {
-    const int p0 = (int)first, unit = p0 / kEmbedUnit, p1 = (int)min(first + kEmbedUnit, (int64_t)held);
+  for (int64_t begin = (int64_t)(blockIdx.x / columns) * kEmbedUnit; begin < held; begin += (int64_t)units * kEmbedUnit) {
+    const int p0 = (int)begin, unit = p0 / kEmbedUnit, p1 = (int)min(begin + kEmbedUnit, (int64_t)held);
     float sum[N];
     auto write = [&](int place, const float* s) {
       if (!active) return;
-      O* const out = (O*)a.out + a.tokens[place] * a.out_row + c;
+      O* const out = (O*)a.out + a.tokens[place] * a.out_row;
+      if constexpr (kPiece<OTY> == N) {
+        typename Elem<OTY>::V o;
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (c + e < a.dim) out[e] = (O)(s[e] * a.scale);
+        for (int e = 0; e < N; ++e) o[e] = (O)(s[e] * a.scale);
+        store_piece<OTY>(out, c, a.dim, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (c + e < a.dim) out[c + e] = (O)(s[e] * a.scale);
+      }
     };
-    auto part = [&](int u, int which) { return a.parts + ((int64_t)u * 2 + which) * a.dim + c; };
+    // (pieces of a unit: of a token that began before it, and of one that goes on behind it; two floats a store)
+    auto part = [&](int u, int which) { return (uint64_t*)(a.parts + ((int64_t)u * 2 + which) * a.parts_row + c); };
     auto put = [&](int which) {
       if (!active) return;
-      float* const p = part(unit, which);
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (c + e < a.dim) put_through(p + e, sum[e]);
+      for (int e = 0; e < N / 2; ++e)
+        put_through(part(unit, which) + e, (uint64_t)__builtin_bit_cast(uint32_t, sum[2 * e]) |
+                                               (uint64_t)__builtin_bit_cast(uint32_t, sum[2 * e + 1]) << 32);
     };
+    int order[kEmbedUnit], first[kEmbedUnit], last[kEmbedUnit];
+#pragma unroll
+    for (int i = 0; i < kEmbedUnit; ++i) {
+      order[i] = a.order[min(p0 + i, p1 - 1)];
+      first[i] = a.first[min(p0 + i, p1 - 1)];
+      last[i] = a.last[min(p0 + i, p1 - 1)];
+    }
     V v[kEmbedUnit];
 #pragma unroll
     for (int i = 0; i < kEmbedUnit; ++i) {
       v[i] = V(0);
-      if (p0 + i < p1 && active) v[i] = load_piece<TY>((const T*)a.dout + a.order[p0 + i] * a.dout_row, c, a.dim);
+      if (active) v[i] = load_piece<TY>((const T*)a.dout + order[i] * a.dout_row, c, a.dim);
     }
     // what is open at this unit's ends
-    const int head_first = a.first[p0], tail_last = a.last[p1 - 1], tail_first = a.first[p1 - 1];
+    const int head_first = first[0], head_last = last[0], tail_last = last[kEmbedUnit - 1], tail_first = first[kEmbedUnit - 1];
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = 0.f;
 #pragma unroll
@@ -225,9 +260,8 @@ __global__ void __launch_bounds__(kThreads) k_embed_sum(EmbedGradArgs a) {
       if (p0 + i >= p1) break;
 #pragma unroll
       for (int e = 0; e < N; ++e) sum[e] += (float)v[i][e];
-      const int f = a.first[p0 + i], l = a.last[p0 + i];
-      if (l == p0 + i + 1) {  // the token's last place
-        if (f >= p0) write(a.order[p0 + i], sum);
+      if (last[i] == p0 + i + 1) {  // the token's last place
+        if (first[i] >= p0) write(order[i], sum);
         else put(0);
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] = 0.f;
@@ -237,41 +271,59 @@ __global__ void __launch_bounds__(kThreads) k_embed_sum(EmbedGradArgs a) {
     // join: the token that began before this unit, and the one that goes on behind it
     auto join = [&](int f, int l) {
       const int u0 = f / kEmbedUnit, u1 = (l - 1) / kEmbedUnit;
-      if (!last_of(a.counters + (int64_t)u0 * gridDim.y + blockIdx.y, u1 - u0 + 1, &flag)) return;
+      if (!last_of(a.counters + (int64_t)u0 * columns + column, u1 - u0 + 1, &flag)) return;
       if (!active) return;
       float s[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) s[e] = 0.f;
-      for (int u = u0; u <= u1; ++u) {
-        const float* const p = part(u, u == u0 ? 1 : 0);
+      constexpr int kBatch = 8;  // units whose pieces are loaded at once
+      for (int b0 = u0; b0 <= u1; b0 += kBatch) {
+        uint64_t w[kBatch][N / 2];
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (c + e < a.dim) s[e] += get_through(p + e);
+        for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+          for (int e = 0; e < N / 2; ++e) {
+            const int u = min(b0 + j, u1);
+            w[j][e] = get_through(part(u, u == u0 ? 1 : 0) + e);
+          }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+          for (int e = 0; e < N / 2; ++e)
+            if (b0 + j <= u1) {
+              s[2 * e] += __builtin_bit_cast(float, (uint32_t)w[j][e]);
+              s[2 * e + 1] += __builtin_bit_cast(float, (uint32_t)(w[j][e] >> 32));
+            }
       }
       write(a.order[f], s);
     };
-    if (head_first < p0) join(head_first, a.last[p0]);
+    if (head_first < p0) join(head_first, head_last);
     if (tail_last > p1 && tail_first >= p0) join(tail_first, tail_last);
   }
 }
 
 template <int TY, int OTY>
 hipError_t launch_grad_typed(const EmbedGradArgs& a, hipStream_t s) {
-  int lg = 8;
-  while ((int64_t)kSortOwn << lg < a.vocab) ++lg;
+  const int lg = embed_grad_lg(a.vocab);
   const int units = (int)((a.tokens_count + (int64_t)kEmbedUnit - 1) / kEmbedUnit);
   const int columns = embed_grad_column_blocks(a.dim, TY);
-  k_embed_sort<OTY><<<1u << lg, kSortThreads, 0, s>>>(a, lg, (int64_t)units * columns);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || units == 0) return e;
+  k_embed_sort<<<1u << lg, kSortThreads, 0, s>>>(a, lg, (int64_t)units * columns);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   // (a launch has fewer than 2^32 threads)
-  const int grid = min(units, max(1, (1 << 23) / columns));
-  k_embed_sum<TY, OTY><<<dim3((unsigned)grid, (unsigned)columns), kThreads, 0, s>>>(a);
+  const int summing = min(units, max(1, (1 << 23) / columns));
+  k_embed_sum<TY, OTY><<<(unsigned)(summing * columns + 8 * num_cus()), kThreads, 0, s>>>(a, lg, summing, columns);
   return hipGetLastError();
 }
 
 }  // namespace
 
+int embed_grad_lg(int64_t vocab) {
+  int lg = 8;
+  while ((int64_t)kSortOwn << lg < vocab) ++lg;
+  return lg;
+}
+int64_t embed_grad_marks(int64_t vocab) { return (int64_t)kSortOwn << embed_grad_lg(vocab); }
 int embed_grad_column_blocks(int32_t dim, int dtype) {
   const int columns = kThreads * (dtype == kF32 ? 4 : 8);
   return (dim + columns - 1) / columns;

@@ -30,11 +30,15 @@ struct EmbedGradArgs {
   int32_t* order;      // [tokens] places, those of one token together, ascending
   int32_t* first;      // [tokens] where the token's places begin in order,
   int32_t* last;       // [tokens] and end
-  float* parts;        // [units][2][dim]
+  uint8_t* occurs;     // [embed_grad_marks]
+  float* parts;        // [units][2][parts_row]
+  int64_t parts_row;   // dim, to whole pieces
 };
 
 constexpr int kEmbedUnit = 16;  // places of `order` that a workgroup sums
 int embed_grad_column_blocks(int32_t dim, int dtype);
+int embed_grad_lg(int64_t vocab);
+int64_t embed_grad_marks(int64_t vocab);
 
 struct NormArgs {
   const void *x, *residual, *weight, *bias;

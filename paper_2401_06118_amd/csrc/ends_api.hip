@@ -31,9 +31,9 @@ bool rows_out(int64_t stride, int64_t rows, int64_t n) { return stride >= (rows 
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 struct EmbedWorkspace {
-  size_t counters, held, order, first, last, parts, bytes;
+  size_t counters, held, order, first, last, occurs, parts, parts_row, bytes;
 };
-EmbedWorkspace embed_workspace(int64_t count, int64_t dim, int32_t dtype) {
+EmbedWorkspace embed_workspace(int64_t count, int64_t vocab, int64_t dim, int32_t dtype) {
   EmbedWorkspace w{};
   const size_t units = (size_t)((count + aqlm::kEmbedUnit - 1) / aqlm::kEmbedUnit);
   const size_t places = up16((size_t)count * 4);
@@ -42,8 +42,10 @@ EmbedWorkspace embed_workspace(int64_t count, int64_t dim, int32_t dtype) {
   w.order = w.held + 16;
   w.first = w.order + places;
   w.last = w.first + places;
-  w.parts = w.last + places;
-  w.bytes = w.parts + units * 2 * (size_t)dim * 4;
+  w.occurs = w.last + places;
+  w.parts = w.occurs + up16((size_t)aqlm::embed_grad_marks(vocab));
+  w.parts_row = ((size_t)dim + 7) / 8 * 8;
+  w.bytes = w.parts + units * 2 * w.parts_row * 4;
   return w;
 }
 
@@ -88,9 +90,9 @@ int aqlm_embed(const void* table, int64_t table_stride, const int32_t* tokens, v
   return status_of(aqlm::launch_embed(a, dtype, (hipStream_t)stream));
 }
 
-size_t aqlm_embed_backward_workspace_bytes(int64_t count, int64_t dim, int32_t dtype) {
-  if (!embed_sizes(count, 1, dim) || !known_dtype(dtype)) return 0;
-  return embed_workspace(count, dim, dtype).bytes;
+size_t aqlm_embed_backward_workspace_bytes(int64_t count, int64_t vocab, int64_t dim, int32_t dtype) {
+  if (!embed_sizes(count, vocab, dim) || !known_dtype(dtype)) return 0;
+  return embed_workspace(count, vocab, dim, dtype).bytes;
 }
 
 int aqlm_embed_backward(const void* dout, int64_t dout_stride, const int32_t* tokens, void* grad, int64_t grad_stride,
@@ -102,7 +104,7 @@ int aqlm_embed_backward(const void* dout, int64_t dout_stride, const int32_t* to
   if (!element_aligned(dout, dtype) || !element_aligned(grad, grad_dtype) || !multiple(tokens, 4) ||
       !multiple(workspace, 16))
     return AQLM_ERR_ALIGN;
-  const EmbedWorkspace w = embed_workspace(count, dim, dtype);
+  const EmbedWorkspace w = embed_workspace(count, vocab, dim, dtype);
   if (workspace_bytes < w.bytes) return AQLM_ERR_WORKSPACE;
   uint8_t* const ws = static_cast<uint8_t*>(workspace);
   aqlm::EmbedGradArgs a{};
@@ -120,7 +122,9 @@ int aqlm_embed_backward(const void* dout, int64_t dout_stride, const int32_t* to
   a.order = reinterpret_cast<int32_t*>(ws + w.order);
   a.first = reinterpret_cast<int32_t*>(ws + w.first);
   a.last = reinterpret_cast<int32_t*>(ws + w.last);
+  a.occurs = ws + w.occurs;
   a.parts = reinterpret_cast<float*>(ws + w.parts);
+  a.parts_row = (int64_t)w.parts_row;
   return status_of(aqlm::launch_embed_grad(a, dtype, grad_dtype, (hipStream_t)stream));
 }
 

@@ -41,11 +41,12 @@ def test_embed(lib):
 
 
 def test_embed_backward(lib):
-    need = lib.aqlm_embed_backward_workspace_bytes(3, 64, F16)
-    assert need > 0 and lib.aqlm_embed_backward_workspace_bytes(0, 64, F16) > 0
-    assert lib.aqlm_embed_backward_workspace_bytes(100000, 64, F16) > lib.aqlm_embed_backward_workspace_bytes(1000, 64, F16)
-    for bad in ((-1, 64, F16), (3, 0, F16), (3, (1 << 24) + 1, F16), (3, 64, 7), (1 << 31, 64, F16)):
-        assert lib.aqlm_embed_backward_workspace_bytes(*bad) == 0
+    room = lib.aqlm_embed_backward_workspace_bytes
+    need = room(3, 10, 64, F16)
+    assert need > 0 and room(0, 10, 64, F16) > 0 and room(100000, 10, 64, F16) > room(1000, 10, 64, F16)
+    for bad in ((-1, 10, 64, F16), (3, 10, 0, F16), (3, 10, (1 << 24) + 1, F16), (3, 10, 64, 7), (1 << 31, 10, 64, F16),
+                (3, 0, 64, F16), (3, (1 << 30) + 1, 64, F16)):
+        assert room(*bad) == 0
 
     def call(dout=P, ds=64, tokens=P, grad=Q, gs=64, dtype=F16, gtype=F16, count=3, vocab=10, dim=64, ws=P, size=need):
         return lib.aqlm_embed_backward(dout, ds, tokens, grad, gs, dtype, gtype, count, vocab, dim, 1.0, ws, size, None)
