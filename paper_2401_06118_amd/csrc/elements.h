@@ -31,20 +31,20 @@ struct Elem<kF32> {
 template <int TY>
 constexpr int kPiece = TY == kF32 ? 4 : 8;
 
-// Elements [at, at + piece) of a row of n; those past its end are 0.
-template <int TY>
+// Elements [at, at + piece) of a row of n; those past its end are 0.  WHOLE: n is whole pieces.
+template <int TY, bool WHOLE = false>
 __device__ __forceinline__ typename Elem<TY>::V load_piece(const void* row, int at, int n) {
   typedef typename Elem<TY>::T T;
   const T* const p = (const T*)row + at;
   if (at + kPiece<TY> <= n) return *(const typename Elem<TY>::V*)p;
   typename Elem<TY>::V v;
 #pragma unroll
-  for (int e = 0; e < kPiece<TY>; ++e) v[e] = at + e < n ? p[e] : (T)0.f;
+  for (int e = 0; e < kPiece<TY>; ++e) v[e] = !WHOLE && at + e < n ? p[e] : (T)0.f;
   return v;
 }
 
 // NT: past the L2s (results that nothing reads soon, more than they hold).
-template <int TY, bool NT = false>
+template <int TY, bool NT = false, bool WHOLE = false>
 __device__ __forceinline__ void store_piece(void* row, int at, int n, const typename Elem<TY>::V& v) {
   typedef typename Elem<TY>::T T;
   T* const p = (T*)row + at;
@@ -53,9 +53,11 @@ __device__ __forceinline__ void store_piece(void* row, int at, int n, const type
     else *(typename Elem<TY>::V*)p = v;
     return;
   }
+  if constexpr (!WHOLE) {
 #pragma unroll
-  for (int e = 0; e < kPiece<TY>; ++e)
-    if (at + e < n) p[e] = v[e];
+    for (int e = 0; e < kPiece<TY>; ++e)
+      if (at + e < n) p[e] = v[e];
+  }
 }
 
 // Sum of v over the 64 lanes in a fixed order, in every lane, for 64-bit types.

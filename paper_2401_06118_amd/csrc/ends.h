@@ -55,14 +55,14 @@ struct NormGradArgs {
   const void *dy, *x, *weight, *dsum;
   void* out;
   float *dweight, *dbias;
-  float* parts;  // [slots][dim] for each of dweight and dbias
+  float* parts;  // [norm_grad_parts()][dim] for each of dweight and dbias
   int64_t dy_row, x_row, dsum_row, out_row, rows;
   int32_t dim;
   bool rms;
   float eps;
 };
 
-int norm_grad_slots(int32_t dim);
+int norm_grad_parts();  // at most
 
 struct DistillArgs {
   const void *logits, *teacher;

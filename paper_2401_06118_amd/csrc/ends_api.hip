@@ -161,7 +161,7 @@ int aqlm_layer_norm(const void* x, int64_t x_stride, const void* residual, int64
 
 size_t aqlm_layer_norm_backward_workspace_bytes(int64_t dim) {
   if (dim <= 0 || dim > aqlm::kNormMaxDim) return 0;
-  return (size_t)aqlm::norm_grad_slots((int32_t)dim) * 2 * (size_t)dim * 4;
+  return (size_t)aqlm::norm_grad_parts() * 2 * (size_t)dim * 4;
 }
 
 int aqlm_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* dsum,

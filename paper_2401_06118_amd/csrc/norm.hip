@@ -40,11 +40,12 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*red)[16][2], int
       for (int k = 0; k < K; ++k) red[turn][wave][k] = v[k];
     }
     lds_barrier();
+    const int first = wave / WAVES * WAVES;  // (of this row)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += red[turn][w][k];
+      for (int w = 0; w < WAVES; ++w) s += red[turn][first + w][k];
       v[k] = s;
     }
     turn ^= 1;
@@ -52,7 +53,7 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*red)[16][2], int
 }
 
 // mu and r of a row held as pieces h (elements past its end are 0).
-template <int TY, int WAVES, int PER>
+template <int TY, int WAVES, int PER, bool WHOLE>
 __device__ __forceinline__ void row_stats(const typename Elem<TY>::V (&h)[PER], int t, int dim, bool rms, float eps,
                                           float (*red)[16][2], int& turn, float& mu, float& r) {
   constexpr int N = kPiece<TY>;
@@ -70,7 +71,7 @@ __device__ __forceinline__ void row_stats(const typename Elem<TY>::V (&h)[PER], 
       const int left = dim - (t + j * WAVES * kWave) * N;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float d = e < left ? (float)h[j][e] - mu : 0.f;
+        const float d = (WHOLE ? 0 : e) < left ? (float)h[j][e] - mu : 0.f;
         q[0] += d;
         q[1] += d * d;
       }
@@ -89,7 +90,8 @@ __device__ __forceinline__ void row_stats(const typename Elem<TY>::V (&h)[PER], 
   }
 }
 
-template <int TY, int WAVES, int PER>
+// WHOLE: rows are whole pieces.
+template <int TY, int WAVES, int PER, bool WHOLE>
 __global__ void __launch_bounds__(kNormThreads<WAVES>) k_norm(NormArgs a) {
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
@@ -101,19 +103,19 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) k_norm(NormArgs a) {
        row += (int64_t)gridDim.x * kRows) {
     V h[PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) h[j] = load_piece<TY>((const T*)a.x + row * a.x_row, (t + j * WAVES * kWave) * N, a.dim);
+    for (int j = 0; j < PER; ++j) h[j] = load_piece<TY, WHOLE>((const T*)a.x + row * a.x_row, (t + j * WAVES * kWave) * N, a.dim);
     if (a.residual != nullptr) {
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         const int c = (t + j * WAVES * kWave) * N;
-        const V o = load_piece<TY>((const T*)a.residual + row * a.residual_row, c, a.dim);
+        const V o = load_piece<TY, WHOLE>((const T*)a.residual + row * a.residual_row, c, a.dim);
 #pragma unroll
         for (int e = 0; e < N; ++e) h[j][e] = (T)((float)h[j][e] + (float)o[e]);
-        if (a.sum != nullptr) store_piece<TY>((T*)a.sum + row * a.sum_row, c, a.dim, h[j]);
+        if (a.sum != nullptr) store_piece<TY, false, WHOLE>((T*)a.sum + row * a.sum_row, c, a.dim, h[j]);
       }
     }
     float mu, r;
-    row_stats<TY, WAVES, PER>(h, t, a.dim, a.rms, a.eps, red, turn, mu, r);
+    row_stats<TY, WAVES, PER, WHOLE>(h, t, a.dim, a.rms, a.eps, red, turn, mu, r);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int c = (t + j * WAVES * kWave) * N;
@@ -121,120 +123,169 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) k_norm(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < N; ++e) y[e] = ((float)h[j][e] - mu) * r;
       if (a.weight != nullptr) {
-        const V w = load_piece<TY>(a.weight, c, a.dim);
+        const V w = load_piece<TY, WHOLE>(a.weight, c, a.dim);
 #pragma unroll
         for (int e = 0; e < N; ++e) y[e] *= (float)w[e];
       }
       if (a.bias != nullptr) {
-        const V b = load_piece<TY>(a.bias, c, a.dim);
+        const V b = load_piece<TY, WHOLE>(a.bias, c, a.dim);
 #pragma unroll
         for (int e = 0; e < N; ++e) y[e] += (float)b[e];
       }
       V o;
 #pragma unroll
       for (int e = 0; e < N; ++e) o[e] = (T)y[e];
-      store_piece<TY>((T*)a.out + row * a.out_row, c, a.dim, o);
+      store_piece<TY, false, WHOLE>((T*)a.out + row * a.out_row, c, a.dim, o);
     }
   }
 }
 
-// Gradients: a slot (the waves of one row) takes every gridDim-th row and adds up the
-// weight's and the bias's gradients of its columns, which go to `parts`.
-template <int TY, int WAVES, int PER>
-__global__ void __launch_bounds__(kNormThreads<WAVES>) k_norm_grad(NormGradArgs a) {
+// Gradients: a workgroup (of a row, or of four rows of a wave each) takes every gridDim-th set of
+// rows and adds up the weight's and the bias's gradients of its columns, which go to `parts`.  The
+// next set is loaded while one is worked on, where the registers hold two.  (Four sets at a time, or
+// sixteen waves a workgroup, two rows: no faster, 2048 x 4096 fp16.)
+template <int WAVES>
+constexpr int kGradRows = WAVES == 1 ? 4 : 1;
+
+template <int TY, int WAVES, int PER, bool WHOLE>
+__global__ void __launch_bounds__((WAVES * kGradRows<WAVES> * kWave)) k_norm_grad(NormGradArgs a) {
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
-  constexpr int N = kPiece<TY>, kRows = WAVES == 1 ? 4 : 1;
+  constexpr int N = kPiece<TY>, kRows = kGradRows<WAVES>, kThreads = WAVES * kRows * kWave;
+  constexpr int kRing = PER * N <= 16 ? 2 : 1;  // sets that are loaded or worked on at a time
   __shared__ float red[2][16][2];
-  const int t = WAVES == 1 ? threadIdx.x % kWave : threadIdx.x;
-  const int slot = blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0), slots = gridDim.x * kRows;
+  const int t = threadIdx.x % (WAVES * kWave), own = threadIdx.x / (WAVES * kWave);
+  const int64_t step = (int64_t)gridDim.x * kRows, slot = (int64_t)blockIdx.x * kRows;
   int turn = 0;
   float dw[PER][N], db[PER][N];
 #pragma unroll
   for (int j = 0; j < PER; ++j)
 #pragma unroll
     for (int e = 0; e < N; ++e) dw[j][e] = db[j][e] = 0.f;
-  for (int64_t row = slot; row < a.rows; row += slots) {
-    V h[PER], dy[PER];
+  struct Row {
+    V h[PER], dy[PER], ds[PER];
+  };
+  auto load = [&](Row& r, int64_t row) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int c = (t + j * WAVES * kWave) * N;
-      h[j] = load_piece<TY>((const T*)a.x + row * a.x_row, c, a.dim);
-      dy[j] = load_piece<TY>((const T*)a.dy + row * a.dy_row, c, a.dim);
+      r.h[j] = load_piece<TY, WHOLE>((const T*)a.x + row * a.x_row, c, a.dim);
+      r.dy[j] = load_piece<TY, WHOLE>((const T*)a.dy + row * a.dy_row, c, a.dim);
+      if (a.dsum != nullptr) r.ds[j] = load_piece<TY, WHOLE>((const T*)a.dsum + row * a.dsum_row, c, a.dim);
     }
-    float mu, r;
-    row_stats<TY, WAVES, PER>(h, t, a.dim, a.rms, a.eps, red, turn, mu, r);
-    float s[2] = {0.f, 0.f};
+  };
+  V w[PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int c = (t + j * WAVES * kWave) * N;
-      V w;
-      if (a.weight != nullptr) w = load_piece<TY>(a.weight, c, a.dim);
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        // (past the row's end dy is 0)
-        const float d = (float)dy[j][e], xh = ((float)h[j][e] - mu) * r, g = a.weight != nullptr ? d * (float)w[e] : d;
-        dw[j][e] += d * xh;
-        db[j][e] += d;
-        s[0] += g * xh;
-        s[1] += g;
-      }
+  for (int j = 0; j < PER; ++j)
+    if (a.weight != nullptr) w[j] = load_piece<TY, WHOLE>(a.weight, (t + j * WAVES * kWave) * N, a.dim);
+  // (a row past the last one is zeros, which add nothing)
+  auto load_own = [&](Row& r, int64_t set) {
+    if (set + own < a.rows) {
+      load(r, set + own);
+      return;
     }
-    row_sums<WAVES>(s, red, turn);
-    const float by = s[0] / (float)a.dim, mean = a.rms ? 0.f : s[1] / (float)a.dim;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int c = (t + j * WAVES * kWave) * N;
-      V w, o;
-      float d[N];
-      if (a.weight != nullptr) w = load_piece<TY>(a.weight, c, a.dim);
+    for (int j = 0; j < PER; ++j)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float xh = ((float)h[j][e] - mu) * r, g = a.weight != nullptr ? (float)dy[j][e] * (float)w[e] : (float)dy[j][e];
-        d[e] = r * (g - xh * by - mean);
+      for (int e = 0; e < N; ++e) r.h[j][e] = r.dy[j][e] = (T)0.f;
+  };
+  Row ring[kRing];
+#pragma unroll
+  for (int d = 0; d < kRing; ++d)
+    if (kRing > 1 && slot + d * step < a.rows) load_own(ring[d], slot + d * step);
+  for (int64_t first = slot; first < a.rows; first += kRing * step) {
+#pragma unroll
+    for (int d = 0; d < kRing; ++d) {
+      const int64_t set = first + d * step, row = set + own;
+      if (set >= a.rows) break;
+      Row& r = ring[d];
+      if (kRing == 1) load_own(r, set);
+      float mu, rs;
+      row_stats<TY, WAVES, PER, WHOLE>(r.h, t, a.dim, a.rms, a.eps, red, turn, mu, rs);
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          // (past the row's end dy is 0)
+          const float d = (float)r.dy[j][e], xh = ((float)r.h[j][e] - mu) * rs, g = a.weight != nullptr ? d * (float)w[j][e] : d;
+          dw[j][e] += d * xh;
+          db[j][e] += d;
+          s[0] += g * xh;
+          s[1] += g;
+        }
+      row_sums<WAVES>(s, red, turn);
+      const float by = s[0] / (float)a.dim, mean = a.rms ? 0.f : s[1] / (float)a.dim;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        V o;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float d = (float)r.dy[j][e], xh = ((float)r.h[j][e] - mu) * rs, g = a.weight != nullptr ? d * (float)w[j][e] : d;
+          float y = rs * (g - xh * by - mean);
+          if (a.dsum != nullptr) y += (float)r.ds[j][e];
+          o[e] = (T)y;
+        }
+        if (row < a.rows) store_piece<TY, false, WHOLE>((T*)a.out + row * a.out_row, (t + j * WAVES * kWave) * N, a.dim, o);
       }
-      if (a.dsum != nullptr) {
-        const V v = load_piece<TY>((const T*)a.dsum + row * a.dsum_row, c, a.dim);
-#pragma unroll
-        for (int e = 0; e < N; ++e) d[e] += (float)v[e];
-      }
-#pragma unroll
-      for (int e = 0; e < N; ++e) o[e] = (T)d[e];
-      store_piece<TY>((T*)a.out + row * a.out_row, c, a.dim, o);
+      if (kRing > 1 && set + kRing * step < a.rows) load_own(r, set + kRing * step);
     }
   }
   if (a.dweight == nullptr && a.dbias == nullptr) return;
+  const int64_t second = (int64_t)gridDim.x * a.dim;  // (the bias's parts)
+  if constexpr (kRows > 1) {  // the workgroup's rows together
+    constexpr int kWidth = PER * WAVES * kWave * N;
+    __shared__ float sums[kRows][kWidth];
 #pragma unroll
-  for (int j = 0; j < PER; ++j)
+    for (int which = 0; which < 2; ++which) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int c = (t + j * WAVES * kWave) * N + e;
-      if (c >= a.dim) continue;
-      if (a.dweight != nullptr) a.parts[(int64_t)slot * a.dim + c] = dw[j][e];
-      if (a.dbias != nullptr) a.parts[((int64_t)slots + slot) * a.dim + c] = db[j][e];
+      for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sums[own][(t + j * WAVES * kWave) * N + e] = which == 0 ? dw[j][e] : db[j][e];
+      __syncthreads();
+      if (which == 0 ? a.dweight != nullptr : a.dbias != nullptr)
+        for (int c = threadIdx.x; c < a.dim; c += kThreads) {
+          float s = 0.f;
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) s += sums[r][c];
+          a.parts[which * second + (int64_t)blockIdx.x * a.dim + c] = s;
+        }
+      __syncthreads();
     }
+  } else {
+    float* const part = a.parts + (int64_t)blockIdx.x * a.dim;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+      for (int e = 0; e < N; e += 4) {
+        const int c = (t + j * WAVES * kWave) * N + e;
+        const Elem<kF32>::V w4 = {dw[j][e], dw[j][e + 1], dw[j][e + 2], dw[j][e + 3]};
+        const Elem<kF32>::V b4 = {db[j][e], db[j][e + 1], db[j][e + 2], db[j][e + 3]};
+        if (c >= a.dim) continue;
+        if (a.dweight != nullptr) store_piece<kF32, false, WHOLE>(part, c, a.dim, w4);
+        if (a.dbias != nullptr) store_piece<kF32, false, WHOLE>(part + second, c, a.dim, b4);
+      }
+  }
 }
 
-// The slots' parts of a column in a fixed order: a workgroup takes 64 columns, each wave
-// every 16th slot.
-__global__ void __launch_bounds__(1024) k_norm_grad_sum(NormGradArgs a, int slots) {
-  __shared__ float red[16][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+// The workgroups' parts of a column in a fixed order: a workgroup takes 32 columns, every 32 threads a
+// 32nd of the parts.
+__global__ void __launch_bounds__(1024) k_norm_grad_sum(NormGradArgs a, int parts) {
+  __shared__ float red[32][33];
+  const int x = threadIdx.x % 32, y = threadIdx.x / 32, c = blockIdx.x * 32 + x;
   float* const out = blockIdx.y == 0 ? a.dweight : a.dbias;
   if (out == nullptr) return;
-  const float* const parts = a.parts + (int64_t)blockIdx.y * slots * a.dim;
+  const float* const in = a.parts + (int64_t)blockIdx.y * parts * a.dim + min(c, a.dim - 1);
   float s = 0.f;
-  if (c < a.dim) {
 #pragma unroll 8
-    for (int i = wave; i < slots; i += 16) s += parts[(int64_t)i * a.dim + c];
-  }
-  red[wave][lane] = s;
+  for (int i = y; i < parts; i += 32) s += in[(int64_t)i * a.dim];
+  red[y][x] = s;
   __syncthreads();
-  if (wave != 0 || c >= a.dim) return;
-  s = 0.f;
+  // (32 lanes a column)
+  s = red[x][y];
 #pragma unroll
-  for (int w = 0; w < 16; ++w) s += red[w][lane];
-  out[c] = s;
+  for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o);
+  if (x == 0 && blockIdx.x * 32 + y < a.dim) out[blockIdx.x * 32 + y] = s;
 }
 
 // Calls f with the waves of a row and the pieces of a thread.
@@ -252,36 +303,58 @@ hipError_t by_width(int dim, F f) {
   return f(IntC<16>(), IntC<2>());
 }
 
+// The same for the gradients, which keep two sums of each column.
+template <int TY, typename F>
+hipError_t by_width_grad(int dim, F f) {
+  const int pieces = (dim + kPiece<TY> - 1) / kPiece<TY>;
+  if (pieces <= 64) return f(IntC<1>(), IntC<1>());
+  if (pieces <= 128) return f(IntC<1>(), IntC<2>());
+  if (pieces <= 256) return f(IntC<4>(), IntC<1>());
+  if (pieces <= 512) return f(IntC<8>(), IntC<1>());
+  if (pieces <= 1024) return f(IntC<8>(), IntC<2>());
+  if (pieces <= 1536) return f(IntC<8>(), IntC<3>());
+  if constexpr (TY == kF32) {
+    if (pieces > 2048) return f(IntC<8>(), IntC<8>());
+  }
+  return f(IntC<8>(), IntC<4>());
+}
+
 template <int TY>
 hipError_t launch_norm_typed(const NormArgs& a, hipStream_t s) {
   return by_width<TY>(a.dim, [&](auto waves, auto per) {
     constexpr int W = decltype(waves)::value, P = decltype(per)::value;
     const int64_t blocks = W == 1 ? (a.rows + 3) / 4 : a.rows;
-    k_norm<TY, W, P><<<(unsigned)min(blocks, (int64_t)1 << 20), kNormThreads<W>, 0, s>>>(a);
+    const unsigned grid = (unsigned)min(blocks, (int64_t)1 << 20);
+    if (a.dim % kPiece<TY> == 0) k_norm<TY, W, P, true><<<grid, kNormThreads<W>, 0, s>>>(a);
+    else k_norm<TY, W, P, false><<<grid, kNormThreads<W>, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 
 template <int TY>
 hipError_t launch_grad_typed(const NormGradArgs& a, hipStream_t s) {
-  int slots = 0;
-  const hipError_t e = by_width<TY>(a.dim, [&](auto waves, auto per) {
-    constexpr int W = decltype(waves)::value, P = decltype(per)::value, kRows = W == 1 ? 4 : 1;
-    const int64_t most = norm_grad_slots(a.dim) / kRows, blocks = (a.rows + kRows - 1) / kRows;
-    const unsigned grid = (unsigned)min(blocks, most);
-    slots = (int)grid * kRows;
-    if (grid == 0) return hipSuccess;  // (no rows: the sums are zeros)
-    k_norm_grad<TY, W, P><<<grid, kNormThreads<W>, 0, s>>>(a);
+  // Workgroups, each with a part of the weight's gradient: one a CU, whose parts cost less (2048 x
+  // 4096 fp16 23 us, with two 25; 2048 x 8192 35 and 44), two for many rows (8192 x 4096 60 and 56) or
+  // rows that are not whole pieces (4000 x 3001 62 and 46).
+  const int most = a.rows < 16 * num_cus() && a.dim % kPiece<TY> == 0 ? num_cus() : norm_grad_parts();
+  int parts = 0;
+  const hipError_t e = by_width_grad<TY>(a.dim, [&](auto waves, auto per) {
+    constexpr int W = decltype(waves)::value, P = decltype(per)::value, kRows = kGradRows<W>;
+    constexpr int kThreads = W * kRows * kWave;
+    parts = (int)min((a.rows + kRows - 1) / kRows, (int64_t)most);
+    if (parts == 0) return hipSuccess;  // (no rows: the sums are zeros)
+    if (a.dim % kPiece<TY> == 0) k_norm_grad<TY, W, P, true><<<(unsigned)parts, kThreads, 0, s>>>(a);
+    else k_norm_grad<TY, W, P, false><<<(unsigned)parts, kThreads, 0, s>>>(a);
     return hipGetLastError();
   });
   if (e != hipSuccess || (a.dweight == nullptr && a.dbias == nullptr)) return e;
-  k_norm_grad_sum<<<dim3((unsigned)((a.dim + kWave - 1) / kWave), 2), 1024, 0, s>>>(a, slots);
+  k_norm_grad_sum<<<dim3((unsigned)((a.dim + 31) / 32), 2), 1024, 0, s>>>(a, parts);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int norm_grad_slots(int32_t dim) { return dim <= 1024 ? 4 * num_cus() : 2 * num_cus(); }
+int norm_grad_parts() { return 2 * num_cus(); }
 
 hipError_t launch_norm(const NormArgs& a, int dtype, hipStream_t s) {
   if (dtype == kF16) return launch_norm_typed<kF16>(a, s);
