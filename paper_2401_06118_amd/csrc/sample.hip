@@ -226,6 +226,62 @@ __device__ __forceinline__ uint64_t sum_few(Shared& sh, int turn, uint64_t m, in
   return m;
 }
 
+// Appends to dest, n of them so far in LDS and `cap` at most, the places of those of a wave's K elements a lane that
+// hit; all lanes call it.  One atomic a wave.
+template <int K, typename H, typename P>
+__device__ __forceinline__ void append(int32_t& n, uint64_t* dest, int cap, H hit, P place) {
+  uint64_t masks[K];
+  int total = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    masks[k] = __ballot(hit(k));
+    total += __popcll(masks[k]);
+  }
+  if (total == 0) return;
+  const int lane = threadIdx.x % kWave;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&n, total);
+  at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (masks[k] == 0) continue;
+    const int to = at + __popcll(masks[k] & ((1ull << lane) - 1));
+    if ((masks[k] >> lane & 1) && to < cap) dest[to] = place(k);
+    at += __popcll(masks[k]);
+  }
+}
+
+// The row's tokens with low <= l c < high appended.
+template <int TY, int THREADS>
+__device__ __forceinline__ void append_row(int32_t& n, uint64_t* dest, int cap, const void* row, int vocab, float c,
+                                           float low, float high) {
+  constexpr int N = kPiece<TY>, kBatch = 32 / N;
+  // (whole waves: lanes past the end have nothing)
+  for (int i0 = 0; i0 < vocab; i0 += kBatch * THREADS * N) {
+    typename Elem<TY>::V v[kBatch];
+    const int i1 = i0 + threadIdx.x * N;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i1 + j * THREADS * N;
+      if (i + N <= vocab) {
+        v[j] = *(const typename Elem<TY>::V*)((const typename Elem<TY>::T*)row + i);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          v[j][e] = i + e < vocab ? ((const typename Elem<TY>::T*)row)[i + e] : (typename Elem<TY>::T)-INFINITY;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; j += 8 / N)  // (8 elements at a time: their masks are 16 scalar registers)
+      append<8>(n, dest, cap, [&](int k) {
+        const float f = (float)v[j + k / N][k % N] * c;
+        return f >= low && f < high;
+      }, [&](int k) {
+        return place_of((float)v[j + k / N][k % N], i1 + (j + k / N) * THREADS * N + k % N);
+      });
+  }
+}
+
 // Calls f(number, logit) for every token of the row that is not masked.
 template <int TY, int THREADS, typename F>
 __device__ __forceinline__ void each(const void* row, int vocab, F f) {
@@ -483,14 +539,14 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
   }
 }
 
-// all: the row's mass.  visit(low, high, edge bin, take) calls take(l, place) for all tokens with
-// low <= l c < high.  kDrawn: the token is written; kKnown: the edge is, and sh.list begins
+// all: the row's mass.  collect(low, high, edge bin, dest, cap) appends the places of all tokens with
+// low <= l c < high to dest, sh.listing of them.  kDrawn: the token is written; kKnown: the edge is, and sh.list begins
 // with the sh.found_in tokens beside it that are kept; kUnknown: draw_slowly.
 // by_count: sh.count need not count all, but show a bin down to which there are k.
 // pool [kPool]: place for tokens, or null; edge.pooled: how many of the edge's bin it has.
 template <int THREADS, typename F>
 __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const SampleArgs& a, int b, const Rules& r,
-                                          bool by_count, uint64_t all, int top_bin, Edge& edge, F visit) {
+                                          bool by_count, uint64_t all, int top_bin, Edge& edge, F collect) {
   constexpr int kEach = kList / THREADS;
   const int tid = threadIdx.x, wave = tid / kWave;
   const bool whole = r.k > 0 && r.top_p;  // (top-p's limit needs the first k's mass)
@@ -504,19 +560,12 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   bool listed = by_count || before + in_edge <= kList;  // all that can be kept is in the list
   float low = bins.lower(edge.bin), high = listed ? INFINITY : bins.upper(edge.bin);
   if (whole && !listed) return kUnknown;
-  auto list = [&](float, uint64_t place) {
-    const int at = atomicAdd(&sh.listing, 1);
-    if (at < kList) sh.list[at] = place;
-  };
   if (listed || in_edge <= kList) {
-    visit(low, high, edge.bin, list);
+    collect(low, high, edge.bin, sh.list, kList);
   } else {
     // more than the list holds: by the 512 parts of the bin
     if (pool == nullptr || in_edge > kPool || !(fabsf(low) < 0x1p14f)) return kUnknown;
-    visit(low, high, edge.bin, [&](float, uint64_t place) {
-      const int at = atomicAdd(&sh.listing, 1);
-      if (at < kPool) pool[at] = place;
-    });
+    collect(low, high, edge.bin, pool, kPool);
     lds_barrier();
     for (int i = tid; i < kBins; i += THREADS) {
       sh.mass[i] = 0;
@@ -542,7 +591,7 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
     if (sh.found_in > kList) return kUnknown;
     for (int i = tid; i < edge.pooled; i += THREADS) {
       const float f = logit_of((uint32_t)(pool[i] >> 32)) * r.c;
-      if (f >= low && f < high) list(f, pool[i]);
+      if (f >= low && f < high) sh.list[atomicAdd(&sh.listing, 1)] = pool[i];
     }
   }
   if (listed) {
@@ -551,7 +600,7 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   }
   lds_barrier();
   const int n = sh.listing;
-  if (n > kList) return kUnknown;  // (by_count only)
+  if (n > kList) return kUnknown;  // (where bins do not count all)
   edge.high = high;
   auto keeps = [&](uint32_t rank, uint64_t mass_before, float l, double most) {
     return (r.k == 0 || rank < (uint32_t)r.k) && (!r.top_p || (double)mass_before < most) &&
@@ -939,7 +988,8 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
       } else {
         all = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, true, false, [](int bin) { return bin; }));
       }
-      o = choose<THREADS>(sh, nullptr, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, auto take) {
+      o = choose<THREADS>(sh, nullptr, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, uint64_t* dest,
+                                                                                         int cap) {
         if (ROUNDS > 1 && by_count) {
           // few threads hold any: theirs are dealt to all
           const bool hit = mine * r.c >= low;
@@ -952,10 +1002,11 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
           lds_barrier();
           const int n = hits;
           if (n <= kHits) {
-            for (int i = tid; i < n * ROUNDS * N; i += THREADS) {
-              const int w = i / (ROUNDS * N), j = i / N % ROUNDS, e = i % N;
+            for (int i0 = 0; i0 < n * ROUNDS * N; i0 += THREADS) {
+              const int i = min(i0 + tid, n * ROUNDS * N - 1), w = i / (ROUNDS * N), j = i / N % ROUNDS, e = i % N;
               const float l = (float)((const T*)&dealt[w][j])[e];
-              if (l * r.c >= low) take(l, place_of(l, (j * THREADS + whose[w]) * N + e));
+              append<1>(sh.listing, dest, cap, [&](int) { return i == i0 + tid && l * r.c >= low; },
+                        [&](int) { return place_of(l, (j * THREADS + whose[w]) * N + e); });
             }
             return;
           }
@@ -963,13 +1014,10 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
 #pragma unroll
         for (int j = 0; j < ROUNDS; ++j) {
           asm volatile("" : "+v"(v[j]));
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            float l = (float)v[j][e];
-            asm volatile("" : "+v"(l));
-            const float f = l * r.c;
-            if (f >= low && f < high) take(l, place_of(l, (j * THREADS + tid) * N + e));
-          }
+          append<N>(sh.listing, dest, cap, [&](int e) {
+            const float f = (float)v[j][e] * r.c;
+            return f >= low && f < high;
+          }, [&](int e) { return place_of((float)v[j][e], (j * THREADS + tid) * N + e); });
         }
       });
     }
@@ -1040,16 +1088,12 @@ __global__ void __launch_bounds__(kSliceThreads) k_sample_slices(SampleArgs a) {
         rec.cut = sh.found - 1;
         const float low = (float)(upper - rec.cut);
 #pragma unroll
-        for (int j = 0; j < ROUNDS; ++j)
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const float l = (float)v[j][e];
-            if (l * r.c >= low) {
-              const int to = atomicAdd(&sh.listing, 1);
-              if (to < kSampleListed)
-                a.lists[at * kSampleListed + to] = place_of(l, slice * kSampleSlice + (j * THREADS + tid) * N + e);
-            }
-          }
+        for (int j = 0; j < ROUNDS; j += 8 / N)
+          append<8>(sh.listing, a.lists + at * kSampleListed, kSampleListed,
+                    [&](int k) { return (float)v[j + k / N][k % N] * r.c >= low; }, [&](int k) {
+                      return place_of((float)v[j + k / N][k % N],
+                                      slice * kSampleSlice + ((j + k / N) * THREADS + tid) * N + k % N);
+                    });
         lds_barrier();
         rec.listed = sh.listing;
         if (rec.listed > kSampleListed) {  // (by_count only)
@@ -1097,7 +1141,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
     const int top_bin = bin_of(r.max_f, r.c), lower = some ? top_bin - bin_of(rec.top, r.c) : 2 * kBins;
     if (has_bins(r)) {
       const uint64_t all = wave_sum64(mass);
-      // Calls f(place) for all that the slices' lists hold.
+      // Calls f(held, place) for all that the slices' lists hold, by whole waves.
       auto lists = [&](auto f) {
         for (int s = wave; s < slices; s += THREADS / kWave) {
           const int n = __builtin_amdgcn_readlane(rec.listed, s);
@@ -1108,15 +1152,15 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
             if (j * kWave < n) e[j] = list[min(j * kWave + lane, n - 1)];
 #pragma unroll
           for (int j = 0; j < kSampleListed / kWave; ++j)
-            if (j * kWave + lane < n) f(e[j]);
+            if (j * kWave < n) f(j * kWave + lane < n, e[j]);
         }
       };
       if (by_count) {
         if (tid < kBins) sh.count[tid] = 0;
         lds_barrier();
-        lists([&](uint64_t place) {
+        lists([&](bool held, uint64_t place) {
           const int bin = top_bin - low_bin_of(logit_of((uint32_t)(place >> 32)), r.c);
-          if (bin < kBins - 1) atomicAdd(&sh.count[bin], 1u);
+          if (held && bin < kBins - 1) atomicAdd(&sh.count[bin], 1u);
         });
       } else if (tid < kBins) {
         // the row's bins, a thread each; the lowest one has what has no mass
@@ -1149,17 +1193,15 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
       lds_barrier();
       // (of counted rows every slice lists the first k, or it does not count here)
       if (!by_count || __ballot(some && rec.cut < 0) == 0)
-        o = choose<THREADS>(sh, pool, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int edge_bin, auto take) {
+        o = choose<THREADS>(sh, pool, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int edge_bin,
+                                                                                uint64_t* dest, int cap) {
           if (by_count || __ballot(some && edge_bin - lower > rec.cut) == 0)
-            lists([&](uint64_t place) {
-              const float l = logit_of((uint32_t)(place >> 32)), f = l * r.c;
-              if (f >= low && f < high) take(l, place);
+            lists([&](bool held, uint64_t place) {
+              const float f = logit_of((uint32_t)(place >> 32)) * r.c;
+              append<1>(sh.listing, dest, cap, [&](int) { return held && f >= low && f < high; }, [&](int) { return place; });
             });
           else
-            each<TY, THREADS>(row, a.vocab, [&](int i, float l) {
-              const float f = l * r.c;
-              if (f >= low && f < high) take(l, place_of(l, i));
-            });
+            append_row<TY, THREADS>(sh.listing, dest, cap, row, a.vocab, r.c, low, high);
         });
     }
     if (o == kDrawn) return;
