@@ -111,6 +111,13 @@ __device__ __forceinline__ uint64_t weight_of(const Rules& r, float l) {
 // 2^y for y <= 0.
 __device__ __forceinline__ double factor(double y) { return y > -1000.0 ? exp2(y) : 0.0; }
 
+// At least as many tokens as have this mass in a bin whose lower end is `lower`: each has the
+// weight there or more.
+__device__ __forceinline__ uint32_t most_of(const Rules& r, uint64_t mass, float lower) {
+  const float each = (r.max_f * r.c - lower) * (1.44269504f / 16.f) - 44.f;  // -log2 of the least weight
+  return mass == 0 ? 0 : (uint32_t)fminf((float)mass * __builtin_amdgcn_exp2f(each) * 1.01f, 1e9f) + 1;
+}
+
 struct Shared {
   union {
     struct {
@@ -487,8 +494,9 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
   uint32_t count[kEach], c = 0;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
-    mass[j] = by_count ? 0 : sh.mass[lane * kEach + j];
-    count[j] = sh.count[lane * kEach + j];
+    const int bin = lane * kEach + j;
+    mass[j] = by_count ? 0 : sh.mass[bin];
+    count[j] = by_count || r.k > 0 || bins.fine ? sh.count[bin] : most_of(r, mass[j], bins.lower(bin));
     m += mass[j];
     c += count[j];
   }
@@ -514,7 +522,7 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     bool limit = r.k > 0 && bc < (uint32_t)r.k && (uint32_t)r.k <= bc + count[j];
-    if (!by_count && !whole) limit |= r.top_p && count[j] != 0 && (double)(bm + mass[j]) >= most;
+    if (!by_count && !whole) limit |= r.top_p && mass[j] != 0 && (double)(bm + mass[j]) >= most;
     if (limit) mine = min(mine, lane * kEach + j);
     bm += mass[j];
     bc += count[j];
@@ -557,10 +565,12 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   uint32_t before = sh.found_count;
   uint64_t before_mass = sh.found_mass;
   uint32_t in_edge = sh.found_in;
-  bool listed = by_count || before + in_edge <= kList;  // all that can be kept is in the list
+  // Whether all that can be kept is in the list.  (Sorting 2048 takes 12 us, twice; a part of a bin that
+  // few share does not need it.)
+  const bool listed = by_count || before + in_edge <= (uint32_t)(whole || pool == nullptr ? kList : kFew);
   float low = bins.lower(edge.bin), high = listed ? INFINITY : bins.upper(edge.bin);
   if (whole && !listed) return kUnknown;
-  if (listed || in_edge <= kList) {
+  if (listed || in_edge <= (uint32_t)(pool == nullptr ? kList : kFew)) {
     collect(low, high, edge.bin, sh.list, kList);
   } else {
     // more than the list holds: by the 512 parts of the bin
@@ -647,6 +657,18 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   }
 
   auto sort = [&](int n) {
+    if (n <= kFew) {  // each to its rank
+      const uint64_t own = tid < n ? sh.list[tid] : 0;
+      int rank = 0;
+      if (wave * kWave < n) {
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += sh.list[j] < own;
+      }
+      lds_barrier();
+      if (tid < n) sh.list[rank] = own;
+      lds_barrier();
+      return;
+    }
     int size = 2;
     while (size < n) size <<= 1;
     for (int i = n + tid; i < size; i += THREADS) sh.list[i] = ~0ull;
@@ -901,7 +923,7 @@ __device__ __forceinline__ int first_of(Shared& sh, const typename Elem<TY>::V (
 // slot(bin): where a bin is kept.
 template <int TY, int ROUNDS, typename S>
 __device__ __forceinline__ uint64_t count_bins(Shared& sh, const Rules& r, typename Elem<TY>::V (&v)[ROUNDS], bool filtered,
-                                               bool by_count, S slot) {
+                                               S slot) {
   constexpr int G = 4;  // weights at a time (all at once would take too many registers)
   const int upper = bin_of(r.max_f, r.c);
   uint64_t total = 0;
@@ -916,17 +938,15 @@ __device__ __forceinline__ uint64_t count_bins(Shared& sh, const Rules& r, typen
         l[e] = (float)v[j][e0 + e];
         asm volatile("" : "+v"(l[e]));
       }
-      if (!by_count) {
 #pragma unroll
-        for (int e = 0; e < G; ++e) total += w[e] = weight_of(r, l[e]);
-      }
+      for (int e = 0; e < G; ++e) total += w[e] = weight_of(r, l[e]);
       if (filtered) {
 #pragma unroll
         for (int e = 0; e < G; ++e) {
           const int bin = upper - low_bin_of(l[e], r.c);  // (masked ones: far below)
           if (bin >= kBins - 1) continue;
-          atomicAdd(&sh.count[slot(bin)], 1u);
-          if (!by_count) atomicAdd((unsigned long long*)&sh.mass[slot(bin)], (unsigned long long)w[e]);
+          if (r.k > 0) atomicAdd(&sh.count[slot(bin)], 1u);  // (else: most_of)
+          atomicAdd((unsigned long long*)&sh.mass[slot(bin)], (unsigned long long)w[e]);
         }
       }
     }
@@ -986,7 +1006,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
         if (bin < kBins - 1) atomicAdd(&sh.count[bin], 1u);
         lds_barrier();
       } else {
-        all = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, true, false, [](int bin) { return bin; }));
+        all = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, true, [](int bin) { return bin; }));
       }
       o = choose<THREADS>(sh, nullptr, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, uint64_t* dest,
                                                                                          int cap) {
@@ -1065,16 +1085,14 @@ __global__ void __launch_bounds__(kSliceThreads) k_sample_slices(SampleArgs a) {
         if (bin < kBins - 1) atomicAdd(&sh.count[slot(bin)], 1u);
         lds_barrier();
       } else {
-        rec.mass = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, filtered, false, slot));
+        rec.mass = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, filtered, slot));
       }
       if (filtered) {
-        if (!by_count) {
-          a.counts[at * kBins + tid] = sh.count[tid];
-          a.masses[at * kBins + tid] = sh.mass[tid];
-        }
+        if (!by_count) a.masses[at * kBins + tid] = sh.mass[tid];
+        if (!by_count && r.k > 0) a.counts[at * kBins + tid] = sh.count[tid];
         // the first tokens: down to the bin with the k-th, or to the last one up to which a list holds all
         uint64_t none = 0;
-        const uint32_t own = sh.count[slot(tid)];
+        const uint32_t own = by_count || r.k > 0 ? sh.count[slot(tid)] : most_of(r, sh.mass[slot(tid)], (float)(upper - tid));
         uint32_t c = own;
         sums_before<THREADS>(sh, none, c);
         if (tid == 0) {
@@ -1174,7 +1192,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
 #pragma unroll
           for (int j = 0; j < kBatch; ++j) {
             const int64_t i = (at + min(s0 + j, slices - 1)) * kBins + tid;
-            counts[j] = a.counts[i];
+            counts[j] = r.k > 0 ? a.counts[i] : 0;
             masses[j] = a.masses[i];
           }
 #pragma unroll
