@@ -2,20 +2,22 @@
 lengths go through the blocks in chunks, then all sequences are decoded together,
 one token a step.
 
-    python3 examples/generate.py [--layers 2] [--tokens 16] [--chunk 64]
+    python3 examples/generate.py [--layers 2] [--tokens 16] [--chunk 64] [--temperature 0.8] [--top-p 0.9]
 
 The model is a small Llama-shaped one with random 2x8 codes and head norms (there
 are no checkpoints here); what it shows is how the calls fit together:
 
-    q, k, v products (gemm)      -> paged_append  (norms, rotation, cache)
+    embed                        -> the residual stream
+    layer_norm (RMS form, with the sum before it)
+    q, k, v products (gemm)      -> paged_append  (head norms, rotation, cache)
                                  -> paged_attention over the cache
     o, gate, up, down products   (gemm)
-    LM head, then process_logits (penalties, biases, a grammar mask), then the
-    largest logit.
+    LM head, then process_logits (penalties, biases, a grammar mask), then sample
+    (temperature 0, the default: the largest logit).
 
-Norms of the residual stream and the gate's activation are plain torch.
-``head_gradients`` shows the training form: gradients of the q and k codebooks of a
-block through rope and its backward.
+The gate's activation is plain torch.  The training forms: ``head_gradients``, the q and k
+codebooks of a block through rope and its backward; ``end_gradients``, a step against a
+teacher's largest logits through the loss, the last norm and the embedding.
 """
 from __future__ import annotations
 
@@ -72,24 +74,26 @@ class Model:
     def forward(self, tokens, cache, block_table, kv_lens, cu_new, max_new):
         """Logits after each sequence's last new token.  ``tokens`` int64 [n], one sequence after
         another; ``kv_lens`` and ``cu_new`` as for aqlm.paged_append."""
-        x = self.embedding[tokens]
+        x, more = aqlm.embed(self.embedding, tokens.int()), None
         for b, (k_cache, v_cache) in zip(self.blocks, cache):
-            h = rms(x)
+            h, x = rms(x, more)
             qkv = b["qkv"](h).view(len(tokens), self.heads + 2 * self.kv, self.dim)
             q, k, v = qkv.split((self.heads, self.kv, self.kv), 1)
             where = (k_cache, v_cache, block_table, kv_lens, cu_new)
             q = aqlm.paged_append(q, k, v, *where, table=self.table, q_weight=b["q_weight"], k_weight=b["k_weight"],
                                   eps=EPS, out=q)
-            x = x + b["o"](aqlm.paged_attention(q, *where, max_new=max_new).flatten(1))
-            h = rms(x)
-            x = x + b["down"]((torch.nn.functional.silu(b["gate"](h).float()) * b["up"](h).float()).half())
-        last = rms(x[cu_new[1:].long() - 1])
+            h, x = rms(x, b["o"](aqlm.paged_attention(q, *where, max_new=max_new).flatten(1)))
+            more = b["down"]((torch.nn.functional.silu(b["gate"](h).float()) * b["up"](h).float()).half())
+        at = cu_new[1:].long() - 1
+        last, _ = rms(x[at], more[at])
         return last @ self.head.t() / self.hidden ** 0.5
 
 
-def rms(x):
-    x = x.float()
-    return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS)).half()
+def rms(x, more):
+    """The norm of the residual stream after ``more`` is added to it, and the stream."""
+    if more is None:
+        return aqlm.layer_norm(x, rms=True, eps=EPS), x
+    return aqlm.layer_norm(x, residual=more, rms=True, eps=EPS)
 
 
 def head_gradients(model, block, x, dq, dk, positions):
@@ -105,8 +109,26 @@ def head_gradients(model, block, x, dq, dk, positions):
     return (*aqlm.backward(*b["qkv"].parts, x, dy), gq_weight, gk_weight)
 
 
-def generate(model, prompts, new_tokens, *, chunk=64, page_size=16, repetition=1.3, presence=0.2, banned=(), allowed=None):
-    """Greedy continuations of the prompts (lists of ids): int64 [sequences, new_tokens]."""
+def end_gradients(model, tokens, weight, teacher_logits, teacher_ids, teacher_lse, loss_scale=1.0):
+    """A step of the model's two ends alone, embedding, norm (``weight``) and head, against a
+    teacher of whom each token's largest logits are known: the mean loss, and loss_scale times its
+    gradients of the embedding (fp32), the norm's weight and the head."""
+    n, scale = len(tokens), model.hidden ** -0.5
+    x = aqlm.embed(model.embedding, tokens)
+    h = aqlm.layer_norm(x, weight, rms=True, eps=EPS)
+    logits = h @ model.head.t() * scale
+    share = torch.full((n,), loss_scale / n, device=logits.device)
+    loss, dlogits = aqlm.distill_loss(logits, teacher_logits, teacher_ids, teacher_lse=teacher_lse, weights=share,
+                                      out=logits)
+    dh = dlogits @ model.head * scale
+    dx, dweight, _ = aqlm.layer_norm_backward(dh, x, weight, rms=True, eps=EPS)
+    return loss.mean(), aqlm.embed_backward(dx, tokens, model.vocab, fp32=True), dweight, dlogits.t() @ h * scale
+
+
+def generate(model, prompts, new_tokens, *, chunk=64, page_size=16, repetition=1.3, presence=0.2, banned=(), allowed=None,
+             temperature=0.0, top_p=1.0, seed=0):
+    """Continuations of the prompts (lists of ids), greedy at temperature 0: int32
+    [sequences, new_tokens]."""
     dev, seqs = model.device, len(prompts)
     most = max(len(p) for p in prompts) + new_tokens
     width = -(-most // page_size)
@@ -143,12 +165,14 @@ def generate(model, prompts, new_tokens, *, chunk=64, page_size=16, repetition=1
     if allowed is not None:
         rules["mask"] = allowed.repeat(seqs, 1)
     cu = torch.arange(seqs + 1, dtype=torch.int32, device=dev)
+    draw = dict(temperature=torch.full((seqs,), temperature, device=dev), top_p=torch.full((seqs,), top_p, device=dev))
+    gen = torch.Generator(device=dev).manual_seed(seed)
     out = []
     for step in range(new_tokens):
         scored = aqlm.process_logits(logits, tokens=history, token_lens=lens, prompt_lens=prompt_lens, **rules)
-        token = scored.argmax(-1)
+        token = aqlm.sample(scored, torch.rand(seqs, generator=gen, device=dev), **draw)
         out.append(token)
-        history.scatter_(1, lens[:, None].long(), token[:, None].to(torch.int32))
+        history.scatter_(1, lens[:, None].long(), token[:, None])
         lens += 1
         if step + 1 < new_tokens:
             logits = model.forward(token, cache, table, lens, cu, 1)
@@ -160,11 +184,14 @@ def main():
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--tokens", type=int, default=16)
     ap.add_argument("--chunk", type=int, default=64)
+    ap.add_argument("--temperature", type=float, default=0.0)
+    ap.add_argument("--top-p", type=float, default=1.0)
     a = ap.parse_args()
     model = Model(layers=a.layers)
     gen = torch.Generator().manual_seed(1)
     prompts = [torch.randint(0, model.vocab, (n,), generator=gen).tolist() for n in (5, 130, 77, 1)]
-    for p, t in zip(prompts, generate(model, prompts, a.tokens, chunk=a.chunk).tolist()):
+    for p, t in zip(prompts, generate(model, prompts, a.tokens, chunk=a.chunk, temperature=a.temperature,
+                                          top_p=a.top_p).tolist()):
         print(f"prompt of {len(p)} tokens ->", t)
 
 

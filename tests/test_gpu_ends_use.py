@@ -237,3 +237,53 @@ def test_step_and_gradients_together(aq):
         assert (got.double() - want).abs().max() <= 1e-5 * want.abs().max()
     for i in range(rows):
         assert int(token[i]) in torch.topk(z[i], 10).indices.tolist()
+
+
+@pytest.fixture(scope="module")
+def example():
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "generate.py")
+    spec = importlib.util.spec_from_file_location("generate_example_ends", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def test_example_draws(aq, example):
+    """Drawn continuations: the same for the same seed, allowed tokens only, the greedy one at a temperature of 0."""
+    model = example.Model()
+    prompts = [[5, 7, 11], [13], [1] * 40]
+    a, b = (example.generate(model, prompts, 6, temperature=0.9, top_p=0.95, seed=4) for _ in range(2))
+    assert torch.equal(a, b) and (a >= 0).all() and (a < model.vocab).all()
+    allowed = torch.zeros(1, -(-model.vocab // 32), dtype=torch.int32, device=DEV)
+    allowed[0, 3] = 0x0F0F
+    out = example.generate(model, prompts, 4, allowed=allowed, temperature=1.5)
+    assert all(96 <= t < 112 and (0x0F0F >> (t - 96)) & 1 for t in out.flatten().tolist())
+    assert torch.equal(example.generate(model, prompts, 3), example.generate(model, prompts, 3, seed=9))
+
+
+def test_example_end_gradients(aq, example):
+    """The gradients of the example's step against automatic differentiation in 64 bits."""
+    model = example.Model(layers=1, hidden=128, vocab=500)
+    ids = ids_of(95, 33, 500)
+    w = (1 + 0.1 * rand(96, 128)).half()
+    teacher = rand(97, 33, 500) * 2
+    top, tid = torch.topk(teacher, 12)
+    lse = torch.logsumexp(teacher, 1)
+    loss, de, dw, dhead = example.end_gradients(model, ids, w, top, tid.int(), lse, loss_scale=1024.0)
+    E, W, H = (t.double().requires_grad_() for t in (model.embedding, w, model.head))
+    held = ((ids >= 0) & (ids < 500))[:, None]
+    x = torch.where(held, E[ids.long().clamp(0, 499)], 0.0)
+    z = (x * (x.square().mean(1, keepdim=True) + example.EPS).rsqrt() * W) @ H.t() / 128 ** 0.5
+    lq, lp = torch.log_softmax(z, 1), top.double() - lse.double()[:, None]
+    outside = torch.ones(33, 500, device=DEV).scatter_(1, tid, 0.0).bool()
+    pr = 1 - lp.exp().sum(1)
+    L = (lp.exp() * (lp - lq.gather(1, tid))).sum(1) + pr * (pr.log() - lq.masked_fill(~outside, -torch.inf).logsumexp(1))
+    L.mean().backward()
+    # about six roundings to fp16 on the way, each of 2^-11 of values of the result's size
+    want = L.mean().item()
+    assert abs(float(loss) - want) <= 6 * 2.0 ** -11 * want
+    for got, want in ((de, E.grad), (dw, W.grad), (dhead, H.grad)):
+        assert (got.double() / 1024 - want).norm() <= 6 * 2.0 ** -11 * want.norm()
