@@ -177,6 +177,23 @@ def test_layer_norm_backward(aq, dtype, dim, rms):
         assert torch.isnan(around(t[which])).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [500, 1000, 2056, 4100, 5120, 8199, 12296, 16384])
+def test_layer_norm_backward_many_rows(aq, dtype, dim):
+    """More rows than workgroups: each takes several, some one more than others."""
+    rows = 1101
+    x = (rand(18, rows, dim) * (0.5 + uniform(19, rows, 1)) + 0.5).to(dtype)
+    dy, w = rand(20, rows, dim, dtype=dtype), rand(21, dim, dtype=dtype)
+    for dsum, rms in ((None, False), (x, True)):
+        (dx, dx_off), (dw, dw_off), (db, db_off) = ref.norm_grad(dy, x, w, dsum, 1e-5, rms)
+        got = aq.layer_norm_backward(dy, x, w, dsum=dsum, rms=rms, bias=True)
+        ref.check(got[0], dx, dx_off + ref.rounded(dx.abs() + dx_off, dtype), "dx")
+        ref.check(got[1], dw, dw_off + ref.rounded(dw, F32), "dweight")
+        ref.check(got[2], db, db_off + ref.rounded(db, F32), "dbias")
+        again = aq.layer_norm_backward(dy, x, w, dsum=dsum, rms=rms, bias=True)
+        assert all(torch.equal(p, q) for p, q in zip(got, again))
+
+
 def test_norm_no_rows(aq):
     x = rand(1, 0, 100)
     w = rand(2, 100)
@@ -261,14 +278,48 @@ def test_distill(aq, dtype, teacher, rows, vocab, n, rest):
     ref.check(g, grad, grad_off + ref.rounded(grad.abs() + grad_off, dtype), "gradient")
 
 
+@pytest.mark.parametrize("dtype,teacher", [(F16, F32), (BF16, F16), (F32, F32)])
+@pytest.mark.parametrize("vocab,n", [(9, 3), (130, 130), (1000, 64), (4099, 20), (16001, 300), (32000, 64), (65531, 50)])
+def test_distill_many_rows(aq, dtype, teacher, vocab, n):
+    """Enough rows that none is cut."""
+    rows = 600
+    some = [0, 1, 2, 3, 300, 599]
+    z, t, ids, lse = distill_case(41, rows, vocab, n, dtype, teacher)
+    if n > 4:
+        ids[3, 4] = ids[3, 1]
+    w = 0.5 + uniform(42, rows)
+    w[1] = 0
+    for rest in (None, lse + 2.0):  # (with the mass of entries that are listed twice below 1)
+        at = None if rest is None else rest[some]
+        loss, loss_off, grad, grad_off = ref.distill(z[some], t[some], ids[some], at, w[some], 1.5)
+        got, g = aq.distill_loss(z, t, ids, teacher_lse=rest, weights=w, temperature=1.5)
+        ref.check(got[some], loss, loss_off, "loss")
+        ref.check(g[some], grad, grad_off + ref.rounded(grad.abs() + grad_off, dtype), "gradient")
+        zs = spaced(z)
+        got2, _ = aq.distill_loss(zs, t, ids, teacher_lse=rest, weights=w, temperature=1.5, out=zs)
+        assert torch.equal(got2, got) and torch.equal(zs, g) and torch.isnan(around(zs)).all()
+        # (a row's results do not depend on the others but by the order of its sums)
+        few, gf = aq.distill_loss(z[some], t[some], ids[some], teacher_lse=at, weights=w[some], temperature=1.5)
+        ref.check(few, loss, loss_off, "loss")
+        ref.check(gf, grad, grad_off + ref.rounded(grad.abs() + grad_off, dtype), "gradient")
+
+
+@pytest.mark.parametrize("rows", [3, 600])
 @pytest.mark.parametrize("rest", [False, True])
-def test_distill_same_id_several_times(aq, rest):
-    z, t, ids, lse = distill_case(35, 3, 4001, 40, F32, F32, short=False)
+def test_distill_same_id_several_times(aq, rest, rows):
+    z, t, ids, lse = (v[:3] for v in distill_case(35, 3, 4001, 40, F32, F32, short=False))
     ids[0, 7] = ids[0, 3]
     ids[0, 39] = ids[0, 3]
     ids[1, :] = 17
     t = t - 3  # (so that the sums of the masses stay below 1)
     lse = lse + 4 if rest else None
+    if rows > 3:  # (rows that are not cut)
+        full = [None if v is None else v.repeat(rows // 3, *[1] * (v.dim() - 1)) for v in (z, t, ids, lse)]
+        loss, loss_off, grad, grad_off = ref.distill(z, t, ids, lse, None, 1.5)
+        got, g = aq.distill_loss(full[0], full[1], full[2], teacher_lse=full[3], temperature=1.5)
+        ref.check(got[-3:], loss, loss_off, "loss")
+        ref.check(g[-3:], grad, grad_off + ref.rounded(grad.abs() + grad_off, F32), "gradient")
+        return
     loss, loss_off, grad, grad_off = ref.distill(z, t, ids, lse, None, 1.5)
     for _ in range(3):
         got, g = aq.distill_loss(z, t, ids, teacher_lse=lse, temperature=1.5)
@@ -397,6 +448,40 @@ def test_sample_ties_and_masks(aq, dtype):
         got = check_sample(aq, x, uniform(45, rows), **rules(46, rows, only))
         assert int(got[1]) == -1 and int(got[2]) == 4000 and int(got[3]) == -1 and int(got[5]) == 77
         assert int(got[6]) in (99, 1003)
+
+
+@pytest.mark.parametrize("vocab", [8000, 30000, 128256, 300007])
+def test_sample_flat_rows(aq, vocab):
+    """Thousands of tokens kept, the last one among thousands that are near it."""
+    x = rand(53, 8, vocab) * torch.tensor([0.01, 0.1, 0.5, 1.0, 1.5, 0.5, 0.5, 0.5], device=DEV)[:, None]
+    u, full = uniform(54, 8), lambda v, t=F32: torch.full((8,), v, dtype=t, device=DEV)  # noqa: E731
+    for r in (dict(top_p=full(0.9)), dict(top_p=full(0.3)), dict(min_p=full(0.05)), dict(top_k=full(700, torch.int32)),
+              dict(top_k=full(vocab // 2, torch.int32)), dict(top_p=full(0.999), min_p=full(0.01)),
+              dict(top_k=full(1500, torch.int32), top_p=full(0.8)), dict(top_k=full(vocab // 3, torch.int32), top_p=full(0.7)),
+              dict(top_p=full(0.9), temperature=full(0.4)), dict(top_k=full(256, torch.int32), top_p=full(0.9))):
+        check_sample(aq, x, u, **r)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [8000, 30000, 50001])
+def test_sample_gaps_and_long_ties(aq, dtype, vocab):
+    """Limits where no logit is, and among thousands of equal ones."""
+    x = torch.full((6, vocab), -5.0, device=DEV)
+    at = torch.randperm(vocab, device=DEV)
+    x[:, at[:3000]] = 5.0
+    x[1, at[3000:3003]] = 7.0
+    x[2, at[3000:6000]] = 4.0
+    x[3] = (rand(55, 1, vocab)[0] * 2).round()
+    x[4] = (rand(56, 1, vocab)[0] * 300).round() / 64
+    x[5, at[:2990]] = -math.inf
+    x = x.to(dtype)
+    u, full = uniform(57, 6), lambda v, t=F32: torch.full((6,), v, dtype=t, device=DEV)  # noqa: E731
+    for r in (dict(min_p=full(0.5)), dict(min_p=full(0.1)), dict(min_p=full(1e-6)), dict(top_p=full(0.5)),
+              dict(top_p=full(0.9999)), dict(top_k=full(100, torch.int32)), dict(top_k=full(2999, torch.int32)),
+              dict(top_k=full(3001, torch.int32)), dict(top_k=full(200, torch.int32), top_p=full(0.5)),
+              dict(top_k=full(2500, torch.int32), top_p=full(0.5)), dict(top_p=full(0.7), min_p=full(0.5)),
+              dict(top_k=full(0, torch.int32), min_p=full(0.5)), dict(temperature=full(0.05), top_p=full(0.5))):
+        check_sample(aq, x, u, **r)
 
 
 def test_sample_extreme_rules(aq):
