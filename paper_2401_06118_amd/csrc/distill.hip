@@ -68,15 +68,25 @@ __device__ __forceinline__ void add_piece(const V& v, int skip, float c, float& 
   for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((f[e] - m) * c);
 }
 
+// A thread's first entry, loaded before anything else is known of the row.
+struct Entry {
+  int id;
+  float t;
+};
+__device__ __forceinline__ Entry first_entry(const DistillArgs& a, int64_t row) {
+  const int k = min((int)threadIdx.x, a.listed - 1);
+  return {a.ids[row * a.ids_row + k], teacher_at(a, row, k)};
+}
+
 // The entries into LDS, the waves' maxima into parts.  logit(k, id): the student's; mark(id).
 template <int THREADS, typename L, typename M>
-__device__ __forceinline__ void read_list(const DistillArgs& a, int64_t row, const List& list,
+__device__ __forceinline__ void read_list(const DistillArgs& a, int64_t row, const Entry& own, const List& list,
                                           Parts<THREADS / kWave>& parts, L logit, M mark) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   float top = -INFINITY, zmax = -INFINITY;
   for (int k = tid; k < a.listed; k += THREADS) {
-    const int id = a.ids[row * a.ids_row + k];
-    const float t = teacher_at(a, row, k);
+    const int id = k == tid ? own.id : a.ids[row * a.ids_row + k];
+    const float t = k == tid ? own.t : teacher_at(a, row, k);
     const bool held = (uint32_t)id < (uint32_t)a.vocab;
     list.id[k] = held ? id : -1;
     if (!held) continue;
@@ -232,6 +242,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(DistillArgs a) {
   const T* const in = (const T*)a.logits + row * a.logits_row;
   T* const out = a.grad != nullptr ? (T*)a.grad + row * a.grad_row : nullptr;
   const int pieces = (a.vocab + N - 1) / N;
+  const Entry own = first_entry(a, row);
   const float weight = a.weights != nullptr ? a.weights[row] : 1.f;
   if (weight == 0.f) {  // its logits are not looked at
     if (tid == 0) a.loss[row] = 0.f;
@@ -245,7 +256,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(DistillArgs a) {
   for (int i = tid; i < words; i += THREADS) bits[i] = i == words - 1 && (a.vocab & 31) != 0 ? ~0u << (a.vocab & 31) : 0u;
   if (tid == 0) parts.twice = 0;
   lds_barrier();
-  read_list<THREADS>(a, row, list, parts, [&](int, int id) { return (float)in[id]; }, [&](int id) {
+  read_list<THREADS>(a, row, own, list, parts, [&](int, int id) { return (float)in[id]; }, [&](int id) {
     if (atomicOr(&bits[id / 32], 1u << (id % 32)) >> (id % 32) & 1) parts.twice = 1;
   });
   lds_barrier();
@@ -352,7 +363,7 @@ __device__ __forceinline__ void sum_row_list(const DistillArgs& a, int64_t row, 
       at = (at + 1) & (slots - 1);
     }
   };
-  read_list<THREADS>(a, row, list, parts, [&](int, int id) { return (float)in[id]; }, [&](int) {});
+  read_list<THREADS>(a, row, first_entry(a, row), list, parts, [&](int, int id) { return (float)in[id]; }, [&](int) {});
   lds_barrier();
   for (int k = tid; k < a.listed; k += THREADS)
     if (list.id[k] >= 0 && atomicMin(&first[slot_of(list.id[k])], k) != INT32_MAX) parts.twice = 1;

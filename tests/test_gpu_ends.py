@@ -327,8 +327,9 @@ def test_distill_same_id_several_times(aq, rest, rows):
         ref.check(g, grad, grad_off + ref.rounded(grad.abs() + grad_off, F32), "gradient")
 
 
+@pytest.mark.parametrize("copies", [1, 80])  # (rows that are cut, and not)
 @pytest.mark.parametrize("rest", [False, True])
-def test_distill_masked_and_special(aq, rest):
+def test_distill_masked_and_special(aq, rest, copies):
     z, t, ids, lse = distill_case(37, 8, 5000, 30, F32, F32, short=False)
     lse = lse if rest else None
     low = torch.finfo(F32).min
@@ -345,7 +346,9 @@ def test_distill_masked_and_special(aq, rest):
     z[6] *= 30  # a student that is sure
     ids[7] = -1
     z[7, 3] = 5.0
-    got, g = aq.distill_loss(z, t, ids, teacher_lse=lse, weights=w, temperature=1.5)
+    many = [None if v is None else v.repeat(copies, *[1] * (v.dim() - 1)) for v in (z, t, ids, lse, w)]
+    got, g = aq.distill_loss(*many[:3], teacher_lse=many[3], weights=many[4], temperature=1.5)
+    got, g = got[-8:], g[-8:]
     for i in (0, 2, 6, 7):
         loss, loss_off, grad, grad_off = ref.distill(z[i:i + 1], t[i:i + 1], ids[i:i + 1],
                                                      None if lse is None else lse[i:i + 1], None, 1.5)
