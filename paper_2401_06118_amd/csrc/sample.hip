@@ -258,11 +258,15 @@ __device__ __forceinline__ void append(int32_t& n, uint64_t* dest, int cap, H hi
   }
 }
 
-// The row's tokens with low <= l c < high appended.
+// The row's tokens with low <= l c < high appended, by all threads.  The numbers first, a lane's own of 32 at a time
+// (few hit: as many steps as the most of a lane), then their logits: 128 rows of 128256 with top-p NN
+// against a ballot an element.
 template <int TY, int THREADS>
 __device__ __forceinline__ void append_row(int32_t& n, uint64_t* dest, int cap, const void* row, int vocab, float c,
                                            float low, float high) {
   constexpr int N = kPiece<TY>, kBatch = 32 / N;
+  typedef typename Elem<TY>::T T;
+  const int lane = threadIdx.x % kWave;
   // (whole waves: lanes past the end have nothing)
   for (int i0 = 0; i0 < vocab; i0 += kBatch * THREADS * N) {
     typename Elem<TY>::V v[kBatch];
@@ -271,21 +275,39 @@ __device__ __forceinline__ void append_row(int32_t& n, uint64_t* dest, int cap, 
     for (int j = 0; j < kBatch; ++j) {
       const int i = i1 + j * THREADS * N;
       if (i + N <= vocab) {
-        v[j] = *(const typename Elem<TY>::V*)((const typename Elem<TY>::T*)row + i);
+        v[j] = *(const typename Elem<TY>::V*)((const T*)row + i);
       } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          v[j][e] = i + e < vocab ? ((const typename Elem<TY>::T*)row)[i + e] : (typename Elem<TY>::T)-INFINITY;
+        for (int e = 0; e < N; ++e) v[j][e] = i + e < vocab ? ((const T*)row)[i + e] : (T)-INFINITY;
       }
     }
+    uint32_t hits = 0;
 #pragma unroll
-    for (int j = 0; j < kBatch; j += 8 / N)  // (8 elements at a time: their masks are 16 scalar registers)
-      append<8>(n, dest, cap, [&](int k) {
-        const float f = (float)v[j + k / N][k % N] * c;
-        return f >= low && f < high;
-      }, [&](int k) {
-        return place_of((float)v[j + k / N][k % N], i1 + (j + k / N) * THREADS * N + k % N);
-      });
+    for (int k = 0; k < 32; ++k) {
+      const float f = (float)v[k / N][k % N] * c;
+      hits |= f >= low && f < high ? 1u << k : 0;
+    }
+    if (__ballot(hits != 0) == 0) continue;
+    const int own = __popc(hits);
+    int incl = own;
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+      const int o = __shfl_up(incl, s);
+      if (lane >= s) incl += o;
+    }
+    int at = 0;
+    if (lane == kWave - 1) at = atomicAdd(&n, incl);
+    at = __builtin_amdgcn_readlane(at, kWave - 1) + incl - own;
+    for (; hits != 0; hits &= hits - 1, ++at) {
+      const int k = __builtin_ctz(hits);
+      if (at < cap) dest[at] = (uint32_t)(i1 + k / N * (THREADS * N) + k % N);
+    }
+  }
+  lds_barrier();
+  const int held = min(n, cap);
+  for (int t = threadIdx.x; t < held; t += THREADS) {
+    const int i = (int)dest[t];
+    dest[t] = place_of((float)((const T*)row)[i], i);
   }
 }
 
