@@ -15,7 +15,8 @@
 // Counts and masses of the tokens by bins of T / 16 (512 of them: what is lower has no mass
 // left) show in which bin the last member lies.  The tokens down to it (or, if those are more
 // than a list holds, that bin's) are collected and sorted; the kept ones are the first of
-// them.  What the list does not hold either (thousands of equal logits) is found by
+// them.  (A top-p of the first k has two last members: the k-th for the mass, then the limit's.)  What the list does not
+// hold either (thousands of equal logits) is found by
 // eleven bits of logit and number at a time (draw_slowly).
 //
 // Rows of up to 32768 logits are a workgroup's each, which holds them in registers.  Longer
@@ -259,8 +260,8 @@ __device__ __forceinline__ void append(int32_t& n, uint64_t* dest, int cap, H hi
 }
 
 // The row's tokens with low <= l c < high appended, by all threads.  The numbers first, a lane's own of 32 at a time
-// (few hit: as many steps as the most of a lane), then their logits: 128 rows of 128256 with top-p NN
-// against a ballot an element.
+// (few hit: as many steps as the most of a lane), then their logits: 9 us instead of the 20
+// that a ballot an element takes for 128256 logits with thousands of hits.
 template <int TY, int THREADS>
 __device__ __forceinline__ void append_row(int32_t& n, uint64_t* dest, int cap, const void* row, int vocab, float c,
                                            float low, float high) {
@@ -506,10 +507,12 @@ struct Bins {
   __device__ int last() const { return fine ? kBins - 1 : kBins - 2; }
 };
 
+// k: the first k are kept, 0 for all; counted: sh.count is known.
 // The edge's bin by one wave, eight bins a lane, from sh.mass and sh.count, and what lies before them:
 // sh.found, that bin, sh.found_in, what it has, and the sums before it; sh.listing: the list's fill.
-__device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_count, bool whole, double most,
-                                          const Bins& bins, uint64_t mass_before, uint32_t count_before) {
+__device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, int k, bool by_count, bool counted, bool whole,
+                                          double most, const Bins& bins, uint64_t mass_before,
+                                          uint32_t count_before) {
   constexpr int kEach = kBins / kWave;
   const int lane = threadIdx.x;
   uint64_t mass[kEach], m = 0;
@@ -518,7 +521,7 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
   for (int j = 0; j < kEach; ++j) {
     const int bin = lane * kEach + j;
     mass[j] = by_count ? 0 : sh.mass[bin];
-    count[j] = by_count || r.k > 0 || bins.fine ? sh.count[bin] : most_of(r, mass[j], bins.lower(bin));
+    count[j] = by_count || counted ? sh.count[bin] : most_of(r, mass[j], bins.lower(bin));
     m += mass[j];
     c += count[j];
   }
@@ -543,7 +546,7 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
   uint32_t bc = count_before;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
-    bool limit = r.k > 0 && bc < (uint32_t)r.k && (uint32_t)r.k <= bc + count[j];
+    bool limit = k > 0 && bc < (uint32_t)k && (uint32_t)k <= bc + count[j];
     if (!by_count && !whole) limit |= r.top_p && mass[j] != 0 && (double)(bm + mass[j]) >= most;
     if (limit) mine = min(mine, lane * kEach + j);
     bm += mass[j];
@@ -569,19 +572,81 @@ __device__ __forceinline__ void find_edge(Shared& sh, const Rules& r, bool by_co
   }
 }
 
-// all: the row's mass.  collect(low, high, edge bin, dest, cap) appends the places of all tokens with
+// The first n of sh.list in order.
+template <int THREADS>
+__device__ __forceinline__ void sort(Shared& sh, int n) {
+  const int tid = threadIdx.x, wave = tid / kWave;
+  if (n <= kFew) {  // each to its rank
+    const uint64_t own = tid < n ? sh.list[tid] : 0;
+    int rank = 0;
+    if (wave * kWave < n) {
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) rank += sh.list[j] < own;
+    }
+    lds_barrier();
+    if (tid < n) sh.list[rank] = own;
+    lds_barrier();
+    return;
+  }
+  int size = 2;
+  while (size < n) size <<= 1;
+  for (int i = n + tid; i < size; i += THREADS) sh.list[i] = ~0ull;
+  lds_barrier();
+  for (int k = 2; k <= size; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      for (int i = tid; i < size / 2; i += THREADS) {
+        const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+        const uint64_t p = sh.list[lo], q = sh.list[hi];
+        if ((p > q) == ((lo & k) == 0)) {
+          sh.list[lo] = q;
+          sh.list[hi] = p;
+        }
+      }
+      lds_barrier();
+    }
+}
+
+// The mass of the first k, or kNone if more than the list holds are in the k-th's bin; collect as in choose.  (Sorting
+// those of one bin: sorting all k to find top-p's limit takes 12 us for 1000, twice.)
+constexpr uint64_t kNone = ~0ull;
+template <int THREADS, typename F>
+__device__ __forceinline__ uint64_t mass_of_first(Shared& sh, const Rules& r, int top_bin, F collect) {
+  constexpr int kEach = kList / THREADS;
+  const int tid = threadIdx.x;
+  const Bins bins{top_bin, false, 0.f};
+  if (tid / kWave == 0) find_edge(sh, r, r.k, false, true, true, 0.0, bins, 0, 0);
+  lds_barrier();
+  const int bin = sh.found;
+  const uint32_t rest = (uint32_t)r.k - min(sh.found_count, (uint32_t)r.k);
+  const uint64_t before = sh.found_mass;
+  if (sh.found_in > kList) return kNone;
+  collect(bins.lower(bin), bins.upper(bin), bin, sh.list, kList);
+  lds_barrier();
+  const int n = min(sh.listing, kList);
+  sort<THREADS>(sh, n);
+  uint64_t m = 0;
+#pragma unroll 1
+  for (int j = 0; j < kEach; ++j) {
+    const int i = j * THREADS + tid;
+    if (i < n && (uint32_t)i < rest) m += weight_of(r, logit_of((uint32_t)(sh.list[i] >> 32)));
+  }
+  return before + sum_all<THREADS>(sh, m);
+}
+
+// k: of the rules, or 0 if `all`, the mass that top-p is of, is that of the first k: as p <= 1 - 2^-24, its last member
+// is one of them.  (Else `all` is the row's.)  collect(low, high, edge bin, dest, cap) appends the places of all tokens with
 // low <= l c < high to dest, sh.listing of them.  kDrawn: the token is written; kKnown: the edge is, and sh.list begins
 // with the sh.found_in tokens beside it that are kept; kUnknown: draw_slowly.
 // by_count: sh.count need not count all, but show a bin down to which there are k.
 // pool [kPool]: place for tokens, or null; edge.pooled: how many of the edge's bin it has.
 template <int THREADS, typename F>
 __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const SampleArgs& a, int b, const Rules& r,
-                                          bool by_count, uint64_t all, int top_bin, Edge& edge, F collect) {
+                                          int k, bool by_count, uint64_t all, int top_bin, Edge& edge, F collect) {
   constexpr int kEach = kList / THREADS;
   const int tid = threadIdx.x, wave = tid / kWave;
-  const bool whole = r.k > 0 && r.top_p;  // (top-p's limit needs the first k's mass)
+  const bool whole = by_count && r.top_p;  // (top-p's limit needs the first k's mass: the list has them)
   Bins bins{top_bin, false, 0.f};
-  if (wave == 0) find_edge(sh, r, by_count, whole, r.p * (double)all, bins, 0, 0);
+  if (wave == 0) find_edge(sh, r, k, by_count, r.k > 0, whole, r.p * (double)all, bins, 0, 0);
   lds_barrier();
   edge.bin = sh.found;
   uint32_t before = sh.found_count;
@@ -589,9 +654,8 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   uint32_t in_edge = sh.found_in;
   // Whether all that can be kept is in the list.  (Sorting 2048 takes 12 us, twice; a part of a bin that
   // few share does not need it.)
-  const bool listed = by_count || before + in_edge <= (uint32_t)(whole || pool == nullptr ? kList : kFew);
+  const bool listed = by_count || before + in_edge <= (uint32_t)(pool == nullptr ? kList : kFew);
   float low = bins.lower(edge.bin), high = listed ? INFINITY : bins.upper(edge.bin);
-  if (whole && !listed) return kUnknown;
   if (listed || in_edge <= (uint32_t)(pool == nullptr ? kList : kFew)) {
     collect(low, high, edge.bin, sh.list, kList);
   } else {
@@ -614,7 +678,7 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
       atomicAdd((unsigned long long*)&sh.mass[bin], (unsigned long long)weight_of(r, l));
     }
     lds_barrier();
-    if (wave == 0) find_edge(sh, r, false, false, r.p * (double)all, bins, before_mass, before);
+    if (wave == 0) find_edge(sh, r, k, false, true, false, r.p * (double)all, bins, before_mass, before);
     lds_barrier();
     before = sh.found_count;
     before_mass = sh.found_mass;
@@ -635,7 +699,7 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   if (n > kList) return kUnknown;  // (where bins do not count all)
   edge.high = high;
   auto keeps = [&](uint32_t rank, uint64_t mass_before, float l, double most) {
-    return (r.k == 0 || rank < (uint32_t)r.k) && (!r.top_p || (double)mass_before < most) &&
+    return (k == 0 || rank < (uint32_t)k) && (!r.top_p || (double)mass_before < most) &&
            (l == r.max_f || (double)l - r.max >= r.lim);
   };
 
@@ -678,37 +742,7 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
     return kDrawn;
   }
 
-  auto sort = [&](int n) {
-    if (n <= kFew) {  // each to its rank
-      const uint64_t own = tid < n ? sh.list[tid] : 0;
-      int rank = 0;
-      if (wave * kWave < n) {
-#pragma unroll 8
-        for (int j = 0; j < n; ++j) rank += sh.list[j] < own;
-      }
-      lds_barrier();
-      if (tid < n) sh.list[rank] = own;
-      lds_barrier();
-      return;
-    }
-    int size = 2;
-    while (size < n) size <<= 1;
-    for (int i = n + tid; i < size; i += THREADS) sh.list[i] = ~0ull;
-    lds_barrier();
-    for (int k = 2; k <= size; k <<= 1)
-      for (int j = k >> 1; j > 0; j >>= 1) {
-        for (int i = tid; i < size / 2; i += THREADS) {
-          const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-          const uint64_t p = sh.list[lo], q = sh.list[hi];
-          if ((p > q) == ((lo & k) == 0)) {
-            sh.list[lo] = q;
-            sh.list[hi] = p;
-          }
-        }
-        lds_barrier();
-      }
-  };
-  sort(n);
+  sort<THREADS>(sh, n);
   // kEach tokens a thread, in order: the kept ones are the first of them
   uint64_t w[kEach], sum = 0;
 #pragma unroll
@@ -776,7 +810,7 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
   for (int j = 0; j < kEach; ++j)
     if (tid * kEach + j < kept) sh.list[tid * kEach + j] = mine[j] << 32 | mine[j] >> 32;
   lds_barrier();
-  sort(kept);
+  sort<THREADS>(sh, kept);
   const uint64_t target = target_of(a.uniform[b], total);
   uint64_t from = 0;
 #pragma unroll
@@ -1030,8 +1064,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
       } else {
         all = sum_all<THREADS>(sh, count_bins<TY, ROUNDS>(sh, r, v, true, [](int bin) { return bin; }));
       }
-      o = choose<THREADS>(sh, nullptr, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int, uint64_t* dest,
-                                                                                         int cap) {
+      auto collect = [&](float low, float high, int, uint64_t* dest, int cap) {
         if (ROUNDS > 1 && by_count) {
           // few threads hold any: theirs are dealt to all
           const bool hit = mine * r.c >= low;
@@ -1061,7 +1094,11 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(SampleArgs a) {
             return f >= low && f < high;
           }, [&](int e) { return place_of((float)v[j][e], (j * THREADS + tid) * N + e); });
         }
-      });
+      };
+      const bool first = r.k > 0 && r.top_p && !by_count;
+      if (first) all = mass_of_first<THREADS>(sh, r, top_bin, collect);
+      if (all != kNone)
+        o = choose<THREADS>(sh, nullptr, a, b, r, first ? 0 : r.k, by_count, all, top_bin, edge, collect);
     }
     if (o == kDrawn) return;
     if (o == kUnknown) return draw_slowly<TY, THREADS>(sh, a, b, r);
@@ -1180,7 +1217,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
     Outcome o = kUnknown;
     const int top_bin = bin_of(r.max_f, r.c), lower = some ? top_bin - bin_of(rec.top, r.c) : 2 * kBins;
     if (has_bins(r)) {
-      const uint64_t all = wave_sum64(mass);
+      uint64_t all = wave_sum64(mass);
       // Calls f(held, place) for all that the slices' lists hold, by whole waves.
       auto lists = [&](auto f) {
         for (int s = wave; s < slices; s += THREADS / kWave) {
@@ -1232,9 +1269,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
       }
       lds_barrier();
       // (of counted rows every slice lists the first k, or it does not count here)
-      if (!by_count || __ballot(some && rec.cut < 0) == 0)
-        o = choose<THREADS>(sh, pool, a, b, r, by_count, all, top_bin, edge, [&](float low, float high, int edge_bin,
-                                                                                uint64_t* dest, int cap) {
+      if (!by_count || __ballot(some && rec.cut < 0) == 0) {
+        auto collect = [&](float low, float high, int edge_bin, uint64_t* dest, int cap) {
           if (by_count || __ballot(some && edge_bin - lower > rec.cut) == 0)
             lists([&](bool held, uint64_t place) {
               const float f = logit_of((uint32_t)(place >> 32)) * r.c;
@@ -1242,7 +1278,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_sample_join(SampleArgs a, int 
             });
           else
             append_row<TY, THREADS>(sh.listing, dest, cap, row, a.vocab, r.c, low, high);
-        });
+        };
+        const bool first = r.k > 0 && r.top_p && !by_count;
+        if (first) all = mass_of_first<THREADS>(sh, r, top_bin, collect);
+        if (all != kNone) o = choose<THREADS>(sh, pool, a, b, r, first ? 0 : r.k, by_count, all, top_bin, edge, collect);
+      }
     }
     if (o == kDrawn) return;
     if (o == kUnknown) return draw_slowly<TY, THREADS>(sh, a, b, r);

@@ -487,6 +487,20 @@ def test_sample_gaps_and_long_ties(aq, dtype, vocab):
         check_sample(aq, x, u, **r)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [600, 8192, 32001, 128256])
+def test_sample_mass_of_many(aq, dtype, vocab):
+    """top-p of the mass of more tokens than a list holds, or than have any mass."""
+    x = rand(58, 6, vocab) * torch.tensor([0.1, 0.7, 1.5, 3.0, 30.0, 2.0], device=DEV)[:, None]
+    x[5, torch.arange(vocab, device=DEV) % 64 != 5] = -math.inf
+    x[0, :vocab // 3] = 0.25
+    x = x.to(dtype)
+    u, full = uniform(59, 6), lambda v, t=F32: torch.full((6,), v, dtype=t, device=DEV)  # noqa: E731
+    for k in (257, 599, vocab // 2, vocab - 1):
+        for p, least in ((0.02, 0.0), (0.5, 0.3), (0.9, 0.0), (0.9999, 0.001), (1.0 - 2.0 ** -24, 0.0)):
+            check_sample(aq, x, u, top_k=full(k, torch.int32), top_p=full(p), min_p=full(least))
+
+
 def test_sample_extreme_rules(aq):
     x = rand(47, 12, 3000) * 3
     u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 2.0, -1.0, math.nan] * 2, device=DEV)
