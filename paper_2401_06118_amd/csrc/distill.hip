@@ -12,7 +12,7 @@
 // is no difference; the list's terms are computed in 64 bits, as the loss is a
 // difference of larger ones.  Bound: memory; logits are read once and the gradient is
 // written once (2048 x 32000 fp16 54.5 us, 4.8 TB/s of both), by rows that are cut logits twice
-// (333 x 128256 bf16 with 200 listed 19 us and 25).
+// (333 x 128256 bf16 with 200 listed 44 us).
 #include "ends.h"
 
 #include "common.h"
@@ -443,7 +443,10 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_slices(DistillArgs a)
   a.slices[row * slices + slice] = DistillSlice{m, s};
 }
 
-template <int TY, int NV>
+// NT: the gradient goes past the L2s.  Where it is more than they hold, that leaves the logits in the caches between
+// the launches (400 x 128256 fp32 125 -> 105 us, 333 x 128256 bf16 50 -> 44; whole rows, read once: 54.5 -> 56.5).
+constexpr int64_t kStreamBytes = 32 << 20;
+template <int TY, int NV, bool NT>
 __global__ void __launch_bounds__(kSliceThreads) k_distill_grad(DistillArgs a) {
   typedef typename Elem<TY>::T T;
   typedef typename Elem<TY>::V V;
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(kSliceThreads) k_distill_grad(DistillArgs a) {
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int at = from + (tid + j * THREADS) * N;
-    if (at < a.vocab) store_piece<TY>(out, at, a.vocab, gradient<TY>(x[j], m, c, by));
+    if (at < a.vocab) store_piece<TY, NT>(out, at, a.vocab, gradient<TY>(x[j], m, c, by));
   }
   __syncthreads();  // the listed ids' gradients go over what was written there
   const int32_t* const ids = a.ids + row * a.ids_row;
@@ -512,7 +515,10 @@ hipError_t launch_slices(DistillArgs a, int slices, hipStream_t s) {
   for (a.row0 = 0; a.row0 < a.rows && e == hipSuccess; a.row0 += 65535) {
     const unsigned n = (unsigned)(a.rows - a.row0 < 65535 ? a.rows - a.row0 : 65535);
     k_distill_slices<TY, NV><<<dim3((unsigned)slices + 1, n), kSliceThreads, lds, s>>>(a);
-    k_distill_grad<TY, NV><<<dim3((unsigned)slices, n), kSliceThreads, 0, s>>>(a);
+    if (a.rows * a.vocab * dtype_bytes(TY) > kStreamBytes)
+      k_distill_grad<TY, NV, true><<<dim3((unsigned)slices, n), kSliceThreads, 0, s>>>(a);
+    else
+      k_distill_grad<TY, NV, false><<<dim3((unsigned)slices, n), kSliceThreads, 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;
@@ -533,7 +539,7 @@ hipError_t launch_typed(const DistillArgs& a, hipStream_t s) {
 }  // namespace
 
 // Rows stay whole where the registers of 512 threads hold one and there are two a CU: fewer leave CUs without work
-// (333 x 128256 bf16 whole 74 us, cut 45; one row 28 and 12).  Slices are narrow where wide ones are fewer than four a
+// (333 x 128256 bf16 whole 74 us, cut 44; one row 28 and 12).  Slices are narrow where wide ones are fewer than four a
 // CU.
 DistillCut distill_cut(int64_t rows, int64_t vocab, int dtype) {
   const int n = dtype == kF32 ? 4 : 8;

@@ -304,6 +304,27 @@ def test_distill_many_rows(aq, dtype, teacher, vocab, n):
         ref.check(gf, grad, grad_off + ref.rounded(grad.abs() + grad_off, dtype), "gradient")
 
 
+@pytest.mark.parametrize("dtype,teacher", [(F16, F32), (BF16, F16), (F32, F32)])
+@pytest.mark.parametrize("vocab", [128256, 128255])
+def test_distill_many_cut_rows(aq, dtype, teacher, vocab):
+    """A gradient of more than the caches next to the processors hold, by slices."""
+    rows, n = 140, 200
+    some = [0, 1, 2, 3, 77, 139]
+    z, t, ids, lse = distill_case(43, rows, vocab, n, dtype, teacher)
+    ids[3, 4] = ids[3, 1]
+    w = 0.5 + uniform(44, rows)
+    w[1] = 0
+    for rest in (None, lse + 2.0):
+        at = None if rest is None else rest[some]
+        loss, loss_off, grad, grad_off = ref.distill(z[some], t[some], ids[some], at, w[some], 1.5)
+        got, g = aq.distill_loss(z, t, ids, teacher_lse=rest, weights=w, temperature=1.5)
+        ref.check(got[some], loss, loss_off, "loss")
+        ref.check(g[some], grad, grad_off + ref.rounded(grad.abs() + grad_off, dtype), "gradient")
+        zs = spaced(z)
+        got2, _ = aq.distill_loss(zs, t, ids, teacher_lse=rest, weights=w, temperature=1.5, out=zs)
+        assert torch.equal(got2, got) and torch.equal(zs, g) and torch.isnan(around(zs)).all()
+
+
 @pytest.mark.parametrize("rows", [3, 600])
 @pytest.mark.parametrize("rest", [False, True])
 def test_distill_same_id_several_times(aq, rest, rows):
