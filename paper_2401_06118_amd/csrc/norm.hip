@@ -156,7 +156,8 @@ __global__ void __launch_bounds__((WAVES * kGradRows<WAVES> * kWave)) k_norm_gra
   constexpr int N = kPiece<TY>, kRows = kGradRows<WAVES>, kThreads = WAVES * kRows * kWave;
   constexpr int kRing = PER * N <= 16 ? 2 : 1;  // sets that are loaded or worked on at a time
   __shared__ float red[2][16][2];
-  const int t = threadIdx.x % (WAVES * kWave), own = threadIdx.x / (WAVES * kWave);
+  const int t = threadIdx.x % (WAVES * kWave), own = kRows > 1 ? threadIdx.x / kWave : 0;
+  static_assert(WAVES == 1 || kRows == 1, "waves of several rows and of a row each");
   const int64_t step = (int64_t)gridDim.x * kRows, slot = (int64_t)blockIdx.x * kRows;
   int turn = 0;
   float dw[PER][N], db[PER][N];
@@ -180,28 +181,19 @@ __global__ void __launch_bounds__((WAVES * kGradRows<WAVES> * kWave)) k_norm_gra
 #pragma unroll
   for (int j = 0; j < PER; ++j)
     if (a.weight != nullptr) w[j] = load_piece<TY, WHOLE>(a.weight, (t + j * WAVES * kWave) * N, a.dim);
-  // (a row past the last one is zeros, which add nothing)
-  auto load_own = [&](Row& r, int64_t set) {
-    if (set + own < a.rows) {
-      load(r, set + own);
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-#pragma unroll
-      for (int e = 0; e < N; ++e) r.h[j][e] = r.dy[j][e] = (T)0.f;
-  };
+  // (A wave without a row is done: its row's sums need no other wave.  Zeros in the place of a row would add
+  // NaN to dw where eps is 0.)
   Row ring[kRing];
 #pragma unroll
   for (int d = 0; d < kRing; ++d)
-    if (kRing > 1 && slot + d * step < a.rows) load_own(ring[d], slot + d * step);
-  for (int64_t first = slot; first < a.rows; first += kRing * step) {
+    if (kRing > 1 && slot + own + d * step < a.rows) load(ring[d], slot + own + d * step);
+  for (int64_t first = slot + own; first < a.rows; first += kRing * step) {
 #pragma unroll
     for (int d = 0; d < kRing; ++d) {
-      const int64_t set = first + d * step, row = set + own;
-      if (set >= a.rows) break;
+      const int64_t row = first + d * step;
+      if (row >= a.rows) break;
       Row& r = ring[d];
-      if (kRing == 1) load_own(r, set);
+      if (kRing == 1) load(r, row);
       float mu, rs;
       row_stats<TY, WAVES, PER, WHOLE>(r.h, t, a.dim, a.rms, a.eps, red, turn, mu, rs);
       float s[2] = {0.f, 0.f};
@@ -228,9 +220,9 @@ __global__ void __launch_bounds__((WAVES * kGradRows<WAVES> * kWave)) k_norm_gra
           if (a.dsum != nullptr) y += (float)r.ds[j][e];
           o[e] = (T)y;
         }
-        if (row < a.rows) store_piece<TY, false, WHOLE>((T*)a.out + row * a.out_row, (t + j * WAVES * kWave) * N, a.dim, o);
+        store_piece<TY, false, WHOLE>((T*)a.out + row * a.out_row, (t + j * WAVES * kWave) * N, a.dim, o);
       }
-      if (kRing > 1 && set + kRing * step < a.rows) load_own(r, set + kRing * step);
+      if (kRing > 1 && row + kRing * step < a.rows) load(r, row + kRing * step);
     }
   }
   if (a.dweight == nullptr && a.dbias == nullptr) return;
