@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "sample_bins.h"
+
 namespace aqlm {
 
 // Row strides in elements.
@@ -130,7 +132,7 @@ constexpr int kSampleSlice = 8192;   // logits of a slice
 // need every token's exponential; by slices 29.)
 inline bool sample_cut(int64_t vocab, bool top_k) { return vocab > (top_k ? kSampleRow : kSampleSlice); }
 constexpr int kSampleSlices = 4096;  // slices of a launch
-constexpr int kSampleBins = 512, kSampleListed = 512;
+constexpr int kSampleListed = 512;
 constexpr size_t kSampleSliceBytes = sizeof(SampleRecord) + kSampleBins * 12 + kSampleListed * 8;
 constexpr int kSampleMaxVocab = 1 << 19;
 constexpr int64_t kSampleMaxRows = 1 << 20;

@@ -30,6 +30,7 @@
 #include "elements.h"
 #include "launch.h"
 #include "lds_sync.h"
+#include "sample_bins.h"
 
 namespace aqlm {
 
@@ -497,17 +498,6 @@ struct Edge {
   int pooled;
 };
 enum Outcome { kDrawn, kKnown, kUnknown };
-
-// The bins: in whole numbers of l c below the largest's, or (fine) the 512 parts of one of them.
-struct Bins {
-  int top;  // of the largest
-  bool fine;
-  float low;  // fine: the lower end
-  __device__ int at(float f) const { return fine ? kBins - 1 - (int)((f - low) * kBins) : top - (int)floorf(f); }
-  __device__ float lower(int bin) const { return fine ? low + (float)(kBins - 1 - bin) / kBins : (float)(top - bin); }
-  __device__ float upper(int bin) const { return lower(bin) + (fine ? 1.f / kBins : 1.f); }
-  __device__ int last() const { return fine ? kBins - 1 : kBins - 2; }
-};
 
 // k: the first k are kept, 0 for all; counted: sh.count is known.
 // The edge's bin by one wave, eight bins a lane, from sh.mass and sh.count, and what lies before them:
@@ -1013,7 +1003,7 @@ __device__ __forceinline__ uint64_t count_bins(Shared& sh, const Rules& r, typen
 
 __device__ __forceinline__ bool by_counts(const Rules& r) { return r.k > 0 && r.k <= kMostK; }
 __device__ __forceinline__ bool is_filtered(const Rules& r) { return r.k > 0 || r.top_p || r.min_p; }
-// Bins are exact whole numbers of 32 bits only for logits that are not huge next to T.
+// Bins are whole numbers of 32 bits only for logits that are not huge next to T.
 __device__ __forceinline__ bool has_bins(const Rules& r) { return fabsf(r.max_f * r.c) < 0x1p29f; }
 
 // A row that a workgroup holds, ROUNDS pieces a thread.
@@ -1165,7 +1155,7 @@ __global__ void __launch_bounds__(kSliceThreads) k_sample_slices(SampleArgs a) {
         if (!by_count && tid < kBins - 1 && c + own <= kSampleListed) atomicMax(&sh.found, tid + 1);
         lds_barrier();
         rec.cut = sh.found - 1;
-        const float low = (float)(upper - rec.cut);
+        const float low = least_not_below(upper - rec.cut);
 #pragma unroll
         for (int j = 0; j < ROUNDS; j += 8 / N)
           append<8>(sh.listing, a.lists + at * kSampleListed, kSampleListed,

@@ -1,10 +1,12 @@
 """The operators of ``ends.py`` where a quantity of theirs reaches a limit."""
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
 
 import ends_reference as ref  # noqa: E402
-from test_gpu_ends import F32, TYPES, aq, rand, uniform  # noqa: E402,F401
+from test_gpu_ends import DEV, F32, TYPES, aq, check_sample, rand, uniform  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +28,28 @@ def test_norm_without_epsilon(aq, dtype, dim, rms):
         ref.check(got[0], dx, dx_off + ref.rounded(dx.abs() + dx_off, dtype), f"dx, {rows} rows")
         ref.check(got[1], dw, dw_off + ref.rounded(dw, F32), f"dweight, {rows} rows")
         ref.check(got[2], db, db_off + ref.rounded(db, F32), f"dbias, {rows} rows")
+
+
+# --------------------------------------------------------------------------- sampling
+
+@pytest.mark.parametrize("vocab", [8000, 30000, 128256])
+@pytest.mark.parametrize("many", [200, 2000])
+@pytest.mark.parametrize("level,temperature", [(100.0, 1e-5), (-100.0, 1e-5), (100.0, 4e-5), (3.0, 1e-6), (1000.0, 1e-4)])
+def test_sample_clusters_at_a_low_temperature(aq, vocab, many, level, temperature):
+    """Hundreds of equal logits at each of neighbouring 32-bit numbers, many units of the temperature's
+    size away from 0: tokens by sixteenths of the temperature are no longer told apart in 32 bits."""
+    rows = 4
+    step = float(torch.finfo(F32).eps) * 2.0 ** math.floor(math.log2(abs(level)))
+    at = torch.stack([torch.randperm(vocab, generator=torch.Generator(device=DEV).manual_seed(i), device=DEV)
+                      for i in range(rows)])
+    x = torch.full((rows, vocab), level - 1.0, device=DEV)
+    for j in range(min(8, vocab // many - 1)):
+        x.scatter_(1, at[:, j * many:(j + 1) * many], level - j * step)
+    assert (x.unique().numel()) == min(8, vocab // many - 1) + 1
+    x[3] = torch.where(x[3] == level, -math.inf, x[3])
+    u, full = uniform(6, rows), lambda v, t=F32: torch.full((rows,), v, dtype=t, device=DEV)  # noqa: E731
+    for r in (dict(), dict(top_p=full(0.3)), dict(top_p=full(0.9)), dict(top_p=full(0.999)), dict(min_p=full(0.3)),
+              dict(min_p=full(0.001)), dict(top_k=full(150, torch.int32)), dict(top_k=full(300, torch.int32)),
+              dict(top_k=full(300, torch.int32), top_p=full(0.9)), dict(top_k=full(2500, torch.int32)),
+              dict(top_k=full(2500, torch.int32), top_p=full(0.9), min_p=full(0.2))):
+        check_sample(aq, x, u, temperature=full(temperature), **r)
