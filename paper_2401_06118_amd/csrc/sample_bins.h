@@ -24,13 +24,14 @@ AQLM_BINS_FN float least_not_below(int n) {
 }
 
 // The bins: in whole numbers of f = l c below the largest's, |f| up to 2^29, or (fine) the 512 parts of one of them.  A
-// bin has the f with lower <= f < upper.
+// bin has the f with lower <= f < upper.  (Fine: |low| below 2^14, so that 512 low is a whole number of 32 bits, and
+// 512 f is exact where f - low is not: just below 0 that is 1.)
 struct Bins {
   int top;  // of the largest
   bool fine;
   float low;  // fine: the lower end
   AQLM_BINS_FN int at(float f) const {
-    return fine ? kSampleBins - 1 - (int)((f - low) * kSampleBins) : top - (int)floorf(f);
+    return fine ? kSampleBins - 1 - ((int)floorf(f * kSampleBins) - (int)(low * kSampleBins)) : top - (int)floorf(f);
   }
   AQLM_BINS_FN float lower(int bin) const {
     return fine ? low + (float)(kSampleBins - 1 - bin) / kSampleBins : least_not_below(top - bin);

@@ -27,6 +27,15 @@ static void whole(float f, int depth) {
   CHECK(b.lower(at_bin) <= f && f < b.upper(at_bin));
 }
 
+static void part(float low, float f) {
+  if (!(low <= f && f < low + 1.f)) return;
+  const Bins b{0, true, low};
+  at_f = f;
+  at_bin = b.at(f);
+  CHECK(at_bin >= 0 && at_bin < 512);
+  CHECK(b.lower(at_bin) <= f && f < b.upper(at_bin));
+}
+
 int main() {
   std::mt19937 gen(5);
   std::uniform_real_distribution<float> unit(0.f, 1.f);
@@ -48,6 +57,18 @@ int main() {
         CHECK((double)std::nextafter(b.lower(at_bin), -INFINITY) < b.top - at_bin);
       }
     }
+  for (int e = 0; e < 14; ++e)
+    for (int sign = -1; sign <= 1; sign += 2) {
+      const float low = (float)(e == 0 ? (sign < 0 ? -1 : 0) : sign * ((1 << e) - (int)(gen() % 2)));
+      for (int round = 0; round < 100000; ++round) {
+        float f = low + unit(gen);
+        if (round % 2) f = low + (float)(gen() % 513) / 512.f;
+        part(low, f);
+        part(low, std::nextafter(f, -INFINITY));
+        part(low, std::nextafter(f, INFINITY));
+      }
+    }
+  for (float f : {-1e-9f, -1e-30f, -1e-45f, -2e-8f, -6e-8f, -1.f / 512, -1.f / 512 - 1e-9f, -0.25f - 1e-8f}) part(-1.f, f);
   std::printf("sample bins ok\n");
   return 0;
 }

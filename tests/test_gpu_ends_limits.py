@@ -53,3 +53,24 @@ def test_sample_clusters_at_a_low_temperature(aq, vocab, many, level, temperatur
               dict(top_k=full(300, torch.int32), top_p=full(0.9)), dict(top_k=full(2500, torch.int32)),
               dict(top_k=full(2500, torch.int32), top_p=full(0.9), min_p=full(0.2))):
         check_sample(aq, x, u, temperature=full(temperature), **r)
+
+
+@pytest.mark.parametrize("level", [0.0, -1.0 / 512, 3.0, -250.0])
+def test_sample_parts_of_a_bin(aq, level):
+    """A bin of thousands of tokens that is divided into 512 parts, many of the tokens just below a part's end; also
+    where that is 0, and 32 bits are finer than next to the bin's other end."""
+    vocab, t = 40000, 16.0  # (bins of one unit)
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    at = torch.randperm(vocab, generator=gen, device=DEV)
+    below = torch.tensor([-1e-9 * 2.0 ** j for j in range(8)], device=DEV)
+    x = torch.full((vocab,), -math.inf, device=DEV)
+    x[at[:100]] = level + 0.5
+    x[at[100:1700]] = torch.minimum(level + below.repeat(200), torch.tensor(level, device=DEV).nextafter(torch.tensor(-math.inf, device=DEV)))
+    x[at[1700:3300]] = level - 0.25 + below.repeat(200)
+    x[at[3300:5000]] = level - 0.9 + 0.8 * torch.rand(1700, generator=gen, device=DEV)
+    rows = 16
+    u, full = uniform(9, rows), lambda v, t=F32: torch.full((rows,), v, dtype=t, device=DEV)  # noqa: E731
+    for r in (dict(top_p=full(0.1)), dict(top_p=full(0.2)), dict(top_p=full(0.335)), dict(top_p=full(0.5)),
+              dict(top_p=full(0.9)), dict(top_k=full(1000, torch.int32)), dict(top_k=full(1701, torch.int32)),
+              dict(top_k=full(4000, torch.int32), top_p=full(0.5)), dict(min_p=full(0.955)), dict(min_p=full(0.96))):
+        check_sample(aq, x.expand(rows, vocab), u, temperature=full(t), **r)
