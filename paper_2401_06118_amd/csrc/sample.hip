@@ -115,8 +115,8 @@ __device__ __forceinline__ uint64_t weight_of(const Rules& r, float l) {
 // 2^y for y <= 0.
 __device__ __forceinline__ double factor(double y) { return y > -1000.0 ? exp2(y) : 0.0; }
 
-// At least as many tokens as have this mass in a bin whose lower end is `lower`: each has the
-// weight there or more.
+// About as many tokens as can have this mass in a bin whose lower end is `lower`, or more: each has the
+// weight there or more (but for its rounding, where that is a few units: whoever lists them counts again).
 __device__ __forceinline__ uint32_t most_of(const Rules& r, uint64_t mass, float lower) {
   const float each = (r.max_f * r.c - lower) * (1.44269504f / 16.f) - 44.f;  // -log2 of the least weight
   return mass == 0 ? 0 : (uint32_t)fminf((float)mass * __builtin_amdgcn_exp2f(each) * 1.01f, 1e9f) + 1;
@@ -660,9 +660,11 @@ __device__ __forceinline__ Outcome choose(Shared& sh, uint64_t* pool, const Samp
       sh.count[i] = 0;
     }
     lds_barrier();
+    // (most_of shows too few where weights are a few units of 2^-44, rounded down)
+    if (sh.listing > kPool) return kUnknown;
     bins.fine = true;
     bins.low = low;
-    edge.pooled = min(sh.listing, kPool);
+    edge.pooled = sh.listing;
     for (int i = tid; i < edge.pooled; i += THREADS) {
       const float l = logit_of((uint32_t)(pool[i] >> 32));
       const int bin = bins.at(l * r.c);
@@ -1165,7 +1167,7 @@ __global__ void __launch_bounds__(kSliceThreads) k_sample_slices(SampleArgs a) {
                     });
         lds_barrier();
         rec.listed = sh.listing;
-        if (rec.listed > kSampleListed) {  // (by_count only)
+        if (rec.listed > kSampleListed) {  // (more than the counts show)
           rec.cut = -1;
           rec.listed = 0;
         }

@@ -74,3 +74,29 @@ def test_sample_parts_of_a_bin(aq, level):
               dict(top_p=full(0.9)), dict(top_k=full(1000, torch.int32)), dict(top_k=full(1701, torch.int32)),
               dict(top_k=full(4000, torch.int32), top_p=full(0.5)), dict(min_p=full(0.955)), dict(min_p=full(0.96))):
         check_sample(aq, x.expand(rows, vocab), u, temperature=full(t), **r)
+
+
+def test_sample_bin_of_more_tokens_than_its_place_holds(aq):
+    """A bin of 9400 tokens of which the slices' masses show fewer: each weighs 1.4 units of 2^-44 of
+    the largest, which the slice with the largest logit counts as 1."""
+    vocab, tail_last, tail_first = 32768, 7600, 1800
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    x = torch.full((vocab,), -math.inf, device=DEV)
+    last = 24576 + torch.randperm(8191, generator=gen, device=DEV)[:tail_last]
+    first = torch.randperm(24576, generator=gen, device=DEV)[:tail_first]
+    tail = torch.cat([first, last])
+    # l in (-30.1875, -30.125): exp(l) 2^44 lies between 1.36 and 1.45
+    x[tail] = -30.1874 + 0.0623 * torch.rand(len(tail), generator=gen, device=DEV)
+    x[vocab - 1] = 0.0
+    least = torch.tensor(math.exp(-30.15), dtype=F32, device=DEV)
+    kept = tail[x[tail].double() >= math.log(float(least))].sort().values
+    assert 3600 < len(kept) < 3900
+    w = torch.exp(x[kept].double()) * 2.0 ** 44
+    assert 1.3 < float(w.min()) and float(w.max()) < 1.5  # (so each is one unit)
+    j = torch.tensor([0, 1, 500, 700, 1000, 1100, 2000, 3000, 3500, len(kept) - 1], device=DEV)
+    # the number of unit j, half a unit on: total is 2^44 (1 + 2^-31)
+    u = ((j.double() + 0.5) * 2.0 ** -44).float()
+    rows = x.expand(len(j), vocab)
+    full = least.expand(len(j)).contiguous()
+    for _ in range(3):
+        assert torch.equal(aq.sample(rows, u, min_p=full), kept[j].int())
