@@ -174,10 +174,10 @@ __device__ __forceinline__ Sums join(const DistillArgs& a, const double (&sum)[4
   r.mass = sum[0];
   if (a.teacher_lse != nullptr) {
     const double p_rest = sum[3] == (double)a.vocab ? 0.0 : sum[0] == sum[0] ? fmax(1.0 - sum[0], 0.0) : sum[0];
-    const double q_rest = rest / r.s_all;
+    const double q_rest = rest / r.s_all;  // (0 where it is below all numbers; not so its logarithm in the loss)
     r.mass = sum[0] + p_rest;
     r.loss = sum[0] != 0.0 ? sum[1] + sum[0] * log_all : 0.0;
-    if (p_rest != 0.0) r.loss += p_rest * log(p_rest / q_rest);
+    if (p_rest != 0.0) r.loss += p_rest * (log(p_rest * r.s_all / s) - ((double)m - r.m_all) * inv);
     r.c_rest = q_rest * r.mass - p_rest;
   } else if (sum[0] != 0.0) {
     r.p_scale = 1.0 / sum[0];

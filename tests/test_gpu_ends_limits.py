@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import ends_reference as ref  # noqa: E402
-from test_gpu_ends import DEV, F32, TYPES, aq, check_sample, rand, uniform  # noqa: E402,F401
+from test_gpu_ends import DEV, F32, TYPES, aq, check_sample, distill_case, rand, uniform  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,38 @@ def test_sample_bin_of_more_tokens_than_its_place_holds(aq):
     full = least.expand(len(j)).contiguous()
     for _ in range(3):
         assert torch.equal(aq.sample(rows, u, min_p=full), kept[j].int())
+
+
+# --------------------------------------------------------------------------- distillation
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("copies", [1, 300])  # (rows that are cut, and not)
+@pytest.mark.parametrize("vocab", [40, 5000])
+def test_distill_rest_far_below_the_list(aq, dtype, copies, vocab):
+    """What is not listed masked with finite numbers, so low that its mass is no number of 64 bits: the
+    loss is that mass's logarithm all the same."""
+    n, tau = 30, 1.5
+    lows = [-1e4, float(torch.finfo(dtype).min), -2000.0, -1100.0]
+    z, t, ids, lse = distill_case(37, len(lows), vocab, n, dtype, F32, short=False)
+    at = ids.long()
+    listed = torch.zeros_like(z, dtype=torch.bool).scatter_(1, at, True)
+    z = torch.where(listed, z, torch.tensor(lows, dtype=dtype, device=DEV)[:, None])
+    lse = lse + 0.1
+    many = [v.repeat(copies, *[1] * (v.dim() - 1)) for v in (z, t, ids, lse)]
+    loss, g = (v[-len(lows):] for v in aq.distill_loss(*many[:3], teacher_lse=many[3], temperature=tau))
+    p = (t.double() / tau - lse.double()[:, None]).exp()
+    rest = 1 - p.sum(1)
+    assert (rest > 0.05).all()
+    zl = z.double().gather(1, at) / tau
+    log_all = torch.logsumexp(zl, 1)  # (the rest adds nothing to it)
+    low = z[~listed].double().view(len(lows), -1)[:, 0] / tau
+    log_rest = low + math.log(vocab - n) - log_all
+    want = (p * (p.log() - zl + log_all[:, None])).sum(1) + rest * (rest.log() - log_rest)
+    # the rest's sum in 32 bits: 128 additions of a thread, 17 waves' parts; then one rounding
+    ref.check(loss, want, want.abs() * 2 * ref.E32 + (128 + 17 + 8) * ref.E32)
+    assert torch.isfinite(g).all()
+    grad = torch.where(listed, 0.0, (-rest / (vocab - n))[:, None])
+    grad.scatter_(1, at, (zl - log_all[:, None]).exp() - p)
+    size = torch.where(listed, 0.0, (rest / (vocab - n))[:, None]).scatter_(1, at, (zl - log_all[:, None]).exp() + p)
+    bound = size / tau * (128 + 17 + 8) * ref.E32
+    ref.check(g, grad / tau, bound + ref.rounded(grad.abs() / tau + bound, dtype))
