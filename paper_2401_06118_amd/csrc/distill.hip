@@ -187,7 +187,8 @@ __device__ __forceinline__ Sums join(const DistillArgs& a, const double (&sum)[4
   } else {  // nothing is listed
     r.loss = r.c_rest = 0.0;
   }
-  r.c_rest = s != 0.0 ? r.c_rest / s : 0.0;
+  // (nothing outside the list: 0; a row without a softmax, all of it masked: NaN)
+  r.c_rest = s != 0.0 || r.c_rest != r.c_rest ? r.c_rest / s : 0.0;
   return r;
 }
 

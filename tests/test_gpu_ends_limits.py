@@ -135,3 +135,18 @@ def test_distill_rest_far_below_the_list(aq, dtype, copies, vocab):
     size = torch.where(listed, 0.0, (rest / (vocab - n))[:, None]).scatter_(1, at, (zl - log_all[:, None]).exp() + p)
     bound = size / tau * (128 + 17 + 8) * ref.E32
     ref.check(g, grad / tau, bound + ref.rounded(grad.abs() / tau + bound, dtype))
+
+
+@pytest.mark.parametrize("copies", [1, 600])
+@pytest.mark.parametrize("rest", [False, True])
+def test_distill_all_masked(aq, copies, rest):
+    """A student's row of nothing but -inf has no softmax: loss and gradient are NaN, all of it."""
+    z, t, ids, lse = distill_case(38, 3, 700, 20, F32, F32, short=False)
+    z[1] = -math.inf
+    many = [v.repeat(copies, *[1] * (v.dim() - 1)) for v in (z, t, ids, lse)]
+    loss, g = aq.distill_loss(*many[:3], teacher_lse=many[3] if rest else None, temperature=1.5)
+    assert torch.isnan(loss[1::3]).all() and torch.isnan(g[1::3]).all()
+    assert torch.isfinite(loss[0::3]).all() and torch.isfinite(g[0::3]).all()
+    assert torch.isfinite(loss[2::3]).all() and torch.isfinite(g[2::3]).all()
+    got, none = aq.distill_loss(z[1:2], t[1:2], ids[1:2], weights=torch.zeros(1, device=DEV))
+    assert float(got[0]) == 0 and not none.any()
