@@ -6,12 +6,11 @@
 #include <atomic>
 #include <cstdint>
 #include <mutex>
-#include <set>
-#include <tuple>
 
 #include "../../include/aqlm.h"
 #include "groups.h"
 #include "launch.h"
+#include "lds_limits.h"
 #include "sorted.h"
 
 namespace aqlm {
@@ -35,21 +34,17 @@ int num_cus() {
   return v;
 }
 
-// The dynamic-LDS limit is a per-device property of a kernel: raise it once
-// per (kernel, device, size), under a lock so that concurrent first calls
-// are safe.
+// The dynamic-LDS limit is a per-device property of a kernel: raise it where a call
+// needs more than was given, under a lock so that concurrent calls are safe.
 hipError_t allow_dynamic_lds(const void* kern, int bytes) {
   int dev = 0;
   const hipError_t d = hipGetDevice(&dev);
   if (d != hipSuccess) return d;
   static std::mutex mu;
-  static std::set<std::tuple<const void*, int, int>> done;
+  static LdsLimits limits;
   const std::lock_guard<std::mutex> lock(mu);
-  const auto key = std::make_tuple(kern, dev, bytes);
-  if (done.count(key)) return hipSuccess;
-  const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == hipSuccess) done.insert(key);
-  return e;
+  return limits.allow(kern, dev, bytes,
+                      [&] { return hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
 }
 
 }  // namespace aqlm

@@ -147,8 +147,8 @@ hipError_t launch_beam_search(const float* w, const float* h, uint8_t* codes, co
                               int32_t sweeps, float* loss, hipStream_t s);
 
 int num_cus();
-// Allows a kernel `bytes` of dynamic LDS on the current device (once per
-// kernel, device and size).
+// Allows a kernel `bytes` of dynamic LDS on the current device (where it has not
+// been given that much before).
 hipError_t allow_dynamic_lds(const void* kern, int bytes);
 
 }  // namespace aqlm

@@ -150,3 +150,16 @@ def test_distill_all_masked(aq, copies, rest):
     assert torch.isfinite(loss[2::3]).all() and torch.isfinite(g[2::3]).all()
     got, none = aq.distill_loss(z[1:2], t[1:2], ids[1:2], weights=torch.zeros(1, device=DEV))
     assert float(got[0]) == 0 and not none.any()
+
+
+def test_distill_long_lists_after_short_ones(aq):
+    """Lists of 2048, which need more of the processors' memory than a kernel has by itself, before and after
+    short ones."""
+    for rows, vocab in ((2, 9000), (600, 9000)):
+        z, t, ids, lse = distill_case(39, rows, vocab, 2048, F32, F32, short=False)
+        want, want_off, grad, grad_off = ref.distill(z[:2], t[:2], ids[:2], None, None, 1.5)
+        for n in (2048, 64, 2048, 1, 2048):
+            loss, g = aq.distill_loss(z, t[:, :n].contiguous(), ids[:, :n].contiguous(), temperature=1.5)
+            if n == 2048:
+                ref.check(loss[:2], want, want_off, "loss")
+                ref.check(g[:2], grad, grad_off + ref.rounded(grad.abs() + grad_off, F32), "gradient")
