@@ -127,7 +127,7 @@ def end_gradients(model, tokens, weight, teacher_logits, teacher_ids, teacher_ls
 
 def generate(model, prompts, new_tokens, *, chunk=64, page_size=16, repetition=1.3, presence=0.2, banned=(), allowed=None,
              temperature=0.0, top_p=1.0, seed=0):
-    """Continuations of the prompts (lists of ids), greedy at temperature 0: int32
+    """Continuations of the prompts (lists of ids), greedy at temperature 0: int64
     [sequences, new_tokens]."""
     dev, seqs = model.device, len(prompts)
     most = max(len(p) for p in prompts) + new_tokens
@@ -176,7 +176,7 @@ def generate(model, prompts, new_tokens, *, chunk=64, page_size=16, repetition=1
         lens += 1
         if step + 1 < new_tokens:
             logits = model.forward(token, cache, table, lens, cu, 1)
-    return torch.stack(out, 1)
+    return torch.stack(out, 1).long()
 
 
 def main():

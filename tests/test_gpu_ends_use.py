@@ -287,3 +287,11 @@ def test_example_end_gradients(aq, example):
     assert abs(float(loss) - want) <= 6 * 2.0 ** -11 * want
     for got, want in ((de, E.grad), (dw, W.grad), (dhead, H.grad)):
         assert (got.double() / 1024 - want).norm() <= 6 * 2.0 ** -11 * want.norm()
+
+
+def test_example_ids_are_indices(aq, example):
+    """Continuations are int64, as ids that torch takes as indices."""
+    model = example.Model(layers=1)
+    out = example.generate(model, [[5, 7], [13]], 2)
+    assert out.dtype == torch.int64 and out.shape == (2, 2)
+    assert model.embedding.gather(0, out).shape == (2, 2)
