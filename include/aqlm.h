@@ -710,8 +710,9 @@ int aqlm_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
  *   loss[row] = sum_k p_k log(p_k / q_k) + p_r log(p_r / q_r)                     (fp32)
  *   grad[row] = weights[row] * dloss[row] / dlogits[row]                   (logits' type)
  * (weights NULL: 1; it carries a loss scale, 1 / tokens, temperature^2).  A row whose weight
- * is 0 has loss and gradient 0, whatever its logits are; so has a row without entries (with
- * teacher_lse its whole mass is one outcome).  grad NULL: the loss alone; it may be the logits
+ * is 0 has loss and gradient 0, whatever its logits are; so has, without teacher_lse, a row
+ * without entries or whose entries' logits are all -inf, and with it a row without entries, whose whole mass is one
+ * outcome.  A row of logits that are all -inf has no softmax: NaN.  grad NULL: the loss alone; it may be the logits
  * (same address and stride).  workspace: aqlm_distill_loss_workspace_bytes(rows, vocab, listed,
  * dtype) bytes (0 for many rows that are not too long), 16-byte aligned, any contents.
  * Deterministic.  Limits: 2^22 - 1 rows, vocab 2^19, 2048 listed. */
@@ -738,7 +739,10 @@ typedef struct aqlm_sampling {
  * -inf is a masked token; a row with NaN, or with nothing else than masked tokens, gives -1.
  * logprob (NULL, or [rows]): the logarithm of the token's share of the kept mass (0 at
  * temperature 0, NaN with -1).  Weights are computed in 64 bits and added as whole multiples of
- * 2^-44: the same token whatever the batch.
+ * 2^-44 of the largest: a row's token depends on the row, its number and its rules alone, as long as
+ * the same of the four rules are given.  (Whether there is a top_k at all decides how rows of 8193 to 32768 logits are
+ * summed up; results of two such calls can differ where a number or a limit lies within vocab * 2^-44 of a
+ * border, relative to the largest weight, which is also how far any result is from that of real numbers.)
  *   workspace: aqlm_sample_workspace_bytes(rows, vocab, rules) bytes, 16-byte aligned, any
  *   contents (0, and not read, up to a vocab of 8192, or of 32768 with top_k).
  * Limits: 2^20 rows, vocab 2^19. */

@@ -8,19 +8,23 @@
 //   token   the first, in the order of numbers, at which the kept mass exceeds u times it
 //
 // Every kept set is a beginning of that order, so only its last member has to be found.
-// Weights are whole multiples of 2^-44, computed in 64 bits, and added as integers: the
-// token does not depend on an order of sums, and differs from that of real numbers
-// only where u is within about 2^-40 of a border.
+// Weights are whole multiples of 2^-44 of the largest, computed in 64 bits, and added as integers: the
+// token does not depend on the order of the atomics.  Each is off by at most 2^-44 of the largest, the mass of
+// n tokens by n 2^-44 of it (by about 2^-37 for 128256 whose roundings cancel as chance has it, by up to 2^-27
+// for as many alike): the token and the kept set are those of real numbers but where u or p lies so near a border.
+// Rows that are cut round the slices' sums once more, and their tokens to finer multiples.
 //
 // Counts and masses of the tokens by bins of T / 16 (512 of them: what is lower has no mass
 // left) show in which bin the last member lies.  The tokens down to it (or, if those are more
 // than a list holds, that bin's) are collected and sorted; the kept ones are the first of
 // them.  (A top-p of the first k has two last members: the k-th for the mass, then the limit's.)  What the list does not
-// hold either (thousands of equal logits) is found by
-// eleven bits of logit and number at a time (draw_slowly).
+// hold either is found by eleven bits of logit and number at a time (draw_slowly): thousands of equal logits; logits of
+// more than 2^25 temperatures; and, for top-k up to 256, cut rows a slice of which has more tokens than its list (512),
+// but fewer than k threads that hold any (the last 1105 of 50257 logits in 16 bits, with top-k 140 and more: a row 86 us,
+// with top-k 100 19).
 //
-// Rows of up to 32768 logits are a workgroup's each, which holds them in registers.  Longer
-// ones are cut into slices of 8192: one launch makes the slices' maxima, bins (relative to
+// Rows that are not cut are a workgroup's each, which holds them in registers (up to 32768 logits with top-k, 8192
+// without: sample_cut).  Longer ones are cut into slices of 8192: one launch makes the slices' maxima, bins (relative to
 // their own maximum) and lists of their first tokens, another joins a row's.  Bound: latency of
 // one row's phases (a row of 32000 11 us with top-k and top-p), with many rows the 64-bit
 // exponentials and the slowest row's join (128 x 128256 fp32 30 us and 30; the logits alone are 13).

@@ -102,6 +102,15 @@ def test_sample_bin_of_more_tokens_than_its_place_holds(aq):
         assert torch.equal(aq.sample(rows, u, min_p=full), kept[j].int())
 
 
+@pytest.mark.parametrize("vocab", [8192, 8193, 32000, 32768, 50001])
+def test_sample_a_top_k_of_others(aq, vocab):
+    """Rows without top-k among requests of which some bring one: summed up differently, drawn alike."""
+    x, u = rand(10, 12, vocab) * 2.5, uniform(11, 12)
+    zeros = torch.zeros(12, dtype=torch.int32, device=DEV)
+    for r in (dict(), dict(top_p=torch.full((12,), 0.9, device=DEV)), dict(min_p=torch.full((12,), 0.05, device=DEV))):
+        assert torch.equal(check_sample(aq, x, u, **r), check_sample(aq, x, u, top_k=zeros, **r))
+
+
 # --------------------------------------------------------------------------- distillation
 
 @pytest.mark.parametrize("dtype", TYPES)
