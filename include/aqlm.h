@@ -711,8 +711,10 @@ int aqlm_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
  *   grad[row] = weights[row] * dloss[row] / dlogits[row]                   (logits' type)
  * (weights NULL: 1; it carries a loss scale, 1 / tokens, temperature^2).  A row whose weight
  * is 0 has loss and gradient 0, whatever its logits are; so has, without teacher_lse, a row
- * without entries or whose entries' logits are all -inf, and with it a row without entries, whose whole mass is one
- * outcome.  A row of logits that are all -inf has no softmax: NaN.  grad NULL: the loss alone; it may be the logits
+ * without entries, or with teacher logits of nothing but -inf, and with it a row without entries (its whole
+ * mass is one outcome).  Other rows of logits that are all -inf have no softmax: NaN.  Where p_r > 0 and
+ * the logits of all tokens outside the entries are -inf, the loss is inf, and the gradient that of the entries,
+ * 0 elsewhere.  grad NULL: the loss alone; it may be the logits
  * (same address and stride).  workspace: aqlm_distill_loss_workspace_bytes(rows, vocab, listed,
  * dtype) bytes (0 for many rows that are not too long), 16-byte aligned, any contents.
  * Deterministic.  Limits: 2^22 - 1 rows, vocab 2^19, 2048 listed. */

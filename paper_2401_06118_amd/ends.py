@@ -90,10 +90,10 @@ def distill_loss(logits, teacher_logits, teacher_ids, *, teacher_lse=None, tempe
     largest logits are known: ``teacher_logits`` [rows, n] (any of the types) of the tokens
     ``teacher_ids`` (int32 [rows, n]; ids outside the vocabulary: no entry).  The teacher's
     probabilities are the softmax of the listed ones, or with ``teacher_lse`` (fp32 [rows],
-    logsumexp of all its logits / temperature) their true ones, the rest of the mass being one
-    outcome.  Returns (loss, gradient): fp32 [rows], and ``weights`` (fp32 [rows]; 1 if not given)
-    times the loss's gradient of ``logits``, of their type (None without ``grad``).  A row of
-    weight 0 has loss and gradient 0, whatever it holds.  ``out`` (the gradient's) may be
+    logsumexp of all its logits / temperature, which is held in 32 bits) their true ones, the rest of
+    the mass being one outcome.  Returns (loss, gradient): fp32 [rows], and ``weights`` (fp32
+    [rows]; 1 if not given) times the loss's gradient of ``logits``, of their type (None without
+    ``grad``).  A row of weight 0 has loss and gradient 0, whatever it holds.  ``out`` (the gradient's) may be
     ``logits`` itself."""
     r = (block._ext or _binding()).distill_loss(logits, teacher_logits, teacher_ids, teacher_lse, weights, temperature,
                                                 grad, out, _handle(logits, stream))
